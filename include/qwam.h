@@ -328,6 +328,159 @@ qwam_status qwam_aog_protected_basis(int32_t d, int32_t r, int32_t iters, const 
  * shape is not supported. */
 int64_t qwam_aog_protected_basis_workspace(int32_t d, int32_t r);
 
+/* ------------------------------------------------------------------------
+ * A single token's step: the packed layers on unquantized tokens, the norms
+ * around a block, and the paged key-value cache with its attention.  The
+ * conventions above hold, except that the alignment and finiteness asked for
+ * are those stated at each call.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Matrix-vector products with the packed 4-bit weights of a layer: for 1 to 16
+ * tokens the weights' stream is what a call costs, so the activation is not
+ * quantized:
+ *     x~      = x * inv_smooth                 (inv_smooth NULL: x)
+ *     y[m, n] = bf16( sum_g ws[g][n] sum_{k in g} x~[m, k] c[n, k]
+ *                     + sum_j t[m, j] L2t[n, j] + bias[n] ),  t = x~ . L1
+ * with the sums and t in float32; x~ enters the matrix cores as two bf16
+ * pieces (within 2^-16 of it), or as it is where inv_smooth is NULL.
+ *   L   in   packed layer: reads K, N, r, group, hadamard, wq, ws, inv_smooth,
+ *            L1f, L2t, bias.  r = 0 (no branch; L1f and L2t are not read), 16,
+ *            32, 48 or 64; hadamard 0
+ *   M   in   1 <= M <= 16 (QWAM_ERR_UNSUPPORTED above)
+ *   x   in   bf16 [M][K]
+ *   y   out  bf16 [M][N]
+ *   workspace  device memory of at least qwam_asp_matvec_workspace(L, M) bytes,
+ *            16-byte aligned (NULL where that is 0); its contents on entry do
+ *            not matter; calls that share it must not overlap
+ */
+qwam_status qwam_asp_matvec(const qwam_layer *L, int32_t M, const uint16_t *x, uint16_t *y,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace qwam_asp_matvec needs for (L, M); -1 if not supported.
+ * Reads K, N, r, group and hadamard of L only. */
+int64_t qwam_asp_matvec_workspace(const qwam_layer *L, int32_t M);
+
+/* The step between two blocks: the branch output of one joins the residual
+ * stream through its (optional) post-norm, gate and residual scale, and the
+ * pre-norm of the next block reads the sum.  Row t belongs to sample t / (T / S). */
+#define QWAM_NORM_RMS 0         /* N(v) = v / sqrt(mean(v^2) + eps)                    */
+#define QWAM_NORM_LAYER 1       /* N(v) = (v - mean(v)) / sqrt(var(v) + eps)           */
+typedef struct qwam_norm {
+    int32_t T, D, S;            /* rows, width, samples: T % S == 0, T <= 1048576, D <= 16384 */
+    int32_t kind;               /* QWAM_NORM_RMS or QWAM_NORM_LAYER, of both norms     */
+    int32_t post;               /* nonzero: the branch is normalized before its gate    */
+    int32_t x_f32;              /* residual stream: nonzero float32, 0 bf16             */
+    float eps;                  /* >= 0, finite                                        */
+    float residual_scale;       /* a, finite                                           */
+    const uint16_t *gate;       /* bf16 [S] rows of D, or NULL for 1                    */
+    const uint16_t *scale;      /* bf16 [S] rows of D, or NULL for 0                    */
+    const uint16_t *shift;      /* bf16 [S] rows of D, or NULL for 0                    */
+    int64_t gate_stride, scale_stride, shift_stride;   /* elements between samples       */
+    const uint16_t *post_weight;/* bf16 [D] or NULL for 1; read with post only          */
+    const uint16_t *weight;     /* bf16 [D] or NULL for 1                               */
+} qwam_norm;
+
+/*
+ * x' = a x + gate u,  u = branch or N(branch) * post_weight
+ * h  = N(x') * weight * (1 + scale) + shift
+ * All in float32 from the inputs; x' and h are each rounded once (h from the
+ * unrounded x').  With branch NULL, x' is x (gate and residual_scale are not
+ * read) and x_out must be NULL: the norm in front of the first block.
+ * x, branch, x_out and h need no alignment beyond their elements' (rows whose
+ * addresses are not multiples of 16 bytes are read element by element).
+ *   x      in   bf16 or float [T][D]
+ *   branch in   bf16 [T][D] or NULL
+ *   x_out  out  as x; may be x itself
+ *   h      out  bf16 [T][D]
+ */
+qwam_status qwam_block_norm(const qwam_norm *p, const void *x, const uint16_t *branch, void *x_out,
+                            uint16_t *h, void *stream);
+
+/*
+ * The gradients of qwam_block_norm at the stored x' (x_out): given those of x'
+ * (dx_out, or NULL for none) and of h (dh),
+ *     d  = dx_out + the gradient of x' through h
+ *     dx = a d;  dbranch = the gradient of gate * u at d
+ * and, for every parameter whose pointer is set, its sum over the rows it
+ * serves, in float32 and in an order that does not change from call to call:
+ * dgate, dscale, dshift [S][D], dpost_weight, dweight [D].  With branch NULL,
+ * dx = d and dbranch, dgate and dpost_weight must be NULL.
+ *   workspace  as for qwam_asp_matvec, qwam_block_norm_backward_workspace(p) bytes
+ */
+qwam_status qwam_block_norm_backward(const qwam_norm *p, const void *dx_out, const uint16_t *dh,
+                                     const void *x_out, const uint16_t *branch, void *dx,
+                                     uint16_t *dbranch, float *dgate, float *dscale, float *dshift,
+                                     float *dpost_weight, float *dweight, void *workspace,
+                                     int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of qwam_block_norm_backward; -1 if the shape is not
+ * supported.  Reads T, D and S only. */
+int64_t qwam_block_norm_backward_workspace(const qwam_norm *p);
+
+/* A paged key-value cache: position p of sequence s lies in row p % page_size
+ * of page table[s][p / page_size].  A table entry outside [0, pages) means no
+ * page: nothing is stored there and attention does not see its positions. */
+#define QWAM_CACHE_BF16 0
+#define QWAM_CACHE_FP8 1        /* e4m3 (finite, no infinities); value = code * scale[head]  */
+typedef struct qwam_cache {
+    int32_t pages;              /* pages in k and v                                     */
+    int32_t page_size;          /* positions of a page: a power of two, 16 .. 4096      */
+    int32_t heads;              /* key heads                                            */
+    int32_t dim;                /* head width, % 8 == 0 (fp8: % 16), 8 .. 256           */
+    int32_t type;               /* QWAM_CACHE_BF16 or QWAM_CACHE_FP8                    */
+    int32_t seqs;               /* rows of the table                                    */
+    int32_t table_width;        /* entries of a row; the first table_width * page_size  */
+                                /* positions of a sequence exist (below 2^31)           */
+    int32_t reserved;           /* 0                                                    */
+    int64_t page_stride, head_stride, row_stride;   /* elements between pages, heads and rows;  */
+                                /* multiples of 8 (fp8: 16), the same for k and v        */
+    void *k, *v;                /* 16-byte aligned                                      */
+    const float *k_scale, *v_scale;                 /* float [heads] (fp8), else not read   */
+    const int32_t *table;       /* [seqs][table_width]                                  */
+} qwam_cache;
+
+/*
+ * New keys and values into the pages: token t goes to position pos[t] of
+ * sequence seq[t].  fp8: code = e4m3(clamp(x / scale[head], -448, 448)), to
+ * nearest, ties to even.  A token whose sequence or position does not exist,
+ * or whose page does not, is not stored (a negative pos marks padding).  Two
+ * tokens of one call must not share a slot.
+ *   tokens   in  >= 1, tokens * heads * dim <= 2^32
+ *   k, v     in  bf16, token t's heads x dim values at t * k_stride (v_stride),
+ *                16-byte aligned, strides % 8 == 0
+ *   seq, pos in  int32 [tokens]
+ */
+qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *k, int64_t k_stride,
+                           const uint16_t *v, int64_t v_stride, const int32_t *seq,
+                           const int32_t *pos, void *stream);
+
+/*
+ * Attention of one new token per sequence over its pages:
+ *     o[b][h] = sum_p softmax_p(scale * q[b][h] . K[b][p][h / G]) V[b][p][h / G]
+ * over the positions start <= p < length, G = q_heads / heads; zeros where
+ * there are none.  Scores, the softmax's maximum and sum, and o in float32;
+ * its weights enter the product with V as two bf16 pieces; o is rounded once.
+ * Values outside the visible positions (NaN, infinities) have no effect.
+ *   q        in  bf16, sequence b's q_heads x dim values at b * q_stride,
+ *                16-byte aligned, q_stride % 8 == 0
+ *   q_heads  in  a multiple of heads, at most 64 per key head, seqs * q_heads <= 2^22
+ *   lengths  in  int32 [seqs], taken as at most max_len and the table's reach,
+ *                and below 0 as 0
+ *   starts   in  int32 [seqs], or NULL for 0
+ *   max_len  in  1 .. table_width * page_size: the call's work is laid out for it
+ *   out      out bf16 [seqs][q_heads][dim]
+ *   workspace  as for qwam_asp_matvec, qwam_paged_attention_workspace bytes
+ */
+qwam_status qwam_paged_attention(const qwam_cache *c, int32_t q_heads, const uint16_t *q,
+                                 int64_t q_stride, const int32_t *lengths, const int32_t *starts,
+                                 int32_t max_len, float scale, uint16_t *out, void *workspace,
+                                 int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of qwam_paged_attention; -1 if not supported.  Reads
+ * the cache's integers only. */
+int64_t qwam_paged_attention_workspace(const qwam_cache *c, int32_t q_heads, int32_t max_len);
+
 /* Message describing the calling thread's last non-OK status ("" if none). */
 const char *qwam_last_error(void);
 

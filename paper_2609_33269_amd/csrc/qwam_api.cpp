@@ -331,6 +331,265 @@ qwam_status qwam_aog_protected_basis(int32_t d, int32_t r, int32_t iters, const 
                                            static_cast<hipStream_t>(stream)));
 }
 
+}  // extern "C"
+
+namespace {
+
+qwam_status check_workspace(const char* fn, const void* workspace, int64_t bytes, int64_t need) {
+  if (need <= 0) return QWAM_OK;
+  if (workspace == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: workspace is NULL", fn);
+  if (!aligned16(workspace)) return fail(QWAM_ERR_MISALIGNED, "%s: workspace is not 16-byte aligned", fn);
+  if (bytes < need)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld needed", fn, static_cast<long long>(bytes),
+                static_cast<long long>(need));
+  return QWAM_OK;
+}
+
+qwam_status check_matvec(const char* fn, const qwam_layer* L, int32_t M) {
+  qwam_status s = check_layer(fn, L, false);
+  if (s != QWAM_OK) return s;
+  if (L->r < 0 || L->r > 64 || L->r % 16 != 0)
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: rank r must be 0, 16, 32, 48 or 64 (got %d)", fn, L->r);
+  if (L->hadamard != 0) return fail(QWAM_ERR_UNSUPPORTED, "%s: layers without rotation only", fn);
+  if ((s = check_m(fn, M)) != QWAM_OK) return s;
+  if (M > qwam::kMatvecMaxM) return fail(QWAM_ERR_UNSUPPORTED, "%s: M = %d exceeds %d", fn, M, qwam::kMatvecMaxM);
+  if (static_cast<int64_t>(L->N) * (L->K / L->group) >= (int64_t(1) << 29))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: N*K/group must be below 2^29", fn);
+  return QWAM_OK;
+}
+
+bool finite(float v) { return v - v == 0.0f; }
+
+// elements of `bytes` bytes each lie at multiples of their size
+bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+#define QWAM_REQUIRE_ELEM(p, bytes)                                                                                  \
+  do {                                                                                                               \
+    if ((p) == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: %s is NULL", fn, #p);                                 \
+    if (!aligned_to(p, bytes)) return fail(QWAM_ERR_MISALIGNED, "%s: %s is not aligned to its elements", fn, #p);    \
+  } while (0)
+#define QWAM_OPTIONAL_ELEM(p, bytes) \
+  do {                               \
+    if ((p) != nullptr) QWAM_REQUIRE_ELEM(p, bytes); \
+  } while (0)
+
+qwam_status check_norm_shape(const char* fn, const qwam_norm* p) {
+  if (p == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: p is NULL", fn);
+  if (p->T <= 0 || p->S <= 0 || p->T % p->S != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: T must be a positive multiple of S (got %d, %d)", fn, p->T, p->S);
+  if (p->D <= 0) return fail(QWAM_ERR_INVALID_ARG, "%s: D must be >= 1 (got %d)", fn, p->D);
+  if (p->D > qwam::kNormMaxD) return fail(QWAM_ERR_UNSUPPORTED, "%s: D = %d exceeds %d", fn, p->D, qwam::kNormMaxD);
+  if (p->T > kMaxM) return fail(QWAM_ERR_UNSUPPORTED, "%s: T = %d exceeds %d", fn, p->T, kMaxM);
+  return QWAM_OK;
+}
+
+qwam_status check_norm(const char* fn, const qwam_norm* p, qwam::NormParams* out) {
+  qwam_status s = check_norm_shape(fn, p);
+  if (s != QWAM_OK) return s;
+  if (p->kind != QWAM_NORM_RMS && p->kind != QWAM_NORM_LAYER)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: kind must be QWAM_NORM_RMS or QWAM_NORM_LAYER (got %d)", fn, p->kind);
+  if (!(p->eps >= 0.0f) || !finite(p->eps)) return fail(QWAM_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", fn);
+  if (!finite(p->residual_scale)) return fail(QWAM_ERR_INVALID_ARG, "%s: residual_scale must be finite", fn);
+  QWAM_OPTIONAL_ELEM(p->gate, 2);
+  QWAM_OPTIONAL_ELEM(p->scale, 2);
+  QWAM_OPTIONAL_ELEM(p->shift, 2);
+  QWAM_OPTIONAL_ELEM(p->post_weight, 2);
+  QWAM_OPTIONAL_ELEM(p->weight, 2);
+  *out = {p->D, p->T / p->S, p->kind == QWAM_NORM_LAYER, p->post != 0, p->x_f32 != 0, p->eps, p->residual_scale,
+          p->gate, p->scale, p->shift, p->gate_stride, p->scale_stride, p->shift_stride, p->post_weight, p->weight};
+  return QWAM_OK;
+}
+
+// the cache's integers
+qwam_status check_cache_shape(const char* fn, const qwam_cache* c, qwam::CacheParams* out) {
+  if (c == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: cache is NULL", fn);
+  if (c->type != QWAM_CACHE_BF16 && c->type != QWAM_CACHE_FP8)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: type must be QWAM_CACHE_BF16 or QWAM_CACHE_FP8 (got %d)", fn, c->type);
+  const int32_t step = c->type == QWAM_CACHE_FP8 ? 16 : 8;
+  if (c->pages <= 0 || c->heads <= 0 || c->seqs <= 0 || c->table_width <= 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: pages, heads, seqs and table_width must be >= 1", fn);
+  if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: page_size must be a power of two in [16, 4096] (got %d)", fn, c->page_size);
+  if (c->dim <= 0 || c->dim % step != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: dim must be a positive multiple of %d (got %d)", fn, step, c->dim);
+  if (c->dim > 256) return fail(QWAM_ERR_UNSUPPORTED, "%s: dim = %d exceeds 256", fn, c->dim);
+  if (c->heads > 4096 || c->seqs > 65535)
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: at most 4096 heads and 65535 sequences", fn);
+  if (static_cast<int64_t>(c->table_width) * c->page_size > INT32_MAX)
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: table_width * page_size must be below 2^31", fn);
+  if (c->reserved != 0) return fail(QWAM_ERR_INVALID_ARG, "%s: reserved must be 0", fn);
+  if (c->page_stride % step != 0 || c->head_stride % step != 0 || c->row_stride % step != 0)
+    return fail(QWAM_ERR_MISALIGNED, "%s: the cache's strides must be multiples of %d", fn, step);
+  *out = {c->pages, __builtin_ctz(static_cast<unsigned>(c->page_size)), c->heads, c->dim, c->seqs, c->table_width,
+          c->page_stride, c->head_stride, c->row_stride, c->k, c->v, c->k_scale, c->v_scale, c->table};
+  return QWAM_OK;
+}
+
+qwam_status check_cache(const char* fn, const qwam_cache* c, qwam::CacheParams* out) {
+  qwam_status s = check_cache_shape(fn, c, out);
+  if (s != QWAM_OK) return s;
+  QWAM_REQUIRE_PTR(c->k);
+  QWAM_REQUIRE_PTR(c->v);
+  QWAM_REQUIRE_ELEM(c->table, 4);
+  if (c->type == QWAM_CACHE_FP8) {
+    QWAM_REQUIRE_ELEM(c->k_scale, 4);
+    QWAM_REQUIRE_ELEM(c->v_scale, 4);
+  }
+  return QWAM_OK;
+}
+
+qwam_status check_attention(const char* fn, const qwam_cache* c, int32_t q_heads, int32_t max_len) {
+  if (q_heads <= 0 || q_heads % c->heads != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: q_heads must be a positive multiple of heads (got %d, %d)", fn, q_heads, c->heads);
+  if (q_heads / c->heads > qwam::kMaxHeadGroup)
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: more than %d query heads per key head", fn, qwam::kMaxHeadGroup);
+  if (static_cast<int64_t>(c->seqs) * q_heads > (1 << 22))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: seqs * q_heads must be at most 2^22", fn);
+  if (max_len < 1 || max_len > static_cast<int64_t>(c->table_width) * c->page_size)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: max_len must be in [1, table_width * page_size] (got %d)", fn, max_len);
+  return QWAM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t qwam_asp_matvec_workspace(const qwam_layer* L, int32_t M) {
+  if (check_matvec("qwam_asp_matvec_workspace", L, M) != QWAM_OK) return -1;
+  ok();
+  return qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->group);
+}
+
+qwam_status qwam_asp_matvec(const qwam_layer* L, int32_t M, const uint16_t* x, uint16_t* y, void* workspace,
+                            int64_t workspace_bytes, void* stream) {
+  const char* fn = "qwam_asp_matvec";
+  qwam_status s = check_matvec(fn, L, M);
+  if (s != QWAM_OK) return s;
+  QWAM_REQUIRE_PTR(L->wq);
+  QWAM_REQUIRE_PTR(L->ws);
+  if (L->r > 0) {
+    QWAM_REQUIRE_PTR(L->L1f);
+    QWAM_REQUIRE_PTR(L->L2t);
+  }
+  if (L->inv_smooth != nullptr && !aligned16(L->inv_smooth))
+    return fail(QWAM_ERR_MISALIGNED, "%s: inv_smooth is not 16-byte aligned", fn);
+  if (L->bias != nullptr && !aligned16(L->bias))
+    return fail(QWAM_ERR_MISALIGNED, "%s: bias is not 16-byte aligned", fn);
+  QWAM_REQUIRE_PTR(x);
+  QWAM_REQUIRE_PTR(y);
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->group))) != QWAM_OK)
+    return s;
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_asp_matvec(M, L->N, L->K, L->r, L->group, x, L->inv_smooth, L->L1f, L->wq, L->ws, L->L2t,
+                                              L->bias, y, workspace, static_cast<hipStream_t>(stream)));
+}
+
+qwam_status qwam_block_norm(const qwam_norm* p, const void* x, const uint16_t* branch, void* x_out, uint16_t* h, void* stream) {
+  const char* fn = "qwam_block_norm";
+  qwam::NormParams np;
+  qwam_status s = check_norm(fn, p, &np);
+  if (s != QWAM_OK) return s;
+  const uintptr_t xe = np.x_f32 ? 4 : 2;
+  QWAM_REQUIRE_ELEM(x, xe);
+  QWAM_REQUIRE_ELEM(h, 2);
+  if (branch != nullptr) {
+    QWAM_REQUIRE_ELEM(branch, 2);
+    QWAM_REQUIRE_ELEM(x_out, xe);
+  } else if (x_out != nullptr) {
+    return fail(QWAM_ERR_INVALID_ARG, "%s: x_out without a branch", fn);
+  }
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_block_norm(np, p->T, x, branch, x_out, h, static_cast<hipStream_t>(stream)));
+}
+
+int64_t qwam_block_norm_backward_workspace(const qwam_norm* p) {
+  if (check_norm_shape("qwam_block_norm_backward_workspace", p) != QWAM_OK) return -1;
+  ok();
+  return qwam::block_norm_bwd_workspace_bytes(p->T, p->D, p->S);
+}
+
+qwam_status qwam_block_norm_backward(const qwam_norm* p, const void* dx_out, const uint16_t* dh, const void* x_out,
+                                     const uint16_t* branch, void* dx, uint16_t* dbranch, float* dgate, float* dscale,
+                                     float* dshift, float* dpost_weight, float* dweight, void* workspace,
+                                     int64_t workspace_bytes, void* stream) {
+  const char* fn = "qwam_block_norm_backward";
+  qwam::NormParams np;
+  qwam_status s = check_norm(fn, p, &np);
+  if (s != QWAM_OK) return s;
+  const uintptr_t xe = np.x_f32 ? 4 : 2;
+  QWAM_OPTIONAL_ELEM(dx_out, xe);
+  QWAM_REQUIRE_ELEM(dh, 2);
+  QWAM_REQUIRE_ELEM(x_out, xe);
+  QWAM_OPTIONAL_ELEM(branch, 2);
+  QWAM_REQUIRE_ELEM(dx, xe);
+  QWAM_OPTIONAL_ELEM(dbranch, 2);
+  QWAM_OPTIONAL_ELEM(dgate, 4);
+  QWAM_OPTIONAL_ELEM(dscale, 4);
+  QWAM_OPTIONAL_ELEM(dshift, 4);
+  QWAM_OPTIONAL_ELEM(dpost_weight, 4);
+  QWAM_OPTIONAL_ELEM(dweight, 4);
+  if (branch == nullptr && (dbranch != nullptr || dgate != nullptr || dpost_weight != nullptr))
+    return fail(QWAM_ERR_INVALID_ARG, "%s: dbranch, dgate or dpost_weight without a branch", fn);
+  if (!np.post && dpost_weight != nullptr)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: dpost_weight without a post-norm", fn);
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::block_norm_bwd_workspace_bytes(p->T, p->D, p->S))) != QWAM_OK)
+    return s;
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_block_norm_bwd(np, p->T, dx_out, dh, x_out, branch, dx, dbranch, dgate, dscale, dshift,
+                                                  dpost_weight, dweight, workspace, static_cast<hipStream_t>(stream)));
+}
+
+qwam_status qwam_kv_append(const qwam_cache* c, int32_t tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                           int64_t v_stride, const int32_t* seq, const int32_t* pos, void* stream) {
+  const char* fn = "qwam_kv_append";
+  qwam::CacheParams cp;
+  qwam_status s = check_cache(fn, c, &cp);
+  if (s != QWAM_OK) return s;
+  if (tokens <= 0) return fail(QWAM_ERR_INVALID_ARG, "%s: tokens must be >= 1 (got %d)", fn, tokens);
+  if (static_cast<int64_t>(tokens) * c->heads * c->dim > (int64_t(1) << 32))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: tokens * heads * dim must be at most 2^32", fn);
+  QWAM_REQUIRE_PTR(k);
+  QWAM_REQUIRE_PTR(v);
+  if (k_stride % 8 != 0 || v_stride % 8 != 0)
+    return fail(QWAM_ERR_MISALIGNED, "%s: k_stride and v_stride must be multiples of 8", fn);
+  QWAM_REQUIRE_ELEM(seq, 4);
+  QWAM_REQUIRE_ELEM(pos, 4);
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_kv_append(cp, c->type == QWAM_CACHE_FP8, tokens, k, k_stride, v, v_stride, seq, pos,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+int64_t qwam_paged_attention_workspace(const qwam_cache* c, int32_t q_heads, int32_t max_len) {
+  const char* fn = "qwam_paged_attention_workspace";
+  qwam::CacheParams cp;
+  if (check_cache_shape(fn, c, &cp) != QWAM_OK || check_attention(fn, c, q_heads, max_len) != QWAM_OK) return -1;
+  ok();
+  return qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len);
+}
+
+qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uint16_t* q, int64_t q_stride,
+                                 const int32_t* lengths, const int32_t* starts, int32_t max_len, float scale, uint16_t* out,
+                                 void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* fn = "qwam_paged_attention";
+  qwam::CacheParams cp;
+  qwam_status s = check_cache(fn, c, &cp);
+  if (s != QWAM_OK) return s;
+  if ((s = check_attention(fn, c, q_heads, max_len)) != QWAM_OK) return s;
+  if (!finite(scale)) return fail(QWAM_ERR_INVALID_ARG, "%s: scale must be finite", fn);
+  QWAM_REQUIRE_PTR(q);
+  if (q_stride % 8 != 0) return fail(QWAM_ERR_MISALIGNED, "%s: q_stride must be a multiple of 8", fn);
+  QWAM_REQUIRE_ELEM(lengths, 4);
+  QWAM_OPTIONAL_ELEM(starts, 4);
+  QWAM_REQUIRE_PTR(out);
+  const bool fp8 = c->type == QWAM_CACHE_FP8;
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, fp8, q_heads, max_len))) !=
+      QWAM_OK)
+    return s;
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_paged_attention(cp, fp8, q_heads, q, q_stride, lengths, starts, max_len, scale, out, workspace,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
 const char* qwam_last_error(void) { return g_err; }
 
 const char* qwam_status_string(qwam_status s) {

@@ -103,4 +103,49 @@ hipError_t launch_asp_layer_small(int M, int N, int K, int r, const uint16_t* x,
 hipError_t launch_group_partials_small(int M, int N, int K, int group, const uint8_t* xq, const uint8_t* wq,
                                        int32_t* P, hipStream_t stream);
 
+// ---- a single token's step ----
+
+// y = x~ . dequantized weights + the branch + bias for M <= kMatvecMaxM tokens
+// (r = 0: no branch; inv_smooth null: x~ = x); the workspace may be null where
+// matvec_workspace_bytes is 0
+constexpr int kMatvecMaxM = 16;
+int64_t matvec_workspace_bytes(int M, int N, int K, int r, int group);
+hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, const uint16_t* x, const float* inv_smooth,
+                             const uint16_t* L1f, const uint8_t* wq, const float* ws, const uint16_t* L2t,
+                             const uint16_t* bias, uint16_t* y, void* workspace, hipStream_t stream);
+
+constexpr int kNormMaxD = 16384;
+
+// qwam_norm as the kernels take it: `rows` rows per sample
+struct NormParams {
+  int D, rows;
+  bool layer, post, x_f32;
+  float eps, residual_scale;
+  const uint16_t *gate, *scale, *shift;
+  int64_t gate_stride, scale_stride, shift_stride;
+  const uint16_t *post_weight, *weight;
+};
+hipError_t launch_block_norm(const NormParams& p, int T, const void* x, const uint16_t* branch, void* xo, uint16_t* h,
+                             hipStream_t stream);
+int64_t block_norm_bwd_workspace_bytes(int T, int D, int S);
+hipError_t launch_block_norm_bwd(const NormParams& p, int T, const void* dxo, const uint16_t* dh, const void* xo,
+                                 const uint16_t* branch, void* dx, uint16_t* dbranch, float* dgate, float* dscale, float* dshift,
+                                 float* dpost_weight, float* dweight, void* workspace, hipStream_t stream);
+
+// qwam_cache as the kernels take it: pages of 1 << page_bits rows
+struct CacheParams {
+  int pages, page_bits, heads, dim, seqs, table_width;
+  int64_t page_stride, head_stride, row_stride;
+  void *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t* table;
+};
+constexpr int kMaxHeadGroup = 64;      // query heads per key head
+hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                            int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream);
+int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len);
+hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
+                                  const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
+                                  void* workspace, hipStream_t stream);
+
 }  // namespace qwam

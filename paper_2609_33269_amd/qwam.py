@@ -13,7 +13,8 @@ argument that is wrong.
 
 Names follow the C ABI (include/qwam.h): pack_weights, quantize_act,
 quantize_act_deflated (both over qwam_quantize_act_ws), asp_linear, asp_layer, debug_group_partials,
-aog_accumulate, aog_protected_basis; and the measurement probes of include/qwam_probe.h:
+asp_matvec, aog_accumulate, aog_protected_basis; block.py holds the norms around a block and
+the paged key-value cache; and the measurement probes of include/qwam_probe.h:
 probe_mfma, probe_valu_fma, probe_copy, probe_empty, probe_gemm_form.
 """
 
@@ -45,7 +46,23 @@ class QwamLayerC(ctypes.Structure):
                 ("wsp", ctypes.c_void_p), ("L1f", ctypes.c_void_p)]
 
 
+class QwamNormC(ctypes.Structure):
+    _fields_ = [("T", _i32), ("D", _i32), ("S", _i32), ("kind", _i32), ("post", _i32), ("x_f32", _i32),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("gate", _c_void_p), ("scale", _c_void_p),
+                ("shift", _c_void_p), ("gate_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+                ("shift_stride", ctypes.c_int64), ("post_weight", _c_void_p), ("weight", _c_void_p)]
+
+
+class QwamCacheC(ctypes.Structure):
+    _fields_ = [("pages", _i32), ("page_size", _i32), ("heads", _i32), ("dim", _i32), ("type", _i32), ("seqs", _i32),
+                ("table_width", _i32), ("reserved", _i32), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("k", _c_void_p), ("v", _c_void_p), ("k_scale", _c_void_p),
+                ("v_scale", _c_void_p), ("table", _c_void_p)]
+
+
 _LP = ctypes.POINTER(QwamLayerC)
+_NP = ctypes.POINTER(QwamNormC)
+_CP = ctypes.POINTER(QwamCacheC)
 SIGNATURES = {
     "qwam_pack_weights": (ctypes.c_int, [_i32, _i32, _i32, _c_void_p, _c_void_p, _c_void_p,
                                          _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
@@ -61,6 +78,16 @@ SIGNATURES = {
     "qwam_debug_group_partials": (ctypes.c_int, [_LP, _i32, _c_void_p, _c_void_p, _c_void_p]),
     "qwam_asp_layer": (ctypes.c_int, [_LP, _i32, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
                                       _c_void_p]),
+    "qwam_asp_matvec": (ctypes.c_int, [_LP, _i32, _c_void_p, _c_void_p, _c_void_p, ctypes.c_int64, _c_void_p]),
+    "qwam_asp_matvec_workspace": (ctypes.c_int64, [_LP, _i32]),
+    "qwam_block_norm": (ctypes.c_int, [_NP, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
+    "qwam_block_norm_backward": (ctypes.c_int, [_NP] + [_c_void_p] * 12 + [ctypes.c_int64, _c_void_p]),
+    "qwam_block_norm_backward_workspace": (ctypes.c_int64, [_NP]),
+    "qwam_kv_append": (ctypes.c_int, [_CP, _i32, _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64, _c_void_p, _c_void_p,
+                                      _c_void_p]),
+    "qwam_paged_attention": (ctypes.c_int, [_CP, _i32, _c_void_p, ctypes.c_int64, _c_void_p, _c_void_p, _i32, ctypes.c_float,
+                                            _c_void_p, _c_void_p, ctypes.c_int64, _c_void_p]),
+    "qwam_paged_attention_workspace": (ctypes.c_int64, [_CP, _i32, _i32]),
     "qwam_aog_accumulate": (ctypes.c_int, [_i32, _i32, _c_void_p, _c_void_p, _c_void_p]),
     "qwam_aog_protected_basis": (ctypes.c_int, [_i32, _i32, _i32, _c_void_p, ctypes.c_float, _c_void_p, _i32,
                                                 _c_void_p, _c_void_p, _c_void_p, ctypes.c_int64, _c_void_p]),
@@ -151,9 +178,9 @@ class PackedLayer:
     r: int
     wq: torch.Tensor          # uint8 [N][K/2]
     ws: torch.Tensor          # float32 [K/64][N]
-    inv_smooth: torch.Tensor  # float32 [K]
-    L1t: torch.Tensor         # bf16 [r][K]
-    L2t: torch.Tensor         # bf16 [N][r]
+    inv_smooth: Optional[torch.Tensor]   # float32 [K]; None: no smoothing (asp_matvec only)
+    L1t: Optional[torch.Tensor]          # bf16 [r][K]; None with r = 0, a layer without a branch (asp_matvec only)
+    L2t: Optional[torch.Tensor]          # bf16 [N][r]; None with r = 0
     bias: Optional[torch.Tensor] = None   # bf16 [N]
     hadamard: int = 0                     # block size of the rotation (Eq. 3), 0 = none
     group: int = GROUP                    # channels per scale: 64, or 32 (App. B.1)
@@ -161,15 +188,17 @@ class PackedLayer:
     wsp: Optional[torch.Tensor] = None    # int32 [K/group][N]: ws as bf16 pieces hi | lo << 16 (asp_linear reads it)
     L1f: Optional[torch.Tensor] = None    # bf16 [K/64][r/16][2][64][8]: L1 in fragment order (the activation calls read it)
 
-    def c_struct(self) -> QwamLayerC:
+    def c_struct(self, matvec: bool = False) -> QwamLayerC:
         G = self.K // self.group
         c = QwamLayerC()
         c.K, c.N, c.r, c.group, c.hadamard = self.K, self.N, self.r, self.group, self.hadamard
         c.wq = _req(self.wq, "wq", torch.uint8, (self.N, self.K // 2))
         c.ws = _req(self.ws, "ws", torch.float32, (G, self.N))
-        c.inv_smooth = _req(self.inv_smooth, "inv_smooth", torch.float32, (self.K,))
-        c.L1t = _req(self.L1t, "L1t", torch.bfloat16, (self.r, self.K))
-        c.L2t = _req(self.L2t, "L2t", torch.bfloat16, (self.N, self.r))
+        if not (matvec and self.inv_smooth is None):
+            c.inv_smooth = _req(self.inv_smooth, "inv_smooth", torch.float32, (self.K,))
+        if not (matvec and self.r == 0):
+            c.L1t = _req(self.L1t, "L1t", torch.bfloat16, (self.r, self.K))
+            c.L2t = _req(self.L2t, "L2t", torch.bfloat16, (self.N, self.r))
         c.bias = None if self.bias is None else _req(self.bias, "bias", torch.bfloat16, (self.N,))
         c.L1 = None if self.L1 is None else _req(self.L1, "L1", torch.bfloat16, (self.K, self.r))
         c.wsp = None if self.wsp is None else _req(self.wsp, "wsp", torch.int32, (G, self.N))
@@ -220,6 +249,15 @@ def make_layer(R: torch.Tensor, smooth: torch.Tensor, L1: torch.Tensor, L2: torc
                        bias=None if bias is None else bias.contiguous(), hadamard=hadamard, group=group)
 
 
+def make_plain_layer(W: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None, group: int = GROUP) -> PackedLayer:
+    """A 4-bit layer without smoothing and branch (r = 0), for asp_matvec: W float32 [N][K] packed with the quantizer
+    of the ASP layers."""
+    N, K = W.shape
+    wq, ws, wsp, _ = pack_weights(W, torch.ones(K, dtype=torch.float32, device=W.device), stream, group)
+    return PackedLayer(K=K, N=N, r=0, wq=wq, ws=ws, wsp=wsp, inv_smooth=None, L1t=None, L2t=None,
+                       bias=None if bias is None else bias.contiguous(), group=group)
+
+
 def quantize_act(layer: PackedLayer, x: torch.Tensor, stream=None, out=None):
     """qwam_quantize_act: x bf16 [M][K] -> (xq uint8 [M][K/2], xs float32 [K/64][M], t bf16 [M][r]).
 
@@ -237,12 +275,17 @@ def _workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
     """Device memory for one call on `stream`.  It is taken from the allocator's
     pool of the stream the call runs on: when it is dropped after the call, the
     next user of that memory runs behind the call's kernels."""
-    if nbytes <= 0:
-        return None
+    return None if nbytes <= 0 else _empty((nbytes,), torch.uint8, device, stream)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor from the allocator's pool of the stream that will write it."""
     if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        raise TypeError("stream must be a torch.cuda.Stream: a bare handle has no pool to take memory from")
     with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _quantize(deflated: bool, name: str, layer: PackedLayer, x: torch.Tensor, stream, out):
@@ -327,6 +370,28 @@ def asp_layer(layer: PackedLayer, x: torch.Tensor, out=None, act_out=None, strea
     st = lib().qwam_asp_layer(ctypes.byref(c), M, _req(x, "x", torch.bfloat16, (M, layer.K)),
                               _req(y, "y", torch.bfloat16, (M, layer.N)), pq, ps, pt, _stream_ptr(stream))
     _check("qwam_asp_layer", st)
+    return y
+
+
+def _need(fn: str, nbytes: int) -> int:
+    """A workspace query's answer; raises where the query refused."""
+    if nbytes < 0:
+        raise QwamError(fn, 2, lib().qwam_last_error().decode())
+    return int(nbytes)
+
+
+def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """qwam_asp_matvec: the packed layer on 1 to 16 tokens without quantizing them.  x bf16 [M][K] -> y bf16 [M][N].
+    `stream` is a torch.cuda.Stream (y and the workspace come from its pool)."""
+    M = x.shape[0]
+    c = layer.c_struct(matvec=True)
+    px = _req(x, "x", torch.bfloat16, (M, layer.K))
+    need = _need("qwam_asp_matvec", lib().qwam_asp_matvec_workspace(ctypes.byref(c), M))
+    y = _empty((M, layer.N), torch.bfloat16, x.device, stream) if out is None else out
+    ws = _workspace(need, x.device, stream)
+    st = lib().qwam_asp_matvec(ctypes.byref(c), M, px, _req(y, "y", torch.bfloat16, (M, layer.N)),
+                               None if ws is None else ws.data_ptr(), need, _stream_ptr(stream))
+    _check("qwam_asp_matvec", st)
     return y
 
 
