@@ -132,6 +132,13 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
     (their rows may be apart: a slice of a modulation's wider output); post_weight, weight bf16 [D].  Each of them may be
     None.  Returns (x' as x, h bf16); without a branch (the norm in front of the first block), (None, h) with x' = x.
     `out` = (x', h) gives the outputs; x' may be x itself."""
+    if stream is None and out is None and norm in NORM_KINDS:
+        done = (_q._call or _q._native()).norm(x, branch, NORM_KINDS[norm], float(eps), float(residual_scale), gate, bool(post_norm),
+                                               post_weight, weight, scale, shift)
+        if done is not None:
+            if type(done) is int:
+                _q._check("qwam_block_norm", done)
+            return done
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (x, branch, gate, post_weight, weight, scale, shift)):
         if out is not None or stream is not None:
@@ -149,6 +156,14 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
     (None: none) and of h.  Returns a dict with dx (as x'), dbranch (bf16), and float32 dgate, dscale, dshift [S][D] and
     dpost_weight, dweight [D] for the parameters given (None for the others).  `wanted` limits the parameters' and the
     branch's gradients to those named."""
+    if stream is None and wanted is None and norm in NORM_KINDS:
+        done = (_q._call or _q._native()).norm_backward(dx_out, dh, x_out, branch, NORM_KINDS[norm], float(eps),
+                                                        float(residual_scale), gate, bool(post_norm), post_weight, weight,
+                                                        scale, shift)
+        if done is not None:
+            if type(done) is int:
+                _q._check("qwam_block_norm_backward", done)
+            return done
     T, D = x_out.shape
     c = _norm_struct(x_out, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift)
     dev = x_out.device
@@ -245,6 +260,11 @@ def _rows(t: torch.Tensor, name: str, shape) -> int:
 def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None) -> None:
     """qwam_kv_append: k, v bf16 [tokens][heads][dim] to position pos[t] of sequence seq[t] (int32 [tokens]), rounded to
     float8 where the pages are.  Tokens without a place (pos < 0, no page) are not stored."""
+    if stream is None:
+        st = (_q._call or _q._native()).append(cache, k, v, seq, pos)
+        if st is not None:
+            _q._check("qwam_kv_append", st)
+            return
     c = cache.c_struct()
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor of three dimensions (tokens, heads, dim)")
@@ -263,6 +283,12 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
     Sequence b sees positions starts[b] (0) to lengths[b] (int32 [sequences]); one that sees none gives zeros.  `scale`
     is dim ** -0.5 unless given.  `max_len` bounds the lengths (the table's reach unless given): the work is laid out
     for it, and positions past it are not seen."""
+    if stream is None:
+        o = (_q._call or _q._native()).attention(cache, q, lengths, starts, scale, max_len, out)
+        if o is not None:
+            if type(o) is int:
+                _q._check("qwam_paged_attention", o)
+            return o
     c = cache.c_struct()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of three dimensions (sequences, heads, dim)")

@@ -6,9 +6,9 @@ raw device pointers plus the current HIP stream across the C ABI.  If the
 library is not built, every call raises: there is no fallback.
 
 The per-token calls (quantize_act, quantize_act_deflated, asp_linear,
-asp_layer) marshal natively (csrc/qwam_binding.cpp); what that path does not
-take (for asp_linear and asp_layer an explicit stream, for all of them an
-argument that fails a check) goes through ctypes here, which raises for the
+asp_layer, asp_matvec and those of block.py) marshal natively
+(csrc/qwam_binding.cpp); what that path does not take (for all but the
+activation calls an explicit stream, for all of them an argument that fails a check) goes through ctypes here, which raises for the
 argument that is wrong.
 
 Names follow the C ABI (include/qwam.h): pack_weights, quantize_act,
@@ -141,7 +141,10 @@ def _native():
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
         mod.bind(*(ctypes.cast(getattr(lib(), f), ctypes.c_void_p).value
-                   for f in ("qwam_quantize_act_ws", "qwam_quantize_act_workspace", "qwam_asp_linear", "qwam_asp_layer")))
+                   for f in ("qwam_quantize_act_ws", "qwam_quantize_act_workspace", "qwam_asp_linear", "qwam_asp_layer", "qwam_asp_matvec",
+                             "qwam_asp_matvec_workspace", "qwam_block_norm", "qwam_block_norm_backward",
+                             "qwam_block_norm_backward_workspace", "qwam_kv_append", "qwam_paged_attention",
+                             "qwam_paged_attention_workspace")))
         _call = mod
     return _call
 
@@ -383,6 +386,12 @@ def _need(fn: str, nbytes: int) -> int:
 def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """qwam_asp_matvec: the packed layer on 1 to 16 tokens without quantizing them.  x bf16 [M][K] -> y bf16 [M][N].
     `stream` is a torch.cuda.Stream (y and the workspace come from its pool)."""
+    if stream is None:
+        y = (_call or _native()).matvec(layer, x, out)
+        if y is not None:
+            if type(y) is int:
+                _check("qwam_asp_matvec", y)
+            return y
     M = x.shape[0]
     c = layer.c_struct(matvec=True)
     px = _req(x, "x", torch.bfloat16, (M, layer.K))
