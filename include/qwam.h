@@ -434,7 +434,8 @@ typedef struct qwam_cache {
                                 /* positions of a sequence exist (below 2^31)           */
     int32_t reserved;           /* 0                                                    */
     int64_t page_stride, head_stride, row_stride;   /* elements between pages, heads and rows;  */
-                                /* multiples of 8 (fp8: 16), the same for k and v        */
+                                /* multiples of 8 (fp8: 16), the same for k and v;       */
+                                /* |row_stride| < 2^26                                  */
     void *k, *v;                /* 16-byte aligned                                      */
     const float *k_scale, *v_scale;                 /* float [heads] (fp8), else not read   */
     const int32_t *table;       /* [seqs][table_width]                                  */

@@ -420,6 +420,9 @@ qwam_status check_cache_shape(const char* fn, const qwam_cache* c, qwam::CachePa
   if (c->reserved != 0) return fail(QWAM_ERR_INVALID_ARG, "%s: reserved must be 0", fn);
   if (c->page_stride % step != 0 || c->head_stride % step != 0 || c->row_stride % step != 0)
     return fail(QWAM_ERR_MISALIGNED, "%s: the cache's strides must be multiples of %d", fn, step);
+  // 16 rows are addressed with 32-bit byte offsets
+  if (c->row_stride <= -(1 << 26) || c->row_stride >= (1 << 26))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: row_stride must be within 2^26", fn);
   *out = {c->pages, __builtin_ctz(static_cast<unsigned>(c->page_size)), c->heads, c->dim, c->seqs, c->table_width,
           c->page_stride, c->head_stride, c->row_stride, c->k, c->v, c->k_scale, c->v_scale, c->table};
   return QWAM_OK;
@@ -438,7 +441,7 @@ qwam_status check_cache(const char* fn, const qwam_cache* c, qwam::CacheParams* 
   return QWAM_OK;
 }
 
-qwam_status check_attention(const char* fn, const qwam_cache* c, int32_t q_heads, int32_t max_len) {
+qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::CacheParams& cp, int32_t q_heads, int32_t max_len) {
   if (q_heads <= 0 || q_heads % c->heads != 0)
     return fail(QWAM_ERR_INVALID_ARG, "%s: q_heads must be a positive multiple of heads (got %d, %d)", fn, q_heads, c->heads);
   if (q_heads / c->heads > qwam::kMaxHeadGroup)
@@ -447,6 +450,8 @@ qwam_status check_attention(const char* fn, const qwam_cache* c, int32_t q_heads
     return fail(QWAM_ERR_UNSUPPORTED, "%s: seqs * q_heads must be at most 2^22", fn);
   if (max_len < 1 || max_len > static_cast<int64_t>(c->table_width) * c->page_size)
     return fail(QWAM_ERR_INVALID_ARG, "%s: max_len must be in [1, table_width * page_size] (got %d)", fn, max_len);
+  if (!qwam::paged_attention_fits(cp, q_heads, max_len))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: too many sequences and heads of too long a max_len for one launch", fn);
   return QWAM_OK;
 }
 
@@ -562,9 +567,9 @@ qwam_status qwam_kv_append(const qwam_cache* c, int32_t tokens, const uint16_t* 
 int64_t qwam_paged_attention_workspace(const qwam_cache* c, int32_t q_heads, int32_t max_len) {
   const char* fn = "qwam_paged_attention_workspace";
   qwam::CacheParams cp;
-  if (check_cache_shape(fn, c, &cp) != QWAM_OK || check_attention(fn, c, q_heads, max_len) != QWAM_OK) return -1;
+  if (check_cache_shape(fn, c, &cp) != QWAM_OK || check_attention(fn, c, cp, q_heads, max_len) != QWAM_OK) return -1;
   ok();
-  return qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len);
+  return qwam::paged_attention_workspace_bytes(cp, q_heads, max_len);
 }
 
 qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uint16_t* q, int64_t q_stride,
@@ -574,7 +579,7 @@ qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uin
   qwam::CacheParams cp;
   qwam_status s = check_cache(fn, c, &cp);
   if (s != QWAM_OK) return s;
-  if ((s = check_attention(fn, c, q_heads, max_len)) != QWAM_OK) return s;
+  if ((s = check_attention(fn, c, cp, q_heads, max_len)) != QWAM_OK) return s;
   if (!finite(scale)) return fail(QWAM_ERR_INVALID_ARG, "%s: scale must be finite", fn);
   QWAM_REQUIRE_PTR(q);
   if (q_stride % 8 != 0) return fail(QWAM_ERR_MISALIGNED, "%s: q_stride must be a multiple of 8", fn);
@@ -582,7 +587,7 @@ qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uin
   QWAM_OPTIONAL_ELEM(starts, 4);
   QWAM_REQUIRE_PTR(out);
   const bool fp8 = c->type == QWAM_CACHE_FP8;
-  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, fp8, q_heads, max_len))) !=
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, q_heads, max_len))) !=
       QWAM_OK)
     return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;

@@ -1,24 +1,39 @@
 // The paged key-value cache: new keys and values into the pages
 // (qwam_kv_append), and the attention of one new token per sequence
-// (qwam_paged_attention), one wave per (sequence, query head).
+// (qwam_paged_attention):
+//   o[h] = sum_p softmax_p(scale q[h] . K[p]) V[p], the G = q_heads / heads query heads of a key head together.
+// Every key and value is read once from HBM and serves G heads; with G <= 16 that
+// is far below what the matrix cores need to be busy, so the stream of the pages
+// is the bound and everything below is laid out for it:
+//
+//   * A workgroup takes one key head (and up to 16 query heads) of one sequence
+//     over a range of its positions, its four waves a quarter each.  Ranges of
+//     256 to 4096 positions, by the work at hand (chunk_of); their partial results
+//     (maximum, sum, unnormalized o, float32) are joined by a second launch, in
+//     order.  A context of one range is finished by the first.
+//   * Keys and values go from HBM to registers in whole row pieces and never
+//     through LDS.  S^T = K q^T (v_mfma_f32_16x16x32_bf16, 16 keys x 16 heads)
+//     leaves in each lane the scores of one head for keys 4c + i, c the lane's
+//     quarter: exactly the keys that the lane has to supply as the second operand
+//     of o^T = V^T S^T if the eight positions of its MFMA slots are read as keys
+//     4c + i and 16 + 4c + i.  So the weights stay where they are computed.
+//   * V^T needs eight keys of one channel in a lane.  Each lane loads the same few
+//     channels of its eight keys (rows whole across 16 lanes) and transposes
+//     that block in its registers, half an instruction per value.
+//   * Softmax with a running maximum and sum in float32, in powers of two; the
+//     weights enter the product with V as two bf16 pieces (within 2^-17), since
+//     the matrix cores are idle most of the time.
+//   * The page of each 16 positions is looked up once per wave, a lane each, and
+//     handed out by readlane, so that addresses are scalar.
+//   * Positions outside [start, length) or without a page get weight 0, and their
+//     values are replaced by 0 before the product (0 * NaN is not 0).
 #include "qwam_device.h"
 #include "qwam_internal.h"
+#include "qwam_mfma.h"
 
 namespace qwam {
 
 namespace {
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int i = 32; i > 0; i >>= 1) v += __shfl_xor(v, i);
-  return v;
-}
-
-template <bool FP8>
-__device__ __forceinline__ float cache_value(const void* p, int64_t i) {
-  if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(p)[i], 0);
-  else return bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
 
 // e4m3 codes of four values: to nearest, ties to even; the caller has clamped them
 __device__ __forceinline__ uint32_t fp8x4(float a, float b, float c, float d) {
@@ -62,44 +77,368 @@ __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, int token
   }
 }
 
-template <bool FP8>
-__global__ __launch_bounds__(64) void paged_attention_kernel(CacheParams c, int q_heads, const uint16_t* q, int64_t q_stride,
-                                                             const int32_t* lengths, const int32_t* starts, int max_len,
-                                                             float scale, uint16_t* out) {
-  const int b = blockIdx.x / q_heads, hq = blockIdx.x % q_heads, h = hq / (q_heads / c.heads);
-  const int lane = threadIdx.x;
-  const int64_t reach = static_cast<int64_t>(c.table_width) << c.page_bits;
-  const int len = static_cast<int>(min(static_cast<int64_t>(min(lengths[b], max_len)), reach));
-  const int first = starts != nullptr ? max(starts[b], 0) : 0;
-  float qv[4], acc[4] = {}, m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int d = lane + 64 * e;
-    qv[e] = d < c.dim ? bf16_to_f32(q[b * q_stride + static_cast<int64_t>(hq) * c.dim + d]) : 0.0f;
-  }
-  const float ks = FP8 ? c.k_scale[h] : 1.0f, vs = FP8 ? c.v_scale[h] : 1.0f;
-  for (int p = first; p < len; ++p) {
-    const int page = c.table[static_cast<int64_t>(b) * c.table_width + (p >> c.page_bits)];
-    if (page < 0 || page >= c.pages) continue;
-    const int64_t at = page * c.page_stride + h * c.head_stride + (p & ((1 << c.page_bits) - 1)) * c.row_stride;
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + 64 * e < c.dim) s += qv[e] * cache_value<FP8>(c.k, at + lane + 64 * e);
-    s = wave_sum(s) * (scale * ks);
-    const float mn = fmaxf(m, s), f = expf(m - mn), w = expf(s - mn);
-    m = mn;
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + 64 * e < c.dim) acc[e] = acc[e] * f + w * cache_value<FP8>(c.v, at + lane + 64 * e);
-  }
-  const float inv = l > 0.0f ? vs / l : 0.0f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (lane + 64 * e < c.dim)
-      out[static_cast<int64_t>(blockIdx.x) * c.dim + lane + 64 * e] = static_cast<uint16_t>(f32_to_bf16_rne(acc[e] * inv));
+namespace {
+
+constexpr int kAttnWaves = 4;
+constexpr int kMinChunk = 256, kMaxChunk = 4096;     // positions of a workgroup; a wave's lanes hold its pages, 16 positions each
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttnArgs {
+  CacheParams c;
+  const uint16_t* q;
+  int64_t q_stride;
+  const int32_t *lengths, *starts;
+  uint16_t* out;
+  float *part, *stat;             // [seqs][q_heads][splits][dim], and (maximum, sum) likewise
+  int q_heads, group, max_len, chunk, splits;
+  float scale;
+};
+
+// visible positions of a sequence: [first, len), and where its ranges start
+struct Span {
+  int first, len, base, count;    // count: ranges
+};
+__device__ __forceinline__ Span span_of(const AttnArgs& a, int b) {
+  Span s;
+  const int64_t reach = static_cast<int64_t>(a.c.table_width) << a.c.page_bits;
+  s.len = static_cast<int>(min(static_cast<int64_t>(min(a.lengths[b], a.max_len)), reach));
+  s.first = a.starts != nullptr ? max(a.starts[b], 0) : 0;
+  s.base = s.first & ~31;
+  s.count = s.len > s.first ? (s.len - s.base + a.chunk - 1) / a.chunk : 0;
+  return s;
 }
+
+// 16-bit halves of two words: (low of a, low of b) or (high of a, high of b)
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// two e4m3 codes of a word (its low or high half) as a bf16 pair, exactly
+template <bool HIGH>
+__device__ __forceinline__ uint32_t fp8_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+}
+
+__device__ __forceinline__ v8bf bf8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(v8bf, make_uint4(a, b, c, d));
+}
+
+}  // namespace
+
+// DP: dim rounded up to 64, 128 or 256; FULL: dim == DP
+template <int DP, bool FP8, bool FULL>
+__global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnArgs a) {
+  constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value
+  constexpr int DC = DP / 16;                     // channels of V in a lane
+  constexpr int NK = DP * EB / 64;                // 16-byte pieces of K in a lane, per 16 keys
+  constexpr int NV = DC * EB / 4;                 // words of V in a lane, per key
+  constexpr int NF = DP / 32;                     // MFMA steps over the channels
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, c = lane >> 4;
+  const int qtiles = (a.group + 15) / 16, rows = a.c.seqs * a.c.heads * qtiles;
+  const int range = blockIdx.x / rows, bh = blockIdx.x % rows / qtiles, qt = blockIdx.x % qtiles;
+  const int h = bh % a.c.heads, b = bh / a.c.heads;
+  const Span sp = span_of(a, b);
+  if (range >= max(sp.count, 1)) return;
+  const int q0 = qt * 16, nq = min(16, a.group - q0);   // query heads of this tile
+  const int64_t head_row = static_cast<int64_t>(b) * a.q_heads + h * a.group + q0;
+  const int D = FULL ? DP : a.c.dim;
+  if (sp.count == 0) {                            // nothing to see: zeros
+    for (int i = threadIdx.x; i < nq * D; i += 64 * kAttnWaves) a.out[head_row * D + i] = 0;
+    return;
+  }
+
+  // this wave's positions [w0, w1), in tiles of 32
+  const int quarter = a.chunk / kAttnWaves;
+  const int w0 = sp.base + range * a.chunk + wave * quarter;
+  const int w1 = min(w0 + quarter, sp.len);
+  const int tiles = w1 > w0 ? (w1 - w0 + 31) / 32 : 0;
+
+  // lane i: the page of positions w0 + 16 i .. +15, or -1
+  int pid = -1;
+  {
+    const int p = w0 + 16 * lane;
+    if (16 * lane < quarter && p < w1) {
+      pid = a.c.table[static_cast<int64_t>(b) * a.c.table_width + (p >> a.c.page_bits)];
+      if (pid >= a.c.pages) pid = -1;
+    }
+  }
+
+  // q as the second operand of S^T: head r, channels of this quarter
+  auto channel = [&](int f) { return FP8 ? 64 * (f >> 1) + 16 * c + 8 * (f & 1) : 32 * f + 8 * c; };
+  v8bf qf[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < nq && (FULL || channel(f) < D))
+      v = *reinterpret_cast<const uint4*>(a.q + b * a.q_stride + static_cast<int64_t>(h * a.group + q0 + r) * D + channel(f));
+    qf[f] = __builtin_bit_cast(v8bf, v);
+  }
+  const float ks = FP8 ? a.c.k_scale[h] : 1.0f;
+  const float sscale = a.scale * ks * kLog2e;
+
+  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride * EB;
+  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride * EB;
+  const int row = static_cast<int>(a.c.row_stride) * EB;          // bytes; 16 rows stay below 2^31
+  const int row_mask = (1 << a.c.page_bits) - 1;
+  // bytes from the head's first row of page 0 to row 0 of 16 positions; a missing page reads page 0, unseen
+  auto place = [&](int i, int& id) -> int64_t {
+    id = __builtin_amdgcn_readlane(pid, i);
+    const int64_t page = id < 0 ? 0 : id;
+    return (page * a.c.page_stride + static_cast<int64_t>((w0 + 16 * i) & row_mask) * a.c.row_stride) * EB;
+  };
+
+  uint4 kr[2][NK];
+  uint32_t vr[8][NV];
+  int id[2], idn[2];
+  int64_t at[2], atn[2];
+  auto load_k = [&](const int64_t (&o)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const int ch = 64 / EB * i + 16 / EB * c;
+        kr[t][i] = make_uint4(0, 0, 0, 0);
+        if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
+      }
+  };
+  auto load_v = [&](const int64_t (&o)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + DC * r * EB);
+#pragma unroll
+      for (int w = 0; w < NV; ++w) vr[j][w] = 0;
+      if constexpr (NV == 8) {
+        if (FULL || DC * r < D) *reinterpret_cast<uint4*>(&vr[j][0]) = *reinterpret_cast<const uint4*>(src);
+        if (FULL || DC * r + 8 < D) *reinterpret_cast<uint4*>(&vr[j][4]) = *reinterpret_cast<const uint4*>(src + 16);
+      } else if (FULL || DC * r < D) {
+        if constexpr (NV == 4) *reinterpret_cast<uint4*>(&vr[j][0]) = *reinterpret_cast<const uint4*>(src);
+        if constexpr (NV == 2) *reinterpret_cast<uint2*>(&vr[j][0]) = *reinterpret_cast<const uint2*>(src);
+        if constexpr (NV == 1) vr[j][0] = *reinterpret_cast<const uint32_t*>(src);
+      }
+    }
+  };
+
+  float m = -INFINITY, l = 0.0f;
+  v4f acc[DC];
+#pragma unroll
+  for (int e = 0; e < DC; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  if (tiles > 0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) at[t] = place(t, id[t]);
+    load_k(at);
+  }
+  for (int tile = 0; tile < tiles; ++tile) {
+    load_v(at);
+    // scores of keys 16 t + 4 c + i, head r
+    v4f s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        v8bf k;
+        if constexpr (FP8) {
+          const uint4 w = kr[t][f >> 1];
+          const uint32_t x = f & 1 ? w.z : w.x, y = f & 1 ? w.w : w.y;
+          k = bf8(fp8_pair<false>(x), fp8_pair<true>(x), fp8_pair<false>(y), fp8_pair<true>(y));
+        } else {
+          k = __builtin_bit_cast(v8bf, kr[t][f]);
+        }
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[f], s[t], 0, 0, 0);
+      }
+    }
+    if (tile + 1 < tiles) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) atn[t] = place(2 * (tile + 1) + t, idn[t]);
+      load_k(atn);
+    }
+    const int p0 = w0 + 32 * tile;
+    const bool whole = p0 >= sp.first && p0 + 32 <= sp.len && id[0] >= 0 && id[1] >= 0;
+    uint32_t seen = 0xFFu;                        // bit j: the lane's key of slot j
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int p = p0 + 16 * (j >> 2) + 4 * c + (j & 3);
+        if (p < sp.first || p >= sp.len || id[j >> 2] < 0) seen &= ~(1u << j);
+      }
+    }
+    float x[8], top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = s[j >> 2][j & 3] * sscale;
+      if (!whole && !(seen >> j & 1u)) x[j] = -INFINITY;
+      top = fmaxf(top, x[j]);
+    }
+    top = max_xor32(max_xor16(top));
+    const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.0f : mn;
+    if (__any(mn > m)) {
+      const float f = __builtin_amdgcn_exp2f(m - base);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < DC; ++e) acc[e] *= f;
+      m = mn;
+    }
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      const float u = __builtin_amdgcn_exp2f(x[j] - base), v = __builtin_amdgcn_exp2f(x[j + 1] - base);
+      l += u + v;
+      hi[j / 2] = bf16_pair(u, v);
+      lo[j / 2] = bf16_pair(u - __uint_as_float(hi[j / 2] << 16), v - __uint_as_float(hi[j / 2] & 0xFFFF0000u));
+    }
+    const v8bf ph = bf8(hi[0], hi[1], hi[2], hi[3]), pl = bf8(lo[0], lo[1], lo[2], lo[3]);
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int w = 0; w < NV; ++w)
+          if (!(seen >> j & 1u)) vr[j][w] = 0;
+    }
+    // o^T += V^T S^T: channel DC r + e of the lane's eight keys
+#pragma unroll
+    for (int w = 0; w < DC / 2; ++w) {
+      uint32_t y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (FP8) y[j] = w & 1 ? fp8_pair<true>(vr[j][w >> 1]) : fp8_pair<false>(vr[j][w >> 1]);
+        else y[j] = vr[j][w];
+      }
+      const v8bf even = bf8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7]));
+      const v8bf odd = bf8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7]));
+      acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph, acc[2 * w], 0, 0, 0);
+      acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph, acc[2 * w + 1], 0, 0, 0);
+      acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl, acc[2 * w], 0, 0, 0);
+      acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl, acc[2 * w + 1], 0, 0, 0);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      at[t] = atn[t];
+      id[t] = idn[t];
+    }
+  }
+
+  // join the waves: one maximum, then sums of l and o through LDS
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  constexpr int RS = DP + 4;                      // floats of an o row in LDS
+  float* const sm = smem;                         // [waves][16] maxima, then sums
+  float* const so = smem + 2 * kAttnWaves * 16;   // [waves][nq][RS]
+  if (c == 0) {
+    sm[wave * 16 + r] = m;
+    sm[(kAttnWaves + wave) * 16 + r] = l;
+  }
+  __syncthreads();
+  float mt = sm[r];
+#pragma unroll
+  for (int w = 1; w < kAttnWaves; ++w) mt = fmaxf(mt, sm[w * 16 + r]);
+  const float f = __builtin_amdgcn_exp2f(m - (mt == -INFINITY ? 0.0f : mt));
+  if (r < nq)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < DC; e += 4)
+        *reinterpret_cast<float4*>(so + (wave * nq + r) * RS + DC * (4 * c + i) + e) =
+            make_float4(acc[e][i] * f, acc[e + 1][i] * f, acc[e + 2][i] * f, acc[e + 3][i] * f);
+  __syncthreads();
+  const float vs = FP8 ? a.c.v_scale[h] : 1.0f;
+  for (int i = threadIdx.x; i < nq * (D / 4); i += 64 * kAttnWaves) {
+    const int g = i / (D / 4), d = (i % (D / 4)) * 4;
+    float top = sm[g], sum = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, sm[w * 16 + g]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) {
+      sum += sm[(kAttnWaves + w) * 16 + g] * __builtin_amdgcn_exp2f(sm[w * 16 + g] - ref);
+      const float4 v = *reinterpret_cast<const float4*>(so + (w * nq + g) * RS + d);
+      o.x += v.x;
+      o.y += v.y;
+      o.z += v.z;
+      o.w += v.w;
+    }
+    const int64_t hr = head_row + g;
+    if (sp.count == 1) {
+      const float n = sum > 0.0f || sum != sum ? vs / sum : 0.0f;
+      *reinterpret_cast<uint2*>(a.out + hr * D + d) = make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
+    } else {
+      const int64_t pr = hr * a.splits + range;
+      *reinterpret_cast<float4*>(a.part + pr * D + d) = o;
+      if (d == 0) {
+        a.stat[2 * pr] = top;
+        a.stat[2 * pr + 1] = sum;
+      }
+    }
+  }
+}
+
+// the ranges of a sequence into one result: one workgroup per (sequence, query head)
+template <bool FP8>
+__global__ __launch_bounds__(64) void attention_join_kernel(AttnArgs a) {
+  const int b = blockIdx.x / a.q_heads, hq = blockIdx.x % a.q_heads, h = hq / a.group;
+  const Span sp = span_of(a, b);
+  if (sp.count <= 1) return;                      // written by the first launch
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * a.splits;
+  const int lane = threadIdx.x, D = a.c.dim;
+  float top = -INFINITY;
+  for (int s = lane; s < sp.count; s += 64) top = fmaxf(top, a.stat[2 * (row + s)]);
+#pragma unroll
+  for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s = 0; s < sp.count; ++s) {
+    const float f = __builtin_amdgcn_exp2f(a.stat[2 * (row + s)] - ref);
+    sum += a.stat[2 * (row + s) + 1] * f;
+    if (4 * lane < D) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + (row + s) * D + 4 * lane);
+      o.x += v.x * f;
+      o.y += v.y * f;
+      o.z += v.z * f;
+      o.w += v.w * f;
+    }
+  }
+  const float n = sum > 0.0f || sum != sum ? (FP8 ? a.c.v_scale[h] : 1.0f) / sum : 0.0f;
+  if (4 * lane < D)
+    *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(blockIdx.x) * D + 4 * lane) =
+        make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
+}
+
+namespace {
+
+int64_t rows_of(const CacheParams& c, int q_heads) {
+  return static_cast<int64_t>(c.seqs) * c.heads * ((q_heads / c.heads + 15) / 16);
+}
+
+// positions of a workgroup: enough workgroups for every CU four times, ranges not below 256 positions
+int chunk_of(const CacheParams& c, int q_heads, int max_len) {
+  const int64_t want = (rows_of(c, q_heads) * max_len + 1023) / 1024;
+  const int64_t n = (want + 127) / 128 * 128;
+  return static_cast<int>(n < kMinChunk ? kMinChunk : n > kMaxChunk ? kMaxChunk : n);
+}
+
+int splits_of(int max_len, int chunk) { return static_cast<int>((static_cast<int64_t>(max_len) + chunk - 1) / chunk); }
+
+template <int DP, bool FP8>
+hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
+  const int nq = a.group < 16 ? a.group : 16;
+  const dim3 grid(static_cast<unsigned>(rows_of(a.c, a.q_heads) * a.splits)), block(64 * kAttnWaves);
+  const int bytes = (2 * kAttnWaves * 16 + kAttnWaves * nq * (DP + 4)) * 4;
+  auto kernel = a.c.dim == DP ? paged_attention_kernel<DP, FP8, true> : paged_attention_kernel<DP, FP8, false>;
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL((attention_join_kernel<FP8>), dim3(static_cast<unsigned>(a.c.seqs) * a.q_heads), dim3(64), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream) {
@@ -110,19 +449,28 @@ hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const ui
   return hipGetLastError();
 }
 
-int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len) { return 0; }
+bool paged_attention_fits(const CacheParams& c, int q_heads, int max_len) {
+  return rows_of(c, q_heads) * splits_of(max_len, chunk_of(c, q_heads, max_len)) < (int64_t(1) << 24);
+}
+
+int64_t paged_attention_workspace_bytes(const CacheParams& c, int q_heads, int max_len) {
+  const int64_t splits = splits_of(max_len, chunk_of(c, q_heads, max_len));
+  return splits <= 1 ? 0 : static_cast<int64_t>(c.seqs) * q_heads * splits * (c.dim + 2) * 4;
+}
 
 hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
                                   const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
                                   void* workspace, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(c.seqs) * q_heads);
+  const int chunk = chunk_of(c, q_heads, max_len), splits = splits_of(max_len, chunk);
+  float* const part = static_cast<float*>(workspace);
+  const AttnArgs a = {c, q, q_stride, lengths, starts, out, part,
+                      splits > 1 ? part + static_cast<int64_t>(c.seqs) * q_heads * splits * c.dim : nullptr,
+                      q_heads, q_heads / c.heads, max_len, chunk, splits, scale};
   if (fp8)
-    hipLaunchKernelGGL((paged_attention_kernel<true>), grid, dim3(64), 0, stream, c, q_heads, q, q_stride, lengths, starts,
-                       max_len, scale, out);
-  else
-    hipLaunchKernelGGL((paged_attention_kernel<false>), grid, dim3(64), 0, stream, c, q_heads, q, q_stride, lengths, starts,
-                       max_len, scale, out);
-  return hipGetLastError();
+    return c.dim <= 64 ? launch_attention<64, true>(a, stream) : c.dim <= 128 ? launch_attention<128, true>(a, stream)
+                                                                              : launch_attention<256, true>(a, stream);
+  return c.dim <= 64 ? launch_attention<64, false>(a, stream) : c.dim <= 128 ? launch_attention<128, false>(a, stream)
+                                                                             : launch_attention<256, false>(a, stream);
 }
 
 }  // namespace qwam
