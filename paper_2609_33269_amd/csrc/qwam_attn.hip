@@ -375,36 +375,55 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
   }
 }
 
-// the ranges of a sequence into one result: one workgroup per (sequence, query head)
-template <bool FP8>
-__global__ __launch_bounds__(64) void attention_join_kernel(AttnArgs a) {
+// the ranges of a sequence into one result: one workgroup per (sequence, query
+// head), LR lanes per row of o, the rows dealt out over the others
+template <int LR, bool FP8>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
+  constexpr int SLOTS = 256 / LR;
+  __shared__ float4 so[SLOTS][LR];
+  __shared__ float ss[SLOTS], st[4];
   const int b = blockIdx.x / a.q_heads, hq = blockIdx.x % a.q_heads, h = hq / a.group;
   const Span sp = span_of(a, b);
   if (sp.count <= 1) return;                      // written by the first launch
   const int64_t row = static_cast<int64_t>(blockIdx.x) * a.splits;
-  const int lane = threadIdx.x, D = a.c.dim;
+  const int slot = threadIdx.x / LR, d = threadIdx.x % LR * 4, D = a.c.dim;
   float top = -INFINITY;
-  for (int s = lane; s < sp.count; s += 64) top = fmaxf(top, a.stat[2 * (row + s)]);
+  for (int s = threadIdx.x; s < sp.count; s += 256) top = fmaxf(top, a.stat[2 * (row + s)]);
 #pragma unroll
   for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  if ((threadIdx.x & 63) == 0) st[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
   const float ref = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s = 0; s < sp.count; ++s) {
-    const float f = __builtin_amdgcn_exp2f(a.stat[2 * (row + s)] - ref);
-    sum += a.stat[2 * (row + s) + 1] * f;
-    if (4 * lane < D) {
-      const float4 v = *reinterpret_cast<const float4*>(a.part + (row + s) * D + 4 * lane);
-      o.x += v.x * f;
-      o.y += v.y * f;
-      o.z += v.z * f;
-      o.w += v.w * f;
+#pragma unroll 4
+  for (int s = slot; s < sp.count; s += SLOTS) {
+    const float2 q = *reinterpret_cast<const float2*>(a.stat + 2 * (row + s));
+    const float f = __builtin_amdgcn_exp2f(q.x - ref);
+    sum = __builtin_fmaf(q.y, f, sum);
+    if (d < D) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + (row + s) * D + d);
+      o.x = __builtin_fmaf(v.x, f, o.x);
+      o.y = __builtin_fmaf(v.y, f, o.y);
+      o.z = __builtin_fmaf(v.z, f, o.z);
+      o.w = __builtin_fmaf(v.w, f, o.w);
     }
   }
+  so[slot][threadIdx.x % LR] = o;
+  if (d == 0) ss[slot] = sum;
+  __syncthreads();
+  if (slot != 0 || d >= D) return;
+  for (int s = 1; s < SLOTS; ++s) {
+    const float4 v = so[s][threadIdx.x % LR];
+    o.x += v.x;
+    o.y += v.y;
+    o.z += v.z;
+    o.w += v.w;
+    sum += ss[s];
+  }
   const float n = sum > 0.0f || sum != sum ? (FP8 ? a.c.v_scale[h] : 1.0f) / sum : 0.0f;
-  if (4 * lane < D)
-    *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(blockIdx.x) * D + 4 * lane) =
-        make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
+  *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(blockIdx.x) * D + d) = make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
 }
 
 namespace {
@@ -434,7 +453,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
   }
   hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a);
   if (a.splits > 1)
-    hipLaunchKernelGGL((attention_join_kernel<FP8>), dim3(static_cast<unsigned>(a.c.seqs) * a.q_heads), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL((attention_join_kernel<DP / 4, FP8>), dim3(static_cast<unsigned>(a.c.seqs) * a.q_heads), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
