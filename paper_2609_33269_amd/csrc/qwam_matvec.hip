@@ -35,10 +35,11 @@ namespace qwam {
 
 namespace {
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;         // of a workgroup; eight where there are few workgroups
+constexpr int kMaxWaves = 8;
 constexpr int kUnit = 128;        // channels of one MFMA step
-constexpr int kCols = 16;         // output channels of a workgroup
-constexpr int kMaxTSplits = 16;   // workgroups of the t launch
+constexpr int kCols = 16;         // output channels of a tile
+constexpr int kMaxSplits = 16;    // parts of K, of y and of t
 
 typedef __bf16 v32bf __attribute__((ext_vector_type(32)));
 
@@ -51,76 +52,82 @@ struct MatvecArgs {
   const uint16_t* L2t;
   const uint16_t* bias;
   uint16_t* y;
-  float* part;                    // partial t of the t launch: [splits][M][r]
-  int M, N, K, r, splits;
+  float *part, *tpart;            // split: partial sums [splits][M][N] of y, [tsplits][M][r] of t; otherwise null
+  int M, N, K, r;
+  int splits, blocks;             // parts of K; workgroups of a part
+  int tsplits, tblocks;           // the same for t, whose workgroups come first
+  int waves, pitch;               // of a workgroup; bytes of a staged vector
 };
 
-// LDS of a workgroup: every wave's staged vectors (rows 16 bytes apart more than
-// their CK values, so that the rows of a fragment read lie on different banks), or
-// the waves' partial results where those are more; an empty row; t
-__host__ __device__ constexpr int row_bytes(int ck) { return ck * 2 + 16; }
+// A staged vector: the channels of a chunk (fewer where a wave has fewer) and 16
+// bytes more, so that the rows of a fragment read lie on different banks.
+constexpr int chunk_channels(int sets, int sl, int nt) { return sets * sl > 16 || nt > 1 ? 256 : 512; }
 
-template <int GS, int SETS, int CK, int RB, bool MAIN, bool SMOOTH>
-__global__ __launch_bounds__(64 * kWaves, 2) void matvec_kernel(MatvecArgs a) {
+template <int GS, int SETS, int NT, int RB, bool SMOOTH>
+__global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a) {
   constexpr int SL = GS == 64 ? 8 : 4;               // rows (vectors) of a set
   constexpr int GPU = kUnit / GS;                    // groups of a unit
+  constexpr int CK = chunk_channels(SETS, SL, NT);   // channels staged at a time
   constexpr int UPC = CK / kUnit;                    // units of a chunk
   constexpr int LPT = CK / 8;                        // lanes that stage one token's chunk, 8 channels each
   constexpr int TPI = 64 / LPT;                      // tokens staged at once
   constexpr int PIECES = SMOOTH ? 2 : 1;             // of a token's x~
   constexpr int NX = (SETS * SL / PIECES + TPI - 1) / TPI;    // staging steps
-  constexpr int TILES = (MAIN ? 1 : 0) + RB;
+  constexpr int TILES = NT + RB;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, c = lane >> 4;
-  const int M = a.M, K = a.K, N = a.N;
-  const int V = M * PIECES;
-  const int n0 = MAIN ? blockIdx.x * kCols : 0;
+  const int M = a.M, K = a.K, N = a.N, V = M * PIECES, waves = a.waves, pitch = a.pitch;
+  const int tgrid = a.tsplits * a.tblocks;
+  const bool branch = static_cast<int>(blockIdx.x) < tgrid;             // a workgroup of t
+  const int index = branch ? blockIdx.x : blockIdx.x - tgrid, nblocks = branch ? a.tblocks : a.blocks;
+  const int split = index / nblocks, block = index % nblocks;
+  const int n0 = branch ? 0 : block * (NT * kCols);  // first output channel
+  const int b0 = block * NT;                         // first 16 directions of t
 
   // this wave's units [lo, hi) of the workgroup's
-  const int units = (K + kUnit - 1) / kUnit;
-  int wlo = 0, whi = units;
-  if constexpr (!MAIN) {
-    const int per = (units + a.splits - 1) / a.splits;
-    wlo = min(units, static_cast<int>(blockIdx.x) * per);
-    whi = min(units, wlo + per);
-  }
-  const int per = (whi - wlo + kWaves - 1) / kWaves;
+  const int units = (K + kUnit - 1) / kUnit, nsplits = branch ? a.tsplits : a.splits, per_split = (units + nsplits - 1) / nsplits;
+  const int wlo = min(units, split * per_split), whi = min(units, wlo + per_split);
+  const int per = (whi - wlo + waves - 1) / waves;
   const int lo = min(whi, wlo + wave * per), hi = min(whi, lo + per);
   const int chunks = (hi - lo + UPC - 1) / UPC;
 
-  uint8_t* const stage = lds + wave * V * row_bytes(CK);
-  const int stage_all = kWaves * V * row_bytes(CK), red_all = kWaves * TILES * SETS * SL * kCols * 4;
+  uint8_t* const stage = lds + wave * V * pitch;
+  const int stage_all = waves * V * pitch, red_all = waves * TILES * SETS * SL * kCols * 4;
   uint8_t* const zero = lds + max(stage_all, red_all);
-  float* const tl = reinterpret_cast<float*>(zero + row_bytes(CK));
-  if (threadIdx.x < row_bytes(CK) / 16) reinterpret_cast<uint4*>(zero)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+  float* const tl = reinterpret_cast<float*>(zero + pitch);
+  for (int i = threadIdx.x; i < pitch / 16; i += 64 * waves) reinterpret_cast<uint4*>(zero)[i] = make_uint4(0, 0, 0, 0);
 
   // out-of-range offsets read zeros: units past hi (kept in the loop's registers
   // but never multiplied) and the codes past the last row
   constexpr uint32_t kNowhere = 0x80000000u;
   const int KB = K / 2;
-  const buf_rsrc w_rsrc = make_rsrc(MAIN ? a.wq + static_cast<int64_t>(n0) * KB : nullptr, MAIN ? kCols * static_cast<uint32_t>(KB) : 0u);
-  const buf_rsrc s_rsrc = make_rsrc(a.ws, MAIN ? static_cast<uint32_t>(K / GS) * static_cast<uint32_t>(N) * 4u : 0u);
+  const uint32_t rows = branch ? 0u : static_cast<uint32_t>(min(NT * kCols, N - n0));
+  const buf_rsrc w_rsrc = make_rsrc(a.wq + static_cast<int64_t>(n0) * KB, rows * static_cast<uint32_t>(KB));
+  const buf_rsrc s_rsrc = make_rsrc(a.ws, static_cast<uint32_t>(K / GS) * static_cast<uint32_t>(N) * 4u);
   const buf_rsrc x_rsrc = make_rsrc(a.x, static_cast<uint32_t>(M) * static_cast<uint32_t>(K) * 2u);
   const buf_rsrc i_rsrc = make_rsrc(a.inv, SMOOTH ? static_cast<uint32_t>(K) * 4u : 0u);
-
-  const buf_rsrc l_rsrc = make_rsrc(a.L1f, RB > 0 ? static_cast<uint32_t>(K) * (RB * 32u) : 0u);
+  const int rb = a.r >> 4;
+  const buf_rsrc l_rsrc = make_rsrc(a.L1f, static_cast<uint32_t>(K) * (rb * 32u));
 
   // the group of this lane's result rows within a unit
   const int half = GS == 64 ? c >> 1 : c;
   struct Codes {
-    uint4 w[UPC];
-    float s[UPC];
+    uint4 w[UPC][NT];
+    float s[UPC][NT];
   };
   auto load_codes = [&](int chunk, Codes& b) __attribute__((always_inline)) {
-    if constexpr (MAIN) {
 #pragma unroll
-      for (int u = 0; u < UPC; ++u) {
-        const int unit = lo + chunk * UPC + u;
-        const bool in = unit < hi;
-        b.w[u] = buf_load16(w_rsrc, in ? static_cast<uint32_t>(col * KB + unit * (kUnit / 2) + c * 16) : kNowhere);
-        b.s[u] = buf_load4f(s_rsrc, in ? (static_cast<uint32_t>(unit * GPU + half) * N + n0 + col) * 4u : kNowhere);
+    for (int u = 0; u < UPC; ++u) {
+      const int unit = lo + chunk * UPC + u;
+      const bool in = unit < hi && !branch;
+      const uint32_t wo = in ? static_cast<uint32_t>(col * KB + unit * (kUnit / 2) + c * 16) : kNowhere;
+      const uint32_t so = in ? (static_cast<uint32_t>(unit * GPU + half) * N + n0 + col) * 4u : kNowhere;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        b.w[u][t] = buf_load16(w_rsrc, wo + static_cast<uint32_t>(t * kCols) * KB);
+        b.s[u][t] = buf_load4f(s_rsrc, so + t * kCols * 4u);
       }
     }
   };
@@ -143,8 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void matvec_kernel(MatvecArgs a) {
     }
   };
   // vector v = token * PIECES + piece; channels past K are staged as zeros
+  const bool staged = sk * 2 + 16 < pitch;
   auto put = [&](int v, uint4 d) __attribute__((always_inline)) {
-    *reinterpret_cast<uint4*>(stage + v * row_bytes(CK) + sk * 2) = d;
+    *reinterpret_cast<uint4*>(stage + v * pitch + sk * 2) = d;
   };
   auto store_x = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -152,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void matvec_kernel(MatvecArgs a) {
       const int m = s * TPI + stok;
       if (s * TPI >= M) break;
       if constexpr (!SMOOTH) {
-        if (m < M) put(m, xr[s]);
+        if (m < M && staged) put(m, xr[s]);
         continue;
       }
       const uint32_t xb[4] = {xr[s].x, xr[s].y, xr[s].z, xr[s].w};
@@ -164,7 +172,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void matvec_kernel(MatvecArgs a) {
         hi_[e] = bf16_pair(v0, v1);
         lo_[e] = bf16_pair(v0 - __uint_as_float(hi_[e] << 16), v1 - __uint_as_float(hi_[e] & 0xFFFF0000u));
       }
-      if (m < M) {
+      if (m < M && staged) {
         put(2 * m, make_uint4(hi_[0], hi_[1], hi_[2], hi_[3]));
         put(2 * m + 1, make_uint4(lo_[0], lo_[1], lo_[2], lo_[3]));
       }
@@ -177,216 +185,329 @@ __global__ __launch_bounds__(64 * kWaves, 2) void matvec_kernel(MatvecArgs a) {
 #pragma unroll
   for (int s = 0; s < SETS; ++s) {
     const int v = s * SL + slot;
-    frag[s] = half == row_half && v < V ? stage + v * row_bytes(CK) + c * 64 : zero;
+    frag[s] = half == row_half && v < V ? stage + v * pitch + c * 64 : zero;
+  }
+  auto fragment = [&](int s, int u, int i) __attribute__((always_inline)) {
+    return __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(frag[s] + u * 256 + i * 16));
+  };
+  // L1 in its fragment order: entry (g, b, h, l, e) holds channel 64 g + 16 (l / 16) + 8 h + e of direction 16 b + l % 16
+  auto l1_fragment = [&](int unit, int b, int i) __attribute__((always_inline)) {
+    const int g = unit * 2 + (c >> 1), l = 16 * (2 * (c & 1) + (i >> 1)) + col;
+    return __builtin_bit_cast(v8bf, buf_load16(l_rsrc, static_cast<uint32_t>(((g * rb + b) * 2 + (i & 1)) * 64 + l) * 16u));
+  };
+
+  // fused t: the one output of this thread needs a row of L2t (no more outputs than threads)
+  const int om = threadIdx.x / kCols, on = n0 + threadIdx.x % kCols;
+  uint4 l2[RB > 0 ? 2 * RB : 1];
+  if constexpr (RB > 0) {
+#pragma unroll
+    for (int q = 0; q < 2 * RB; ++q)
+      if (om < M) l2[q] = reinterpret_cast<const uint4*>(a.L2t + static_cast<int64_t>(on) * (16 * RB))[q];
   }
 
-  v4f acc[MAIN ? SETS : 1], at[RB > 0 ? RB : 1][SETS];
+  v4f acc[TILES][SETS];
 #pragma unroll
-  for (int s = 0; s < (MAIN ? SETS : 1); ++s) acc[s] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < TILES; ++t)
 #pragma unroll
-  for (int b = 0; b < RB; ++b)
+    for (int s = 0; s < SETS; ++s) acc[t][s] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // fused t: a unit's fragments of L1 are requested one unit ahead
+  v8bf l1[RB > 0 ? RB : 1][4];
+  auto load_l1 = [&](int unit) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) at[b][s] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < RB; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l1[t][i] = l1_fragment(unit, t, i);
+  };
 
   auto process = [&](int chunk, const Codes& b) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < UPC; ++u) {
       const int unit = lo + chunk * UPC + u;
       if (unit >= hi) break;
-      v8s f[4];
-      if constexpr (MAIN) {
-        const v8i q = codes_to_fp6(b.w[u]);
+      v8bf f[NT][4];
+      struct Four { v8s f[4]; };
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const v8i q = codes_to_fp6(b.w[u][t]);
         const v6u q6 = {static_cast<unsigned>(q[0]), static_cast<unsigned>(q[1]), static_cast<unsigned>(q[2]),
                         static_cast<unsigned>(q[3]), static_cast<unsigned>(q[4]), static_cast<unsigned>(q[5])};
-        const v32bf d = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q6, 8.0f);
-        struct Four { v8s f[4]; };
-        const Four four = __builtin_bit_cast(Four, d);
+        const Four four = __builtin_bit_cast(Four, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q6, 8.0f));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = four.f[i];
+        for (int i = 0; i < 4; ++i) f[t][i] = __builtin_bit_cast(v8bf, four.f[i]);
       }
-      // L1 fragments: entry (g, b, h, l, e) holds channel 64 g + 16 (l / 16) + 8 h + e of direction 16 b + l % 16
-      v8s l1[RB > 0 ? RB : 1][4];
+      // a set's fragments are read while the one before is multiplied, and not
+      // further ahead (the compiler would read them all, and spill)
+      v8bf x[2][4];
 #pragma unroll
-      for (int bb = 0; bb < RB; ++bb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int g = unit * 2 + (c >> 1), ll = 16 * (2 * (c & 1) + (i >> 1)) + col;
-          l1[bb][i] = __builtin_bit_cast(v8s, buf_load16(l_rsrc, static_cast<uint32_t>(((g * RB + bb) * 2 + (i & 1)) * 64 + ll) * 16u));
-        }
+      for (int i = 0; i < 4; ++i) x[0][i] = fragment(0, u, i);
 #pragma unroll
       for (int s = 0; s < SETS; ++s) {
-        v4f p = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (s + 1 < SETS) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[(s + 1) & 1][i] = fragment(s + 1, u, i);
+        }
+        v4f p[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) p[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint8_t* src = frag[s] + u * 256 + i * 16;
-          const v8bf x = __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(src));
-          if constexpr (MAIN) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(v8bf, f[i]), p, 0, 0, 0);
 #pragma unroll
-          for (int bb = 0; bb < RB; ++bb)
-            at[bb][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(v8bf, l1[bb][i]), at[bb][s], 0, 0, 0);
-        }
-        if constexpr (MAIN) {
+          for (int t = 0; t < NT; ++t) p[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], f[t][i], p[t], 0, 0, 0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[s][e] = __builtin_fmaf(p[e], b.s[u], acc[s][e]);
+          for (int t = 0; t < RB; ++t) acc[NT + t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], l1[t][i], acc[NT + t][s], 0, 0, 0);
         }
-        // many sets: their fragments are not all read ahead (it spilled)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][s][e] = __builtin_fmaf(p[t][e], b.s[u][t], acc[t][s][e]);
         if constexpr (SETS >= 4) __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (RB > 0) load_l1(unit + 1);
     }
+  };
+  // the same against L1: directions 16 (b0 + t) .., no scales
+  struct Branch {
+    v8bf f[NT][4];
+  };
+  auto load_branch = [&](int unit, Branch& l) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l.f[t][i] = l1_fragment(unit, min(b0 + t, rb - 1), i);
   };
 
-  Codes b0, b1;
-  if (chunks > 0) {
-    load_x(0);
-    load_codes(0, b0);
-  }
-  __syncthreads();                 // the empty slot
-  auto step = [&](int chunk, const Codes& now, Codes& next) __attribute__((always_inline)) {
-    store_x();
-    if (chunk + 1 < chunks) {
-      load_x(chunk + 1);
-      load_codes(chunk + 1, next);
+  if (branch) {
+    __syncthreads();               // the empty row
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      Branch l;
+      load_x(chunk);
+      load_branch(lo + chunk * UPC, l);
+      store_x();
+#pragma unroll 1
+      for (int u = 0; u < UPC; ++u) {
+        const int unit = lo + chunk * UPC + u;
+        if (unit >= hi) break;
+        if (u > 0) load_branch(unit, l);
+#pragma unroll
+        for (int s = 0; s < SETS; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const v8bf x = fragment(s, u, i);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, l.f[t][i], acc[t][s], 0, 0, 0);
+          }
+      }
     }
-    process(chunk, now);
-  };
-  for (int chunk = 0; chunk < chunks; chunk += 2) {
-    step(chunk, b0, b1);
-    if (chunk + 1 < chunks) step(chunk + 1, b1, b0);
+  } else {
+    Codes now, next;
+    if (chunks > 0) {
+      load_x(0);
+      load_codes(0, now);
+      if constexpr (RB > 0) load_l1(lo);
+    }
+    __syncthreads();
+    auto step = [&](int chunk, const Codes& b, Codes& ahead) __attribute__((always_inline)) {
+      store_x();
+      if (chunk + 1 < chunks) {
+        load_x(chunk + 1);
+        load_codes(chunk + 1, ahead);
+      }
+      process(chunk, b);
+    };
+    for (int chunk = 0; chunk < chunks; chunk += 2) {
+      step(chunk, now, next);
+      if (chunk + 1 < chunks) step(chunk + 1, next, now);
+    }
   }
 
   // sum over a unit's groups, then the waves' sums through LDS
   __syncthreads();
   float* const red = reinterpret_cast<float*>(lds);
-  auto put_sums = [&](int tile, int s, v4f v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float q = v[e];
-      q += __shfl_xor(q, 32);
-      if constexpr (GS == 32) q += __shfl_xor(q, 16);
-      if (c < SL / 4) red[((wave * TILES + tile) * SETS * SL + s * SL + 4 * c + e) * kCols + col] = q;
-    }
-  };
+  for (int t = 0; t < TILES; ++t)
 #pragma unroll
-  for (int s = 0; s < SETS; ++s) {
-    if constexpr (MAIN) put_sums(0, s, acc[s]);
+    for (int s = 0; s < SETS; ++s)
 #pragma unroll
-    for (int b = 0; b < RB; ++b) put_sums((MAIN ? 1 : 0) + b, s, at[b][s]);
-  }
+      for (int e = 0; e < 4; ++e) {
+        float q = acc[t][s][e];
+        q += __shfl_xor(q, 32);
+        if constexpr (GS == 32) q += __shfl_xor(q, 16);
+        if (c < SL / 4) red[((wave * TILES + t) * SETS * SL + s * SL + 4 * c + e) * kCols + col] = q;
+      }
   __syncthreads();
   auto total = [&](int tile, int m, int j) {
     float s = 0.0f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) s += red[((w * TILES + tile) * SETS * SL + m * PIECES + p) * kCols + j];
+      for (int w = 0; w < waves; ++w) s += red[((w * TILES + tile) * SETS * SL + m * PIECES + p) * kCols + j];
     return s;
   };
-  if constexpr (!MAIN) {
-    for (int i = threadIdx.x; i < M * a.r; i += 64 * kWaves) {
-      const int m = i / a.r, j = i % a.r;
-      a.part[static_cast<int64_t>(blockIdx.x) * M * a.r + i] = total(j >> 4, m, j & 15);
+  if (a.part != nullptr) {
+    const int width = branch ? a.r : N, first = branch ? 16 * b0 : n0, count = min(NT * kCols, width - first);
+    float* const out = (branch ? a.tpart : a.part) + static_cast<int64_t>(split) * M * width + first;
+    for (int i = threadIdx.x; i < M * count; i += 64 * waves) {
+      const int m = i / count, j = i % count;
+      out[static_cast<int64_t>(m) * width + j] = total(j / kCols, m, j % kCols);
     }
-  } else {
-    if (a.r > 0) {
-      for (int i = threadIdx.x; i < M * a.r; i += 64 * kWaves) {
-        float t = 0.0f;
-        if constexpr (RB > 0) {
-          t = total(1 + ((i % a.r) >> 4), i / a.r, i & 15);
-        } else {
-          for (int s = 0; s < a.splits; ++s) t += a.part[static_cast<int64_t>(s) * M * a.r + i];
-        }
-        tl[i] = t;
-      }
-      __syncthreads();
-    }
-    for (int i = threadIdx.x; i < M * kCols; i += 64 * kWaves) {
-      const int m = i / kCols, j = i % kCols;
-      float s = total(0, m, j);
-      const uint4* l2 = reinterpret_cast<const uint4*>(a.L2t + static_cast<int64_t>(n0 + j) * a.r);
-      for (int q = 0; q < a.r / 8; ++q) {
-        const uint4 w = l2[q];
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    return;
+  }
+  if constexpr (RB > 0) {
+    for (int i = threadIdx.x; i < M * (16 * RB); i += 64 * waves) tl[i] = total(NT + (i % (16 * RB)) / 16, i / (16 * RB), i % 16);
+    __syncthreads();
+  }
+  const int count = min(NT * kCols, N - n0);
+  for (int i = threadIdx.x; i < M * count; i += 64 * waves) {
+    const int m = i / count, j = i % count, n = n0 + j;
+    float s = total(j / kCols, m, j % kCols);
+    if constexpr (RB > 0) {         // NT = 1: m = om, n = on
+#pragma unroll
+      for (int q = 0; q < 2 * RB; ++q) {
+        const uint32_t u[4] = {l2[q].x, l2[q].y, l2[q].z, l2[q].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s = __builtin_fmaf(tl[m * a.r + 8 * q + 2 * e], __uint_as_float(u[e] << 16), s);
-          s = __builtin_fmaf(tl[m * a.r + 8 * q + 2 * e + 1], __uint_as_float(u[e] & 0xFFFF0000u), s);
+          s = __builtin_fmaf(tl[m * 16 * RB + 8 * q + 2 * e], __uint_as_float(u[e] << 16), s);
+          s = __builtin_fmaf(tl[m * 16 * RB + 8 * q + 2 * e + 1], __uint_as_float(u[e] & 0xFFFF0000u), s);
         }
       }
-      if (a.bias != nullptr) s += bf16_to_f32(a.bias[n0 + j]);
-      a.y[static_cast<int64_t>(m) * N + n0 + j] = static_cast<uint16_t>(f32_to_bf16_rne(s));
     }
+    if (a.bias != nullptr) s += bf16_to_f32(a.bias[n]);
+    a.y[static_cast<int64_t>(m) * N + n] = static_cast<uint16_t>(f32_to_bf16_rne(s));
   }
 }
 
-template <int GS, int SETS, int RB, bool MAIN, bool SMOOTH>
-hipError_t launch(const MatvecArgs& a, unsigned grid, hipStream_t stream) {
-  constexpr int SL = GS == 64 ? 8 : 4, TILES = (MAIN ? 1 : 0) + RB;
-  constexpr int CK = SETS * SL > 16 ? 256 : 512;     // staged channels: about 16 KB for a wave at most
-  const int stage = kWaves * a.M * (SMOOTH ? 2 : 1) * row_bytes(CK), red = kWaves * TILES * SETS * SL * kCols * 4;
-  const int bytes = (stage > red ? stage : red) + row_bytes(CK) + a.M * a.r * 4;
-  auto kernel = matvec_kernel<GS, SETS, CK, RB, MAIN, SMOOTH>;
+// at most kMaxSplits values `step` apart, all requested before the first is added (a
+// loop would wait for each: 14 parts of t took 7 us)
+__device__ __forceinline__ float sum_parts(const float* p, int64_t step, int count) {
+  float v[kMaxSplits], s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits; ++i) v[i] = i < count ? p[i * step] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits; ++i) s += v[i];
+  return s;
+}
+
+// the parts of K in order, the branch and the bias: 64 channels and four tokens a
+// workgroup, a wave each.  Everything is requested before t is summed.
+__global__ __launch_bounds__(256) void matvec_join_kernel(MatvecArgs a) {
+  constexpr int kTokens = 4;
+  __shared__ float tl[kTokens * 64];
+  const int lane = threadIdx.x & 63, n = blockIdx.x * 64 + lane, m0 = blockIdx.y * kTokens, m = m0 + (threadIdx.x >> 6);
+  const bool mine = n < a.N && m < a.M;
+  float v = 0.0f, bias = 0.0f;
+  uint4 w[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (mine && q < a.r / 8) w[q] = reinterpret_cast<const uint4*>(a.L2t + static_cast<int64_t>(n) * a.r)[q];
+  if (mine) {
+    if (a.bias != nullptr) bias = bf16_to_f32(a.bias[n]);
+    v = sum_parts(a.part + static_cast<int64_t>(m) * a.N + n, static_cast<int64_t>(a.M) * a.N, a.splits);
+  }
+  // this workgroup's tokens have r sums of t each: at most 256, one a thread
+  if (threadIdx.x < min(kTokens, a.M - m0) * a.r)
+    tl[threadIdx.x] = sum_parts(a.tpart + static_cast<int64_t>(m0) * a.r + threadIdx.x, static_cast<int64_t>(a.M) * a.r, a.tsplits);
+  __syncthreads();
+  if (!mine) return;
+  const float* const t = tl + (m - m0) * a.r;
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (q < a.r / 8) {
+      const uint32_t u[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v = __builtin_fmaf(t[8 * q + 2 * e], __uint_as_float(u[e] << 16), v);
+        v = __builtin_fmaf(t[8 * q + 2 * e + 1], __uint_as_float(u[e] & 0xFFFF0000u), v);
+      }
+    }
+  a.y[static_cast<int64_t>(m) * a.N + n] = static_cast<uint16_t>(f32_to_bf16_rne(v + bias));
+}
+
+// How a call runs: `nt` tiles of 16 channels a workgroup; t in the same workgroups
+// (fused), or in `tsplits` workgroups of its own for each part of K, y in `splits`,
+// and a second launch that joins them.
+struct Form {
+  int nt, splits, tsplits;
+  bool fused;
+};
+
+// (a layer with a branch is taken as smoothed: the workspace query does not read inv_smooth)
+Form form_of(int M, int N, int K, int r, int group, bool smooth) {
+  const int units = (K + kUnit - 1) / kUnit, tiles = N / kCols;
+  // t once per workgroup: cheaper than a launch while all of them read little of L1
+  const bool fused = r == 0 || (r == 16 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(8) << 20));
+  const int V = M * (r > 0 || smooth ? 2 : 1);
+  int nt = V <= 4 ? 1 : V <= 8 || V > (group == 64 ? 16 : 8) ? 2 : 4;      // (more than two sets of four tiles spill)
+  if (fused) {
+    while (nt > 1 && tiles < 256 * nt) nt /= 2;
+    if (r > 0) nt = 1;
+    return {nt, 1, 0, true};
+  }
+  if (nt < 2 && tiles < 512) nt = 2;
+  const int blocks = (tiles + nt - 1) / nt;
+  auto within = [](int v, int most) { return v < 1 ? 1 : v < most ? v : most; };
+  const int most = within((units + kWaves - 1) / kWaves, kMaxSplits);
+  return {nt, within(512 / blocks, most), most, false};
+}
+
+template <int GS, int SETS, int NT, int RB, bool SMOOTH>
+hipError_t launch(MatvecArgs a, hipStream_t stream) {
+  constexpr int SL = GS == 64 ? 8 : 4, TILES = NT + RB, CK = chunk_channels(SETS, SL, NT);
+  const int units = (a.K + kUnit - 1) / kUnit, per_split = (units + a.splits - 1) / a.splits;
+  a.blocks = (a.N / kCols + NT - 1) / NT;
+  a.tblocks = (a.r / 16 + NT - 1) / NT;
+  const int grid = a.blocks * a.splits + a.tblocks * a.tsplits;
+  // a wave has a unit at least; the fused t also a thread for each output
+  a.waves = RB == 0 && per_split >= 8 && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
+  const int per = (per_split + a.waves - 1) / a.waves * kUnit;
+  a.pitch = (per < CK ? per : CK) * 2 + 16;
+  const int stage = a.waves * a.M * (SMOOTH ? 2 : 1) * a.pitch, red = a.waves * TILES * SETS * SL * kCols * 4;
+  const int bytes = (stage > red ? stage : red) + a.pitch + a.M * RB * 64;
+  auto kernel = matvec_kernel<GS, SETS, NT, RB, SMOOTH>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), bytes, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(grid)), dim3(64 * a.waves), bytes, stream, a);
   return hipGetLastError();
 }
 
-template <int GS, int RB, bool MAIN, bool SMOOTH>
-hipError_t launch_sets(const MatvecArgs& a, unsigned grid, hipStream_t stream) {
+template <int GS, int NT, int RB, bool SMOOTH>
+hipError_t launch_sets(const MatvecArgs& a, hipStream_t stream) {
   const int n = (a.M * (SMOOTH ? 2 : 1) + (GS == 64 ? 7 : 3)) / (GS == 64 ? 8 : 4);
-  if (n <= 1) return launch<GS, 1, RB, MAIN, SMOOTH>(a, grid, stream);
-  if (n <= 2) return launch<GS, 2, RB, MAIN, SMOOTH>(a, grid, stream);
-  if constexpr (GS == 32 || SMOOTH)
-    if (n <= 4) return launch<GS, 4, RB, MAIN, SMOOTH>(a, grid, stream);
-  if constexpr (GS == 32 && SMOOTH) return launch<GS, 8, RB, MAIN, SMOOTH>(a, grid, stream);
+  if (n <= 1) return launch<GS, 1, NT, RB, SMOOTH>(a, stream);
+  if (n <= 2) return launch<GS, 2, NT, RB, SMOOTH>(a, stream);
+  if constexpr ((GS == 32 || SMOOTH) && NT < 4)
+    if (n <= 4) return launch<GS, 4, NT, RB, SMOOTH>(a, stream);
+  if constexpr (GS == 32 && SMOOTH && NT < 4) return launch<GS, 8, NT, RB, SMOOTH>(a, stream);
   return hipErrorInvalidValue;
 }
 
-template <int RB>
-hipError_t launch_main(const MatvecArgs& a, int group, unsigned grid, hipStream_t stream) {
-  if (a.inv != nullptr)
-    return group == 32 ? launch_sets<32, RB, true, true>(a, grid, stream) : launch_sets<64, RB, true, true>(a, grid, stream);
-  return group == 32 ? launch_sets<32, RB, true, false>(a, grid, stream) : launch_sets<64, RB, true, false>(a, grid, stream);
-}
-
-// t has no scales: its rows are split as for groups of 64
-template <int RB>
-hipError_t launch_t(const MatvecArgs& a, unsigned grid, hipStream_t stream) {
-  return a.inv != nullptr ? launch_sets<64, RB, false, true>(a, grid, stream) : launch_sets<64, RB, false, false>(a, grid, stream);
-}
-
-// t in the main launch: where reading L1 once per workgroup costs less than a launch
-bool fused_t(int N, int K, int r) { return r == 16 && static_cast<int64_t>(N / kCols) * K * r * 2 <= (int64_t(8) << 20); }
-
-int t_splits(int K) {
-  const int units = (K + kUnit - 1) / kUnit, n = (units + kWaves - 1) / kWaves;
-  return n < kMaxTSplits ? n : kMaxTSplits;
+template <int NT, int RB>
+hipError_t launch_main(const MatvecArgs& a, int group, hipStream_t stream) {
+  if (a.inv != nullptr) return group == 32 ? launch_sets<32, NT, RB, true>(a, stream) : launch_sets<64, NT, RB, true>(a, stream);
+  return group == 32 ? launch_sets<32, NT, RB, false>(a, stream) : launch_sets<64, NT, RB, false>(a, stream);
 }
 
 }  // namespace
 
-int64_t matvec_workspace_bytes(int M, int N, int K, int r) {
-  return r == 0 || fused_t(N, K, r) ? 0 : static_cast<int64_t>(t_splits(K)) * M * r * 4;
+int64_t matvec_workspace_bytes(int M, int N, int K, int r, int group) {
+  const Form f = form_of(M, N, K, r, group, true);
+  return f.fused ? 0 : (static_cast<int64_t>(f.splits) * N + static_cast<int64_t>(f.tsplits) * r) * M * 4;
 }
 
 hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, const uint16_t* x, const float* inv_smooth,
                              const uint16_t* L1f, const uint8_t* wq, const float* ws, const uint16_t* L2t,
                              const uint16_t* bias, uint16_t* y, void* workspace, hipStream_t stream) {
-  const MatvecArgs a = {x, inv_smooth, L1f, wq, ws, L2t, bias, y, static_cast<float*>(workspace), M, N, K, r, t_splits(K)};
-  const unsigned grid = static_cast<unsigned>(N / kCols);
-  if (r > 0) {
-    if (fused_t(N, K, r)) return launch_main<1>(a, group, grid, stream);
-    hipError_t e = hipErrorInvalidValue;
-    const unsigned s = static_cast<unsigned>(a.splits);
-    if (r == 16) e = launch_t<1>(a, s, stream);
-    if (r == 32) e = launch_t<2>(a, s, stream);
-    if (r == 48) e = launch_t<3>(a, s, stream);
-    if (r == 64) e = launch_t<4>(a, s, stream);
-    if (e != hipSuccess) return e;
-  }
-  return launch_main<0>(a, group, grid, stream);
+  const Form f = form_of(M, N, K, r, group, inv_smooth != nullptr);
+  float* const part = f.fused ? nullptr : static_cast<float*>(workspace);
+  const MatvecArgs a = {x, inv_smooth, L1f, wq, ws, L2t, bias, y, part, f.fused ? nullptr : part + static_cast<int64_t>(f.splits) * M * N,
+                        M, N, K, r, f.splits, 0, f.tsplits, 0, 0, 0};
+  if (f.fused && r > 0) return launch_main<1, 1>(a, group, stream);
+  const hipError_t e = f.nt == 1 ? launch_main<1, 0>(a, group, stream) : f.nt == 2 ? launch_main<2, 0>(a, group, stream)
+                                                                                   : launch_main<4, 0>(a, group, stream);
+  if (f.fused || e != hipSuccess) return e;
+  hipLaunchKernelGGL(matvec_join_kernel, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>((M + 3) / 4)), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace qwam

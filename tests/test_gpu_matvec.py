@@ -115,6 +115,19 @@ def test_plain(M, group):
         _check(layer, x, Q.asp_matvec(layer, x))
 
 
+@pytest.mark.parametrize("group", [64, 32])
+@pytest.mark.parametrize("smooth", [False, True])
+def test_wide_layers(group, smooth):
+    """Many output channels: wider workgroups, by the tokens' pieces; with a branch and without."""
+    for r in (0, 32):
+        layer = _layer(320, 16400, r, group, smooth=smooth or r > 0, seed=r)
+        if not smooth:
+            layer = dataclasses.replace(layer, inv_smooth=None)
+        for M in (1, 3, 5, 8, 9, 16):
+            x = _x(M, 320)
+            _check(layer, x, Q.asp_matvec(layer, x))
+
+
 def test_largest_width():
     layer = _layer(65536, 32, 16, 64)
     for M in (1, 16):
