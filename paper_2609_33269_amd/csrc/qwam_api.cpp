@@ -450,7 +450,7 @@ qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::Cac
     return fail(QWAM_ERR_UNSUPPORTED, "%s: seqs * q_heads must be at most 2^22", fn);
   if (max_len < 1 || max_len > static_cast<int64_t>(c->table_width) * c->page_size)
     return fail(QWAM_ERR_INVALID_ARG, "%s: max_len must be in [1, table_width * page_size] (got %d)", fn, max_len);
-  if (!qwam::paged_attention_fits(cp, q_heads, max_len))
+  if (!qwam::paged_attention_fits(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len))
     return fail(QWAM_ERR_UNSUPPORTED, "%s: too many sequences and heads of too long a max_len for one launch", fn);
   return QWAM_OK;
 }
@@ -569,7 +569,7 @@ int64_t qwam_paged_attention_workspace(const qwam_cache* c, int32_t q_heads, int
   qwam::CacheParams cp;
   if (check_cache_shape(fn, c, &cp) != QWAM_OK || check_attention(fn, c, cp, q_heads, max_len) != QWAM_OK) return -1;
   ok();
-  return qwam::paged_attention_workspace_bytes(cp, q_heads, max_len);
+  return qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len);
 }
 
 qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uint16_t* q, int64_t q_stride,
@@ -587,7 +587,7 @@ qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uin
   QWAM_OPTIONAL_ELEM(starts, 4);
   QWAM_REQUIRE_PTR(out);
   const bool fp8 = c->type == QWAM_CACHE_FP8;
-  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, q_heads, max_len))) !=
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len))) !=
       QWAM_OK)
     return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;

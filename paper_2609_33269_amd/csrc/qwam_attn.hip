@@ -7,8 +7,8 @@
 // is the bound and everything below is laid out for it:
 //
 //   * A workgroup takes one key head (and up to 16 query heads) of one sequence
-//     over a range of its positions, its four waves a quarter each.  Ranges of
-//     256 to 4096 positions, by the work at hand (chunk_of); their partial results
+//     over a range of its positions, its waves 32 of them in turn.  Ranges of up to
+//     4096 positions, by the work at hand (plan_of); their partial results
 //     (maximum, sum, unnormalized o, float32) are joined by a second launch, in
 //     order.  A context of one range is finished by the first.
 //   * Keys and values go from HBM to registers in whole row pieces and never
@@ -27,6 +27,8 @@
 //     handed out by readlane, so that addresses are scalar.
 //   * Positions outside [start, length) or without a page get weight 0, and their
 //     values are replaced by 0 before the product (0 * NaN is not 0).
+#include <initializer_list>
+
 #include "qwam_device.h"
 #include "qwam_internal.h"
 #include "qwam_mfma.h"
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, int token
 namespace {
 
 constexpr int kAttnWaves = 4;
-constexpr int kMinChunk = 256, kMaxChunk = 4096;     // positions of a workgroup; a wave's lanes hold its pages, 16 positions each
+constexpr int kMaxChunk = 4096;     // positions of a workgroup, the pages of 16 in each lane
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttnArgs {
@@ -126,7 +128,7 @@ __device__ __forceinline__ v8bf bf8(uint32_t a, uint32_t b, uint32_t c, uint32_t
 
 // DP: dim rounded up to 64, 128 or 256; FULL: dim == DP
 template <int DP, bool FP8, bool FULL>
-__global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void paged_attention_kernel(AttnArgs a) {
   constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value
   constexpr int DC = DP / 16;                     // channels of V in a lane
   constexpr int NK = DP * EB / 64;                // 16-byte pieces of K in a lane, per 16 keys
@@ -136,6 +138,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, c = lane >> 4;
+  constexpr int waves = kAttnWaves;
   const int qtiles = (a.group + 15) / 16, rows = a.c.seqs * a.c.heads * qtiles;
   const int range = blockIdx.x / rows, bh = blockIdx.x % rows / qtiles, qt = blockIdx.x % qtiles;
   const int h = bh % a.c.heads, b = bh / a.c.heads;
@@ -145,24 +148,22 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
   const int64_t head_row = static_cast<int64_t>(b) * a.q_heads + h * a.group + q0;
   const int D = FULL ? DP : a.c.dim;
   if (sp.count == 0) {                            // nothing to see: zeros
-    for (int i = threadIdx.x; i < nq * D; i += 64 * kAttnWaves) a.out[head_row * D + i] = 0;
+    for (int i = threadIdx.x; i < nq * D; i += 64 * waves) a.out[head_row * D + i] = 0;
     return;
   }
 
-  // this wave's positions [w0, w1), in tiles of 32
-  const int quarter = a.chunk / kAttnWaves;
-  const int w0 = sp.base + range * a.chunk + wave * quarter;
-  const int w1 = min(w0 + quarter, sp.len);
-  const int tiles = w1 > w0 ? (w1 - w0 + 31) / 32 : 0;
+  // positions [r0, r1) in tiles of 32, every `waves`-th of them this wave's
+  const int r0 = sp.base + range * a.chunk, r1 = min(r0 + a.chunk, sp.len);
+  const int tiles = max(0, (r1 - r0 + 31) / 32 - wave + waves - 1) / waves;
+  auto start = [&](int tile) { return r0 + 32 * (tile * waves + wave); };
 
-  // lane i: the page of positions w0 + 16 i .. +15, or -1
+  // lane i: the page of the first or second 16 positions of tile i / 2, or -1
   int pid = -1;
   {
-    const int p = w0 + 16 * lane;
-    if (16 * lane < quarter && p < w1) {
+    const int p = start(lane >> 1) + 16 * (lane & 1);
+    if (p < r0 + a.chunk && (p >> a.c.page_bits) < a.c.table_width)       // (does not wait for the length)
       pid = a.c.table[static_cast<int64_t>(b) * a.c.table_width + (p >> a.c.page_bits)];
-      if (pid >= a.c.pages) pid = -1;
-    }
+    if (pid >= a.c.pages || p >= r1) pid = -1;
   }
 
   // q as the second operand of S^T: head r, channels of this quarter
@@ -183,14 +184,17 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
   const int row = static_cast<int>(a.c.row_stride) * EB;          // bytes; 16 rows stay below 2^31
   const int row_mask = (1 << a.c.page_bits) - 1;
   // bytes from the head's first row of page 0 to row 0 of 16 positions; a missing page reads page 0, unseen
-  auto place = [&](int i, int& id) -> int64_t {
-    id = __builtin_amdgcn_readlane(pid, i);
+  auto place = [&](int tile, int t, int& id) -> int64_t {
+    id = __builtin_amdgcn_readlane(pid, 2 * tile + t);
     const int64_t page = id < 0 ? 0 : id;
-    return (page * a.c.page_stride + static_cast<int64_t>((w0 + 16 * i) & row_mask) * a.c.row_stride) * EB;
+    return (page * a.c.page_stride + static_cast<int64_t>((start(tile) + 16 * t) & row_mask) * a.c.row_stride) * EB;
   };
 
   uint4 kr[2][NK];
-  uint32_t vr[8][NV];
+  // heads of 64: V comes a tile ahead too (in wider ones its registers cost more waves than that gains: 4 x 16
+  // heads of 64 over 16384 positions 32.6 -> 27.6 us, 16 x 8 x 3 of 128 over 4096 18.2 -> 19.2)
+  constexpr bool V_AHEAD = DP == 64;
+  uint32_t va[8][NV], vb[8][NV];
   int id[2], idn[2];
   int64_t at[2], atn[2];
   auto load_k = [&](const int64_t (&o)[2]) __attribute__((always_inline)) {
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
         if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
       }
   };
-  auto load_v = [&](const int64_t (&o)[2]) __attribute__((always_inline)) {
+  auto load_v = [&](const int64_t (&o)[2], uint32_t (&vr)[8][NV]) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + DC * r * EB);
@@ -227,11 +231,12 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
 
   if (tiles > 0) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) at[t] = place(t, id[t]);
+    for (int t = 0; t < 2; ++t) at[t] = place(0, t, id[t]);
     load_k(at);
+    if constexpr (V_AHEAD) load_v(at, va);
   }
-  for (int tile = 0; tile < tiles; ++tile) {
-    load_v(at);
+  auto turn = [&](int tile, uint32_t (&vr)[8][NV], uint32_t (&vn)[8][NV]) __attribute__((always_inline)) {
+    if constexpr (!V_AHEAD) load_v(at, vr);
     // scores of keys 16 t + 4 c + i, head r
     v4f s[2];
 #pragma unroll
@@ -252,10 +257,11 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
     }
     if (tile + 1 < tiles) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) atn[t] = place(2 * (tile + 1) + t, idn[t]);
+      for (int t = 0; t < 2; ++t) atn[t] = place(tile + 1, t, idn[t]);
       load_k(atn);
+      if constexpr (V_AHEAD) load_v(atn, vn);
     }
-    const int p0 = w0 + 32 * tile;
+    const int p0 = start(tile);
     const bool whole = p0 >= sp.first && p0 + 32 <= sp.len && id[0] >= 0 && id[1] >= 0;
     uint32_t seen = 0xFFu;                        // bit j: the lane's key of slot j
     if (!whole) {
@@ -318,6 +324,14 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
       at[t] = atn[t];
       id[t] = idn[t];
     }
+  };
+  if constexpr (V_AHEAD) {
+    for (int tile = 0; tile < tiles; tile += 2) {
+      turn(tile, va, vb);
+      if (tile + 1 < tiles) turn(tile + 1, vb, va);
+    }
+  } else {
+    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vb);
   }
 
   // join the waves: one maximum, then sums of l and o through LDS
@@ -325,15 +339,14 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
   l += __shfl_xor(l, 32);
   constexpr int RS = DP + 4;                      // floats of an o row in LDS
   float* const sm = smem;                         // [waves][16] maxima, then sums
-  float* const so = smem + 2 * kAttnWaves * 16;   // [waves][nq][RS]
+  float* const so = smem + 2 * waves * 16;        // [waves][nq][RS]
   if (c == 0) {
     sm[wave * 16 + r] = m;
-    sm[(kAttnWaves + wave) * 16 + r] = l;
+    sm[(waves + wave) * 16 + r] = l;
   }
   __syncthreads();
   float mt = sm[r];
-#pragma unroll
-  for (int w = 1; w < kAttnWaves; ++w) mt = fmaxf(mt, sm[w * 16 + r]);
+  for (int w = 1; w < waves; ++w) mt = fmaxf(mt, sm[w * 16 + r]);
   const float f = __builtin_amdgcn_exp2f(m - (mt == -INFINITY ? 0.0f : mt));
   if (r < nq)
 #pragma unroll
@@ -344,16 +357,14 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
             make_float4(acc[e][i] * f, acc[e + 1][i] * f, acc[e + 2][i] * f, acc[e + 3][i] * f);
   __syncthreads();
   const float vs = FP8 ? a.c.v_scale[h] : 1.0f;
-  for (int i = threadIdx.x; i < nq * (D / 4); i += 64 * kAttnWaves) {
+  for (int i = threadIdx.x; i < nq * (D / 4); i += 64 * waves) {
     const int g = i / (D / 4), d = (i % (D / 4)) * 4;
     float top = sm[g], sum = 0.0f;
-#pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, sm[w * 16 + g]);
+    for (int w = 1; w < waves; ++w) top = fmaxf(top, sm[w * 16 + g]);
     const float ref = top == -INFINITY ? 0.0f : top;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-      sum += sm[(kAttnWaves + w) * 16 + g] * __builtin_amdgcn_exp2f(sm[w * 16 + g] - ref);
+    for (int w = 0; w < waves; ++w) {
+      sum += sm[(waves + w) * 16 + g] * __builtin_amdgcn_exp2f(sm[w * 16 + g] - ref);
       const float4 v = *reinterpret_cast<const float4*>(so + (w * nq + g) * RS + d);
       o.x += v.x;
       o.y += v.y;
@@ -376,7 +387,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void paged_attention_kernel(AttnAr
 }
 
 // the ranges of a sequence into one result: one workgroup per (sequence, query
-// head), LR lanes per row of o, the rows dealt out over the others
+// head, 4 LR channels of o), the ranges dealt out over its groups of LR lanes
 template <int LR, bool FP8>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   constexpr int SLOTS = 256 / LR;
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   const Span sp = span_of(a, b);
   if (sp.count <= 1) return;                      // written by the first launch
   const int64_t row = static_cast<int64_t>(blockIdx.x) * a.splits;
-  const int slot = threadIdx.x / LR, d = threadIdx.x % LR * 4, D = a.c.dim;
+  const int slot = threadIdx.x / LR, d = (blockIdx.y * LR + threadIdx.x % LR) * 4, D = a.c.dim;
   float top = -INFINITY;
   for (int s = threadIdx.x; s < sp.count; s += 256) top = fmaxf(top, a.stat[2 * (row + s)]);
 #pragma unroll
@@ -397,21 +408,33 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   const float ref = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int s = slot; s < sp.count; s += SLOTS) {
-    const float2 q = *reinterpret_cast<const float2*>(a.stat + 2 * (row + s));
-    const float f = __builtin_amdgcn_exp2f(q.x - ref);
-    sum = __builtin_fmaf(q.y, f, sum);
-    if (d < D) {
-      const float4 v = *reinterpret_cast<const float4*>(a.part + (row + s) * D + d);
-      o.x = __builtin_fmaf(v.x, f, o.x);
-      o.y = __builtin_fmaf(v.y, f, o.y);
-      o.z = __builtin_fmaf(v.z, f, o.z);
-      o.w = __builtin_fmaf(v.w, f, o.w);
+  // so many rows requested before the first is added
+  constexpr int AHEAD = LR == 8 ? 4 : 8;
+  for (int s0 = slot; s0 < sp.count; s0 += SLOTS * AHEAD) {
+    float2 q[AHEAD];
+    float4 v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int s = s0 + u * SLOTS;
+      q[u] = make_float2(-INFINITY, 0.0f);
+      v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (s < sp.count) {
+        q[u] = *reinterpret_cast<const float2*>(a.stat + 2 * (row + s));
+        if (d < D) v[u] = *reinterpret_cast<const float4*>(a.part + (row + s) * D + d);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const float f = __builtin_amdgcn_exp2f(q[u].x - ref);
+      sum = __builtin_fmaf(q[u].y, f, sum);
+      o.x = __builtin_fmaf(v[u].x, f, o.x);
+      o.y = __builtin_fmaf(v[u].y, f, o.y);
+      o.z = __builtin_fmaf(v[u].z, f, o.z);
+      o.w = __builtin_fmaf(v[u].w, f, o.w);
     }
   }
   so[slot][threadIdx.x % LR] = o;
-  if (d == 0) ss[slot] = sum;
+  if (threadIdx.x % LR == 0) ss[slot] = sum;
   __syncthreads();
   if (slot != 0 || d >= D) return;
   for (int s = 1; s < SLOTS; ++s) {
@@ -432,14 +455,28 @@ int64_t rows_of(const CacheParams& c, int q_heads) {
   return static_cast<int64_t>(c.seqs) * c.heads * ((q_heads / c.heads + 15) / 16);
 }
 
-// positions of a workgroup: enough workgroups for every CU four times, ranges not below 256 positions
-int chunk_of(const CacheParams& c, int q_heads, int max_len) {
-  const int64_t want = (rows_of(c, q_heads) * max_len + 1023) / 1024;
-  const int64_t n = (want + 127) / 128 * 128;
-  return static_cast<int>(n < kMinChunk ? kMinChunk : n > kMaxChunk ? kMaxChunk : n);
-}
+// How a call is laid out: positions of a workgroup (a range), ranges of the longest sequence.
+struct Plan {
+  int chunk, splits;
+};
 
-int splits_of(int max_len, int chunk) { return static_cast<int>((static_cast<int64_t>(max_len) + chunk - 1) / chunk); }
+constexpr int kOneRange = 512;
+
+Plan plan_of(const CacheParams& c, bool fp8, int q_heads, int max_len) {
+  auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
+  const int64_t rows = rows_of(c, q_heads);
+  // one range where a second launch would cost as much as the waves' turns (1.1 us for
+  // each 128 positions of 8 x 3 heads of 128; 64 sequences of 500: 13.5 us, in two ranges 18.6)
+  if (max_len <= kOneRange) return {static_cast<int>(up(max_len, 32)), 1};
+  // enough workgroups for every CU four times; no more than 256 ranges to join, and
+  // their partial results at most 1/16 of what they read
+  const int64_t heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16;
+  int64_t n = (rows * max_len + 1023) / 1024;
+  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 64 * heads / (fp8 ? 1 : 2), int64_t(128)})
+    n = n < least ? least : n;
+  n = up(n, 128) > kMaxChunk ? kMaxChunk : up(n, 128);
+  return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n)};
+}
 
 template <int DP, bool FP8>
 hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
@@ -452,8 +489,11 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((attention_join_kernel<DP / 4, FP8>), dim3(static_cast<unsigned>(a.c.seqs) * a.q_heads), dim3(256), 0, stream, a);
+  const unsigned heads = static_cast<unsigned>(a.c.seqs) * a.q_heads;
+  if (a.splits > 16)
+    hipLaunchKernelGGL((attention_join_kernel<8, FP8>), dim3(heads, (a.c.dim + 31) / 32), dim3(256), 0, stream, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL((attention_join_kernel<DP / 4, FP8>), dim3(heads), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -468,23 +508,23 @@ hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const ui
   return hipGetLastError();
 }
 
-bool paged_attention_fits(const CacheParams& c, int q_heads, int max_len) {
-  return rows_of(c, q_heads) * splits_of(max_len, chunk_of(c, q_heads, max_len)) < (int64_t(1) << 24);
+bool paged_attention_fits(const CacheParams& c, bool fp8, int q_heads, int max_len) {
+  return rows_of(c, q_heads) * plan_of(c, fp8, q_heads, max_len).splits < (int64_t(1) << 23);
 }
 
-int64_t paged_attention_workspace_bytes(const CacheParams& c, int q_heads, int max_len) {
-  const int64_t splits = splits_of(max_len, chunk_of(c, q_heads, max_len));
+int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len) {
+  const int64_t splits = plan_of(c, fp8, q_heads, max_len).splits;
   return splits <= 1 ? 0 : static_cast<int64_t>(c.seqs) * q_heads * splits * (c.dim + 2) * 4;
 }
 
 hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
                                   const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
                                   void* workspace, hipStream_t stream) {
-  const int chunk = chunk_of(c, q_heads, max_len), splits = splits_of(max_len, chunk);
+  const Plan p = plan_of(c, fp8, q_heads, max_len);
   float* const part = static_cast<float*>(workspace);
   const AttnArgs a = {c, q, q_stride, lengths, starts, out, part,
-                      splits > 1 ? part + static_cast<int64_t>(c.seqs) * q_heads * splits * c.dim : nullptr,
-                      q_heads, q_heads / c.heads, max_len, chunk, splits, scale};
+                      p.splits > 1 ? part + static_cast<int64_t>(c.seqs) * q_heads * p.splits * c.dim : nullptr,
+                      q_heads, q_heads / c.heads, max_len, p.chunk, p.splits, scale};
   if (fp8)
     return c.dim <= 64 ? launch_attention<64, true>(a, stream) : c.dim <= 128 ? launch_attention<128, true>(a, stream)
                                                                               : launch_attention<256, true>(a, stream);

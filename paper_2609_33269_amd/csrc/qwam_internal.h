@@ -143,8 +143,8 @@ struct CacheParams {
 constexpr int kMaxHeadGroup = 64;      // query heads per key head
 hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream);
-bool paged_attention_fits(const CacheParams& c, int q_heads, int max_len);      // one launch's workgroups
-int64_t paged_attention_workspace_bytes(const CacheParams& c, int q_heads, int max_len);
+bool paged_attention_fits(const CacheParams& c, bool fp8, int q_heads, int max_len);      // one launch's workgroups
+int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len);
 hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
                                   const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
                                   void* workspace, hipStream_t stream);
