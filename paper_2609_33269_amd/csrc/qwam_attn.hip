@@ -45,37 +45,38 @@ __device__ __forceinline__ uint32_t fp8x4(float a, float b, float c, float d) {
 
 }  // namespace
 
-// one thread per 8 values of a token's head, keys (blockIdx.y = 0) or values (1)
+// one thread per 8 keys and the 8 values beside them (at most 2^29 threads, so that indexes are divided in 32 bits)
 template <bool FP8>
-__global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, int tokens, const uint16_t* k, int64_t k_stride,
+__global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t threads, const uint16_t* k, int64_t k_stride,
                                                         const uint16_t* v, int64_t v_stride, const int32_t* seq,
                                                         const int32_t* pos) {
-  const int per_head = c.dim / 8, per_token = c.heads * per_head;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int t = static_cast<int>(i / per_token), w = static_cast<int>(i % per_token);
-  if (t >= tokens) return;
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= threads) return;
+  const uint32_t per_head = c.dim / 8, row = i / per_head, t = row / c.heads, head = row - t * c.heads, d = (i - row * per_head) * 8;
   const int s = seq[t], q = pos[t];
+  const uint4 in[2] = {*reinterpret_cast<const uint4*>(k + t * k_stride + head * c.dim + d),
+                       *reinterpret_cast<const uint4*>(v + t * v_stride + head * c.dim + d)};
   if (s < 0 || s >= c.seqs || q < 0 || (q >> c.page_bits) >= c.table_width) return;
   const int page = c.table[static_cast<int64_t>(s) * c.table_width + (q >> c.page_bits)];
   if (page < 0 || page >= c.pages) return;
-  const int head = w / per_head, d = (w % per_head) * 8;
-  const uint16_t* src = blockIdx.y == 0 ? k + t * k_stride : v + t * v_stride;
-  const uint4 in = *reinterpret_cast<const uint4*>(src + head * c.dim + d);
   const int64_t at = page * c.page_stride + head * c.head_stride + (q & ((1 << c.page_bits) - 1)) * c.row_stride + d;
-  void* base = blockIdx.y == 0 ? c.k : c.v;
-  if constexpr (FP8) {
-    const float scale = (blockIdx.y == 0 ? c.k_scale : c.v_scale)[head];
-    float f[8];
-    const uint32_t u[4] = {in.x, in.y, in.z, in.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = bf16_to_f32((u[e >> 1] >> (16 * (e & 1))) & 0xFFFFu) / scale;
-      f[e] = x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f);
+  for (int w = 0; w < 2; ++w) {
+    void* const base = w == 0 ? c.k : c.v;
+    if constexpr (FP8) {
+      const float scale = (w == 0 ? c.k_scale : c.v_scale)[head];
+      float f[8];
+      const uint32_t u[4] = {in[w].x, in[w].y, in[w].z, in[w].w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = bf16_to_f32((u[e >> 1] >> (16 * (e & 1))) & 0xFFFFu) / scale;
+        f[e] = x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f);
+      }
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(base) + at) =
+          make_uint2(fp8x4(f[0], f[1], f[2], f[3]), fp8x4(f[4], f[5], f[6], f[7]));
+    } else {
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) = in[w];
     }
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(base) + at) =
-        make_uint2(fp8x4(f[0], f[1], f[2], f[3]), fp8x4(f[4], f[5], f[6], f[7]));
-  } else {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) = in;
   }
 }
 
@@ -501,10 +502,10 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
 
 hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream) {
-  const int64_t n = static_cast<int64_t>(tokens) * c.heads * (c.dim / 8);
-  const dim3 grid(static_cast<unsigned>((n + 255) / 256), 2);
-  if (fp8) hipLaunchKernelGGL((kv_append_kernel<true>), grid, dim3(256), 0, stream, c, tokens, k, k_stride, v, v_stride, seq, pos);
-  else hipLaunchKernelGGL((kv_append_kernel<false>), grid, dim3(256), 0, stream, c, tokens, k, k_stride, v, v_stride, seq, pos);
+  const uint32_t n = static_cast<uint32_t>(static_cast<int64_t>(tokens) * c.heads * (c.dim / 8));
+  const dim3 grid((n + 255) / 256), block(256);
+  if (fp8) hipLaunchKernelGGL((kv_append_kernel<true>), grid, block, 0, stream, c, n, k, k_stride, v, v_stride, seq, pos);
+  else hipLaunchKernelGGL((kv_append_kernel<false>), grid, block, 0, stream, c, n, k, k_stride, v, v_stride, seq, pos);
   return hipGetLastError();
 }
 
