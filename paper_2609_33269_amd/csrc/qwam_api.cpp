@@ -462,7 +462,7 @@ extern "C" {
 int64_t qwam_asp_matvec_workspace(const qwam_layer* L, int32_t M) {
   if (check_matvec("qwam_asp_matvec_workspace", L, M) != QWAM_OK) return -1;
   ok();
-  return qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->group);
+  return qwam::matvec_workspace_bytes(M, L->N, L->K, L->r);
 }
 
 qwam_status qwam_asp_matvec(const qwam_layer* L, int32_t M, const uint16_t* x, uint16_t* y, void* workspace,
@@ -482,7 +482,7 @@ qwam_status qwam_asp_matvec(const qwam_layer* L, int32_t M, const uint16_t* x, u
     return fail(QWAM_ERR_MISALIGNED, "%s: bias is not 16-byte aligned", fn);
   QWAM_REQUIRE_PTR(x);
   QWAM_REQUIRE_PTR(y);
-  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->group))) != QWAM_OK)
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::matvec_workspace_bytes(M, L->N, L->K, L->r))) != QWAM_OK)
     return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;
   return launched(fn, qwam::launch_asp_matvec(M, L->N, L->K, L->r, L->group, x, L->inv_smooth, L->L1f, L->wq, L->ws, L->L2t,

@@ -15,12 +15,13 @@
 //   * x~ = x * inv_smooth is not a bf16 number.  It enters as two, hi = bf16(x~)
 //     and lo = bf16(x~ - hi), within 2^-17 of x~: each piece is a row of its own
 //     (few tokens leave most of the 16 rows empty anyway).
-//   * A wave's 16 bytes per lane are 32 consecutive codes of a row, so one MFMA
-//     spans 128 channels: two groups of 64 or four of 32, each with its own scale.
-//     The rows are therefore split between the groups (eight rows each, or
-//     four), a row holding zeros outside its group: the result rows of a
-//     group are its partial sums and take its scale.  More vectors than rows are
-//     further sets of rows against the same codes.
+//   * A wave's 16 bytes per lane are 32 consecutive codes of a row, so its four
+//     quarters hold 128 channels: two groups of 64 or four of 32, each with its own
+//     scale, while an MFMA sums over the quarters.  Half-wave and 16-lane swaps (eight
+//     instructions a step) first give every quarter its share of each group.
+//     (Rows that hold zeros outside their group do without the swaps, but need two or
+//     four times the MFMAs and LDS reads from 8 or 4 vectors on: 14336 x 3072, 7 tokens,
+//     groups of 32 took 18.7 us so.)
 //   * The pieces are staged in the wave's own part of LDS, CK channels at a time,
 //     while the codes of the next CK are on their way; no barrier until the end.
 //   * t comes from the same instructions (L1 in fragment order as the other
@@ -61,18 +62,32 @@ struct MatvecArgs {
 
 // A staged vector: the channels of a chunk (fewer where a wave has fewer) and 16
 // bytes more, so that the rows of a fragment read lie on different banks.
-constexpr int chunk_channels(int sets, int sl, int nt) { return sets * sl > 16 || nt > 1 ? 256 : 512; }
+constexpr int chunk_channels(int mv, int nt) { return mv > 16 || nt > 1 ? 256 : 512; }
+constexpr int kRows = 16;         // vectors of a set
 
-template <int GS, int SETS, int NT, int RB, bool SMOOTH>
+// the upper 32 lanes' a and the lower 32 lanes' b change places; the same for odd and even rows of 16 lanes
+__device__ __forceinline__ void swap32(unsigned& a, unsigned& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+__device__ __forceinline__ void swap16(unsigned& a, unsigned& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
+// MV: vectors the instance has registers for
+template <int GS, int MV, int NT, int RB, bool SMOOTH>
 __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a) {
-  constexpr int SL = GS == 64 ? 8 : 4;               // rows (vectors) of a set
   constexpr int GPU = kUnit / GS;                    // groups of a unit
-  constexpr int CK = chunk_channels(SETS, SL, NT);   // channels staged at a time
+  constexpr int SETS = (MV + kRows - 1) / kRows;
+  constexpr int CK = chunk_channels(MV, NT);         // channels staged at a time
   constexpr int UPC = CK / kUnit;                    // units of a chunk
   constexpr int LPT = CK / 8;                        // lanes that stage one token's chunk, 8 channels each
   constexpr int TPI = 64 / LPT;                      // tokens staged at once
   constexpr int PIECES = SMOOTH ? 2 : 1;             // of a token's x~
-  constexpr int NX = (SETS * SL / PIECES + TPI - 1) / TPI;    // staging steps
+  constexpr int NX = (MV / PIECES + TPI - 1) / TPI;           // staging steps
   constexpr int TILES = NT + RB;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
 
@@ -94,7 +109,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   const int chunks = (hi - lo + UPC - 1) / UPC;
 
   uint8_t* const stage = lds + wave * V * pitch;
-  const int stage_all = waves * V * pitch, red_all = waves * TILES * SETS * SL * kCols * 4;
+  const int stage_all = waves * V * pitch, red_all = waves * TILES * SETS * kRows * kCols * 4;
   uint8_t* const zero = lds + max(stage_all, red_all);
   float* const tl = reinterpret_cast<float*>(zero + pitch);
   for (int i = threadIdx.x; i < pitch / 16; i += 64 * waves) reinterpret_cast<uint4*>(zero)[i] = make_uint4(0, 0, 0, 0);
@@ -111,8 +126,8 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   const int rb = a.r >> 4;
   const buf_rsrc l_rsrc = make_rsrc(a.L1f, static_cast<uint32_t>(K) * (rb * 32u));
 
-  // the group of this lane's result rows within a unit
-  const int half = GS == 64 ? c >> 1 : c;
+  // the group of a unit whose scale this lane loads
+  const int sgroup = GS == 64 ? c >> 1 : c;
   struct Codes {
     uint4 w[UPC][NT];
     float s[UPC][NT];
@@ -123,7 +138,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
       const int unit = lo + chunk * UPC + u;
       const bool in = unit < hi && !branch;
       const uint32_t wo = in ? static_cast<uint32_t>(col * KB + unit * (kUnit / 2) + c * 16) : kNowhere;
-      const uint32_t so = in ? (static_cast<uint32_t>(unit * GPU + half) * N + n0 + col) * 4u : kNowhere;
+      const uint32_t so = in ? (static_cast<uint32_t>(unit * GPU + sgroup) * N + n0 + col) * 4u : kNowhere;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         b.w[u][t] = buf_load16(w_rsrc, wo + static_cast<uint32_t>(t * kCols) * KB);
@@ -179,21 +194,21 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
     }
   };
 
-  // this lane's row: (group of the unit, vector of the set); outside its group it reads zeros
-  const int row_half = GS == 64 ? col >> 3 : col >> 2, slot = col & (SL - 1);
+  // Channels of fragment i of a unit in quarter c, after the codes' swaps: 32 i + 8 c .. (groups
+  // of 32), 64 (i / 2) + 32 (c % 2) + 16 (c / 2) + 8 (i % 2) .. (of 64)
   const uint8_t* frag[SETS];
 #pragma unroll
   for (int s = 0; s < SETS; ++s) {
-    const int v = s * SL + slot;
-    frag[s] = half == row_half && v < V ? stage + v * pitch + c * 64 : zero;
+    const int v = s * kRows + col;
+    frag[s] = v < V ? stage + v * pitch + (GS == 64 ? 64 * (c & 1) + 32 * (c >> 1) : 16 * c) : zero;
   }
   auto fragment = [&](int s, int u, int i) __attribute__((always_inline)) {
-    return __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(frag[s] + u * 256 + i * 16));
+    return __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(frag[s] + u * 256 + (GS == 64 ? 128 * (i >> 1) + 16 * (i & 1) : 64 * i)));
   };
   // L1 in its fragment order: entry (g, b, h, l, e) holds channel 64 g + 16 (l / 16) + 8 h + e of direction 16 b + l % 16
   auto l1_fragment = [&](int unit, int b, int i) __attribute__((always_inline)) {
-    const int g = unit * 2 + (c >> 1), l = 16 * (2 * (c & 1) + (i >> 1)) + col;
-    return __builtin_bit_cast(v8bf, buf_load16(l_rsrc, static_cast<uint32_t>(((g * rb + b) * 2 + (i & 1)) * 64 + l) * 16u));
+    const int g = unit * 2 + (i >> 1), l = 16 * (2 * (GS == 64 ? c & 1 : i & 1) + (c >> 1)) + col, h = GS == 64 ? i & 1 : c & 1;
+    return __builtin_bit_cast(v8bf, buf_load16(l_rsrc, static_cast<uint32_t>(((g * rb + b) * 2 + h) * 64 + l) * 16u));
   };
 
   // fused t: the one output of this thread needs a row of L2t (no more outputs than threads)
@@ -226,18 +241,44 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
       const int unit = lo + chunk * UPC + u;
       if (unit >= hi) break;
       v8bf f[NT][4];
-      struct Four { v8s f[4]; };
+      float sc[NT][GPU];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const v8i q = codes_to_fp6(b.w[u][t]);
         const v6u q6 = {static_cast<unsigned>(q[0]), static_cast<unsigned>(q[1]), static_cast<unsigned>(q[2]),
                         static_cast<unsigned>(q[3]), static_cast<unsigned>(q[4]), static_cast<unsigned>(q[5])};
-        const Four four = __builtin_bit_cast(Four, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q6, 8.0f));
+        struct Words { unsigned w[16]; };
+        Words d = __builtin_bit_cast(Words, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q6, 8.0f));
+        // the halves' second and first 16 channels change places: words 0-7 now belong to
+        // the first 64 channels in every lane, 8-15 to the others
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[t][i] = __builtin_bit_cast(v8bf, four.f[i]);
+        for (int j = 0; j < 8; ++j) swap32(d.w[j], d.w[8 + j]);
+        unsigned s0 = __float_as_uint(b.s[u][t]), s1 = s0;
+        swap32(s0, s1);
+        if constexpr (GS == 32) {
+          // and the same within each half, by 8 channels: words 4i .. 4i + 3 belong to group i
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            swap16(d.w[j], d.w[4 + j]);
+            swap16(d.w[8 + j], d.w[12 + j]);
+          }
+          unsigned s2 = s1, s3 = s1;
+          s1 = s0;
+          swap16(s0, s1);
+          swap16(s2, s3);
+          sc[t][0] = __uint_as_float(s0);
+          sc[t][1] = __uint_as_float(s1);
+          sc[t][GPU - 2] = __uint_as_float(s2);
+          sc[t][GPU - 1] = __uint_as_float(s3);
+        } else {
+          sc[t][0] = __uint_as_float(s0);
+          sc[t][1] = __uint_as_float(s1);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          f[t][i] = __builtin_bit_cast(v8bf, make_uint4(d.w[4 * i], d.w[4 * i + 1], d.w[4 * i + 2], d.w[4 * i + 3]));
       }
-      // a set's fragments are read while the one before is multiplied, and not
-      // further ahead (the compiler would read them all, and spill)
+      // a set's fragments are read while the one before is multiplied
       v8bf x[2][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[0][i] = fragment(0, u, i);
@@ -247,21 +288,23 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[(s + 1) & 1][i] = fragment(s + 1, u, i);
         }
-        v4f p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int g = 0; g < GPU; ++g) {
+          v4f p[NT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+          for (int t = 0; t < NT; ++t) p[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) p[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], f[t][i], p[t], 0, 0, 0);
+          for (int i = g * (4 / GPU); i < (g + 1) * (4 / GPU); ++i) {
 #pragma unroll
-          for (int t = 0; t < RB; ++t) acc[NT + t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], l1[t][i], acc[NT + t][s], 0, 0, 0);
+            for (int t = 0; t < NT; ++t) p[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], f[t][i], p[t], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < RB; ++t) acc[NT + t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], l1[t][i], acc[NT + t][s], 0, 0, 0);
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][s][e] = __builtin_fmaf(p[t][e], sc[t][g], acc[t][s][e]);
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][s][e] = __builtin_fmaf(p[t][e], b.s[u][t], acc[t][s][e]);
-        if constexpr (SETS >= 4) __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (RB > 0) load_l1(unit + 1);
     }
@@ -321,7 +364,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
     }
   }
 
-  // sum over a unit's groups, then the waves' sums through LDS
+  // the waves' sums through LDS: row 4 c + e, column col of each tile
   __syncthreads();
   float* const red = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -329,18 +372,13 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
 #pragma unroll
     for (int s = 0; s < SETS; ++s)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float q = acc[t][s][e];
-        q += __shfl_xor(q, 32);
-        if constexpr (GS == 32) q += __shfl_xor(q, 16);
-        if (c < SL / 4) red[((wave * TILES + t) * SETS * SL + s * SL + 4 * c + e) * kCols + col] = q;
-      }
+      for (int e = 0; e < 4; ++e) red[((wave * TILES + t) * SETS * kRows + s * kRows + 4 * c + e) * kCols + col] = acc[t][s][e];
   __syncthreads();
   auto total = [&](int tile, int m, int j) {
     float s = 0.0f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
-      for (int w = 0; w < waves; ++w) s += red[((w * TILES + tile) * SETS * SL + m * PIECES + p) * kCols + j];
+      for (int w = 0; w < waves; ++w) s += red[((w * TILES + tile) * SETS * kRows + m * PIECES + p) * kCols + j];
     return s;
   };
   if (a.part != nullptr) {
@@ -431,27 +469,30 @@ struct Form {
 };
 
 // (a layer with a branch is taken as smoothed: the workspace query does not read inv_smooth)
-Form form_of(int M, int N, int K, int r, int group, bool smooth) {
+Form form_of(int M, int N, int K, int r, bool smooth) {
   const int units = (K + kUnit - 1) / kUnit, tiles = N / kCols;
   // t once per workgroup: cheaper than a launch while all of them read little of L1
   const bool fused = r == 0 || (r == 16 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(8) << 20));
   const int V = M * (r > 0 || smooth ? 2 : 1);
-  int nt = V <= 4 ? 1 : V <= 8 || V > (group == 64 ? 16 : 8) ? 2 : 4;      // (more than two sets of four tiles spill)
+  // Wider workgroups stage x for more channels; the widest hold fewer waves.  4096 x 28672, plain, one token 14.5 us with
+  // one tile and 15.6 with two, 8 tokens 22.5 and 18.2, 16 tokens 20.7 with two and 19.6 with four.
   if (fused) {
+    int nt = r > 0 || V <= 4 ? 1 : V <= 8 || V > 16 ? 2 : 4;      // (two sets of four tiles spill)
     while (nt > 1 && tiles < 256 * nt) nt /= 2;
-    if (r > 0) nt = 1;
     return {nt, 1, 0, true};
   }
-  if (nt < 2 && tiles < 512) nt = 2;
-  const int blocks = (tiles + nt - 1) / nt;
+  // 3072 x 9216, rank 32, one token 10.5 us with one tile and 11.7 with two (fewer channels: the same)
+  const int nt = V <= 4 && tiles >= 512 ? 1 : 2, blocks = (tiles + nt - 1) / nt;
   auto within = [](int v, int most) { return v < 1 ? 1 : v < most ? v : most; };
   const int most = within((units + kWaves - 1) / kWaves, kMaxSplits);
-  return {nt, within(512 / blocks, most), most, false};
+  // about 512 workgroups, and no more of the largest, of which a CU holds two: 14336 x 3072, 16 tokens, 18.4 us in five
+  // parts, 20.9 in four, 22.4 in eight; 3072 x 9216, 4 tokens, 13.2 us in one and 11.5 in two, 16 tokens 17.9 and 19.7
+  return {nt, within((V > 16 ? 512 : 512 + blocks / 2) / blocks, most), most, false};
 }
 
-template <int GS, int SETS, int NT, int RB, bool SMOOTH>
+template <int GS, int MV, int NT, int RB, bool SMOOTH>
 hipError_t launch(MatvecArgs a, hipStream_t stream) {
-  constexpr int SL = GS == 64 ? 8 : 4, TILES = NT + RB, CK = chunk_channels(SETS, SL, NT);
+  constexpr int SETS = (MV + kRows - 1) / kRows, TILES = NT + RB, CK = chunk_channels(MV, NT);
   const int units = (a.K + kUnit - 1) / kUnit, per_split = (units + a.splits - 1) / a.splits;
   a.blocks = (a.N / kCols + NT - 1) / NT;
   a.tblocks = (a.r / 16 + NT - 1) / NT;
@@ -460,9 +501,9 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   a.waves = RB == 0 && per_split >= 8 && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
   const int per = (per_split + a.waves - 1) / a.waves * kUnit;
   a.pitch = (per < CK ? per : CK) * 2 + 16;
-  const int stage = a.waves * a.M * (SMOOTH ? 2 : 1) * a.pitch, red = a.waves * TILES * SETS * SL * kCols * 4;
+  const int stage = a.waves * a.M * (SMOOTH ? 2 : 1) * a.pitch, red = a.waves * TILES * SETS * kRows * kCols * 4;
   const int bytes = (stage > red ? stage : red) + a.pitch + a.M * RB * 64;
-  auto kernel = matvec_kernel<GS, SETS, NT, RB, SMOOTH>;
+  auto kernel = matvec_kernel<GS, MV, NT, RB, SMOOTH>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
@@ -472,33 +513,32 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
 }
 
 template <int GS, int NT, int RB, bool SMOOTH>
-hipError_t launch_sets(const MatvecArgs& a, hipStream_t stream) {
-  const int n = (a.M * (SMOOTH ? 2 : 1) + (GS == 64 ? 7 : 3)) / (GS == 64 ? 8 : 4);
-  if (n <= 1) return launch<GS, 1, NT, RB, SMOOTH>(a, stream);
-  if (n <= 2) return launch<GS, 2, NT, RB, SMOOTH>(a, stream);
-  if constexpr ((GS == 32 || SMOOTH) && NT < 4)
-    if (n <= 4) return launch<GS, 4, NT, RB, SMOOTH>(a, stream);
-  if constexpr (GS == 32 && SMOOTH && NT < 4) return launch<GS, 8, NT, RB, SMOOTH>(a, stream);
+hipError_t launch_vectors(const MatvecArgs& a, hipStream_t stream) {
+  const int V = a.M * (SMOOTH ? 2 : 1);
+  if constexpr (NT <= 2)
+    if (V <= 4) return launch<GS, 4, NT, RB, SMOOTH>(a, stream);
+  if (V <= 16) return launch<GS, 16, NT, RB, SMOOTH>(a, stream);
+  if constexpr (SMOOTH && NT <= 2) return launch<GS, 32, NT, RB, SMOOTH>(a, stream);
   return hipErrorInvalidValue;
 }
 
 template <int NT, int RB>
 hipError_t launch_main(const MatvecArgs& a, int group, hipStream_t stream) {
-  if (a.inv != nullptr) return group == 32 ? launch_sets<32, NT, RB, true>(a, stream) : launch_sets<64, NT, RB, true>(a, stream);
-  return group == 32 ? launch_sets<32, NT, RB, false>(a, stream) : launch_sets<64, NT, RB, false>(a, stream);
+  if (a.inv != nullptr) return group == 32 ? launch_vectors<32, NT, RB, true>(a, stream) : launch_vectors<64, NT, RB, true>(a, stream);
+  return group == 32 ? launch_vectors<32, NT, RB, false>(a, stream) : launch_vectors<64, NT, RB, false>(a, stream);
 }
 
 }  // namespace
 
-int64_t matvec_workspace_bytes(int M, int N, int K, int r, int group) {
-  const Form f = form_of(M, N, K, r, group, true);
+int64_t matvec_workspace_bytes(int M, int N, int K, int r) {
+  const Form f = form_of(M, N, K, r, true);
   return f.fused ? 0 : (static_cast<int64_t>(f.splits) * N + static_cast<int64_t>(f.tsplits) * r) * M * 4;
 }
 
 hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, const uint16_t* x, const float* inv_smooth,
                              const uint16_t* L1f, const uint8_t* wq, const float* ws, const uint16_t* L2t,
                              const uint16_t* bias, uint16_t* y, void* workspace, hipStream_t stream) {
-  const Form f = form_of(M, N, K, r, group, inv_smooth != nullptr);
+  const Form f = form_of(M, N, K, r, inv_smooth != nullptr);
   float* const part = f.fused ? nullptr : static_cast<float*>(workspace);
   const MatvecArgs a = {x, inv_smooth, L1f, wq, ws, L2t, bias, y, part, f.fused ? nullptr : part + static_cast<int64_t>(f.splits) * M * N,
                         M, N, K, r, f.splits, 0, f.tsplits, 0, 0, 0};
