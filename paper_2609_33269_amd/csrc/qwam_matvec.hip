@@ -17,11 +17,12 @@
 //     (few tokens leave most of the 16 rows empty anyway).
 //   * A wave's 16 bytes per lane are 32 consecutive codes of a row, so its four
 //     quarters hold 128 channels: two groups of 64 or four of 32, each with its own
-//     scale, while an MFMA sums over the quarters.  Half-wave and 16-lane swaps (eight
-//     instructions a step) first give every quarter its share of each group.
-//     (Rows that hold zeros outside their group do without the swaps, but need two or
-//     four times the MFMAs and LDS reads from 8 or 4 vectors on: 14336 x 3072, 7 tokens,
-//     groups of 32 took 18.7 us so.)
+//     scale, while an MFMA sums over the quarters.  Up to four vectors have a row per
+//     group, which holds zeros outside it.  For more, half-wave and 16-lane swaps
+//     (eight or sixteen instructions a step) first give every quarter its share of
+//     each group, and a vector has one row.  (The swaps for all: one token at 4096 x 28672 14.6 us
+//     instead of 14.0.  Rows per group for all: two to four times the MFMAs and LDS
+//     reads, 18.7 us instead of 16.5 for 7 tokens at 14336 x 3072 in groups of 32.)
 //   * The pieces are staged in the wave's own part of LDS, CK channels at a time,
 //     while the codes of the next CK are on their way; no barrier until the end.
 //   * t comes from the same instructions (L1 in fragment order as the other
@@ -83,6 +84,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   constexpr int GPU = kUnit / GS;                    // groups of a unit
   constexpr int SETS = (MV + kRows - 1) / kRows;
   constexpr int CK = chunk_channels(MV, NT);         // channels staged at a time
+  // row 4 g + v is vector v within group g of a unit; not with t beside y, whose fragments of L1 then come in
+  // smaller pieces (1024 x 1024 4.9 us instead of 4.6)
+  constexpr bool GROUP_ROWS = MV == 4 && RB == 0;
   constexpr int UPC = CK / kUnit;                    // units of a chunk
   constexpr int LPT = CK / 8;                        // lanes that stage one token's chunk, 8 channels each
   constexpr int TPI = 64 / LPT;                      // tokens staged at once
@@ -126,8 +130,8 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   const int rb = a.r >> 4;
   const buf_rsrc l_rsrc = make_rsrc(a.L1f, static_cast<uint32_t>(K) * (rb * 32u));
 
-  // the group of a unit whose scale this lane loads
-  const int sgroup = GS == 64 ? c >> 1 : c;
+  // the group of a unit whose scale this lane loads (with rows per group, that of its result rows)
+  const int sgroup = GS == 32 ? c : GROUP_ROWS ? c & 1 : c >> 1;
   struct Codes {
     uint4 w[UPC][NT];
     float s[UPC][NT];
@@ -194,20 +198,23 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
     }
   };
 
-  // Channels of fragment i of a unit in quarter c, after the codes' swaps: 32 i + 8 c .. (groups
-  // of 32), 64 (i / 2) + 32 (c % 2) + 16 (c / 2) + 8 (i % 2) .. (of 64)
+  // Channels of fragment i of a unit in quarter c: 32 c + 8 i .. as the codes are loaded, after their
+  // swaps 32 i + 8 c .. (groups of 32) or 64 (i / 2) + 32 (c % 2) + 16 (c / 2) + 8 (i % 2) .. (of 64)
   const uint8_t* frag[SETS];
 #pragma unroll
   for (int s = 0; s < SETS; ++s) {
-    const int v = s * kRows + col;
-    frag[s] = v < V ? stage + v * pitch + (GS == 64 ? 64 * (c & 1) + 32 * (c >> 1) : 16 * c) : zero;
+    const int v = GROUP_ROWS ? col & 3 : s * kRows + col;
+    const bool mine = v < V && (!GROUP_ROWS || (GS == 64 ? c >> 1 : c) == col >> 2);
+    frag[s] = mine ? stage + v * pitch + (GROUP_ROWS ? 64 * c : GS == 64 ? 64 * (c & 1) + 32 * (c >> 1) : 16 * c) : zero;
   }
   auto fragment = [&](int s, int u, int i) __attribute__((always_inline)) {
-    return __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(frag[s] + u * 256 + (GS == 64 ? 128 * (i >> 1) + 16 * (i & 1) : 64 * i)));
+    const int at = GROUP_ROWS ? 16 * i : GS == 64 ? 128 * (i >> 1) + 16 * (i & 1) : 64 * i;
+    return __builtin_bit_cast(v8bf, *reinterpret_cast<const v8s*>(frag[s] + u * 256 + at));
   };
   // L1 in its fragment order: entry (g, b, h, l, e) holds channel 64 g + 16 (l / 16) + 8 h + e of direction 16 b + l % 16
   auto l1_fragment = [&](int unit, int b, int i) __attribute__((always_inline)) {
-    const int g = unit * 2 + (i >> 1), l = 16 * (2 * (GS == 64 ? c & 1 : i & 1) + (c >> 1)) + col, h = GS == 64 ? i & 1 : c & 1;
+    const int k = GROUP_ROWS ? 32 * c + 8 * i : GS == 64 ? 64 * (i >> 1) + 32 * (c & 1) + 16 * (c >> 1) + 8 * (i & 1) : 32 * i + 8 * c;
+    const int g = unit * 2 + (k >> 6), l = (k & 48) + col, h = k >> 3 & 1;
     return __builtin_bit_cast(v8bf, buf_load16(l_rsrc, static_cast<uint32_t>(((g * rb + b) * 2 + h) * 64 + l) * 16u));
   };
 
@@ -241,6 +248,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
       const int unit = lo + chunk * UPC + u;
       if (unit >= hi) break;
       v8bf f[NT][4];
+      constexpr int SUMS = GROUP_ROWS ? 1 : GPU;     // products with a scale of their own
       float sc[NT][GPU];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -249,30 +257,31 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
                         static_cast<unsigned>(q[3]), static_cast<unsigned>(q[4]), static_cast<unsigned>(q[5])};
         struct Words { unsigned w[16]; };
         Words d = __builtin_bit_cast(Words, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q6, 8.0f));
-        // the halves' second and first 16 channels change places: words 0-7 now belong to
-        // the first 64 channels in every lane, 8-15 to the others
-#pragma unroll
-        for (int j = 0; j < 8; ++j) swap32(d.w[j], d.w[8 + j]);
-        unsigned s0 = __float_as_uint(b.s[u][t]), s1 = s0;
-        swap32(s0, s1);
-        if constexpr (GS == 32) {
-          // and the same within each half, by 8 channels: words 4i .. 4i + 3 belong to group i
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            swap16(d.w[j], d.w[4 + j]);
-            swap16(d.w[8 + j], d.w[12 + j]);
-          }
-          unsigned s2 = s1, s3 = s1;
-          s1 = s0;
-          swap16(s0, s1);
-          swap16(s2, s3);
-          sc[t][0] = __uint_as_float(s0);
-          sc[t][1] = __uint_as_float(s1);
-          sc[t][GPU - 2] = __uint_as_float(s2);
-          sc[t][GPU - 1] = __uint_as_float(s3);
+        if constexpr (GROUP_ROWS) {
+          sc[t][0] = b.s[u][t];
         } else {
-          sc[t][0] = __uint_as_float(s0);
-          sc[t][1] = __uint_as_float(s1);
+          // the halves' second and first 16 channels change places: words 0-7 now belong to
+          // the first 64 channels in every lane, 8-15 to the others
+#pragma unroll
+          for (int j = 0; j < 8; ++j) swap32(d.w[j], d.w[8 + j]);
+          unsigned q0 = __float_as_uint(b.s[u][t]), q1 = q0;
+          swap32(q0, q1);
+          if constexpr (GS == 32) {
+            // and the same within each half, by 8 channels: words 4i .. 4i + 3 belong to group i
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              swap16(d.w[j], d.w[4 + j]);
+              swap16(d.w[8 + j], d.w[12 + j]);
+            }
+            unsigned q2 = q1, q3 = q1;
+            q1 = q0;
+            swap16(q0, q1);
+            swap16(q2, q3);
+            sc[t][GPU - 2] = __uint_as_float(q2);
+            sc[t][GPU - 1] = __uint_as_float(q3);
+          }
+          sc[t][0] = __uint_as_float(q0);
+          sc[t][1] = __uint_as_float(q1);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -289,12 +298,12 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
           for (int i = 0; i < 4; ++i) x[(s + 1) & 1][i] = fragment(s + 1, u, i);
         }
 #pragma unroll
-        for (int g = 0; g < GPU; ++g) {
+        for (int g = 0; g < SUMS; ++g) {
           v4f p[NT];
 #pragma unroll
           for (int t = 0; t < NT; ++t) p[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int i = g * (4 / GPU); i < (g + 1) * (4 / GPU); ++i) {
+          for (int i = g * (4 / SUMS); i < (g + 1) * (4 / SUMS); ++i) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) p[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s & 1][i], f[t][i], p[t], 0, 0, 0);
 #pragma unroll
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
     }
   }
 
-  // the waves' sums through LDS: row 4 c + e, column col of each tile
+  // the waves' sums through LDS: vector 4 c + e, column col of each tile
   __syncthreads();
   float* const red = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -372,7 +381,15 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
 #pragma unroll
     for (int s = 0; s < SETS; ++s)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[((wave * TILES + t) * SETS * kRows + s * kRows + 4 * c + e) * kCols + col] = acc[t][s][e];
+      for (int e = 0; e < 4; ++e) {
+        float q = acc[t][s][e];
+        if constexpr (GROUP_ROWS) {                  // row 4 g + v: the groups' sums of vector e
+          q += __shfl_xor(q, 16);
+          if constexpr (GS == 32) q += __shfl_xor(q, 32);
+          if (c != 0) continue;
+        }
+        red[((wave * TILES + t) * SETS * kRows + s * kRows + 4 * c + e) * kCols + col] = q;
+      }
   __syncthreads();
   auto total = [&](int tile, int m, int j) {
     float s = 0.0f;
@@ -498,7 +515,7 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   a.tblocks = (a.r / 16 + NT - 1) / NT;
   const int grid = a.blocks * a.splits + a.tblocks * a.tsplits;
   // a wave has a unit at least; the fused t also a thread for each output
-  a.waves = RB == 0 && per_split >= 8 && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
+  a.waves = per_split >= (RB == 0 ? 8 : 16) && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
   const int per = (per_split + a.waves - 1) / a.waves * kUnit;
   a.pitch = (per < CK ? per : CK) * 2 + 16;
   const int stage = a.waves * a.M * (SMOOTH ? 2 : 1) * a.pitch, red = a.waves * TILES * SETS * kRows * kCols * 4;
