@@ -132,9 +132,9 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
     (their rows may be apart: a slice of a modulation's wider output); post_weight, weight bf16 [D].  Each of them may be
     None.  Returns (x' as x, h bf16); without a branch (the norm in front of the first block), (None, h) with x' = x.
     `out` = (x', h) gives the outputs; x' may be x itself."""
-    if stream is None and out is None and norm in NORM_KINDS:
-        done = (_q._call or _q._native()).norm(x, branch, NORM_KINDS[norm], float(eps), float(residual_scale), gate, bool(post_norm),
-                                               post_weight, weight, scale, shift)
+    if stream is None and out is None:
+        done = (_q._call or _q._native()).norm(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale,
+                                               shift)
         if done is not None:
             if type(done) is int:
                 _q._check("qwam_block_norm", done)
@@ -156,10 +156,9 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
     (None: none) and of h.  Returns a dict with dx (as x'), dbranch (bf16), and float32 dgate, dscale, dshift [S][D] and
     dpost_weight, dweight [D] for the parameters given (None for the others).  `wanted` limits the parameters' and the
     branch's gradients to those named."""
-    if stream is None and wanted is None and norm in NORM_KINDS:
-        done = (_q._call or _q._native()).norm_backward(dx_out, dh, x_out, branch, NORM_KINDS[norm], float(eps),
-                                                        float(residual_scale), gate, bool(post_norm), post_weight, weight,
-                                                        scale, shift)
+    if stream is None and wanted is None:
+        done = (_q._call or _q._native()).norm_backward(dx_out, dh, x_out, branch, norm, eps, residual_scale, gate, post_norm,
+                                                        post_weight, weight, scale, shift)
         if done is not None:
             if type(done) is int:
                 _q._check("qwam_block_norm_backward", done)

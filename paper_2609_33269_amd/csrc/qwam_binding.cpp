@@ -302,17 +302,19 @@ const at::Tensor* tensor_of(PyObject* o) {
   return t.is_cuda() ? &t : nullptr;
 }
 
-// the arguments that the norm's calls share, from `a`: norm (0 or 1), eps, residual_scale, gate, post_norm, post_weight,
+// the arguments that the norm's calls share, from `a`: norm ("rms" or "layer"), eps, residual_scale, gate, post_norm, post_weight,
 // weight, scale, shift
 constexpr int kNormArgs = 9;
 bool norm_of(PyObject* const* a, int64_t T, int64_t D, bool f32, qwam_norm& p) {
-  if (!PyLong_Check(a[0]) || !PyFloat_Check(a[1]) || !PyFloat_Check(a[2]) || !PyBool_Check(a[4]) || T > INT32_MAX || D > INT32_MAX)
+  if (!PyUnicode_Check(a[0]) || !PyFloat_Check(a[1]) || !PyFloat_Check(a[2]) || !PyBool_Check(a[4]) || T > INT32_MAX || D > INT32_MAX)
     return false;
   p = {};
   p.T = static_cast<int32_t>(T);
   p.D = static_cast<int32_t>(D);
   p.S = 1;
-  p.kind = static_cast<int32_t>(PyLong_AsLong(a[0]));
+  if (PyUnicode_CompareWithASCIIString(a[0], "rms") == 0) p.kind = QWAM_NORM_RMS;
+  else if (PyUnicode_CompareWithASCIIString(a[0], "layer") == 0) p.kind = QWAM_NORM_LAYER;
+  else return false;
   p.post = a[4] == Py_True;
   p.x_f32 = f32;
   p.eps = static_cast<float>(PyFloat_AS_DOUBLE(a[1]));

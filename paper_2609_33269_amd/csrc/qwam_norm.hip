@@ -59,14 +59,21 @@ __device__ __forceinline__ Raw<F32> load8(const void* p, int64_t at, int lane, i
     } else {
       *reinterpret_cast<uint4*>(&r.w[0]) = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at + i);
     }
-  } else {
+  } else if (D > 0) {
+    // past the end the last value is read and dropped: a load under a condition of its
+    // own would be waited for before the next
+    uint32_t q[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int i = place<TPR, false>(lane, k, e);
-      if (i < D) {
-        if constexpr (F32) r.w[e] = __float_as_uint(static_cast<const float*>(p)[at + i]);
-        else r.w[e / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[at + i]) << (16 * (e & 1));
-      }
+      const int64_t i = at + min(place<TPR, false>(lane, k, e), D - 1);
+      if constexpr (F32) q[e] = static_cast<const uint32_t*>(p)[i];
+      else q[e] = static_cast<const uint16_t*>(p)[i];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (place<TPR, false>(lane, k, e) >= D) q[e] = 0;
+      if constexpr (F32) r.w[e] = q[e];
+      else r.w[e / 2] |= q[e] << (16 * (e & 1));
     }
   }
   return r;

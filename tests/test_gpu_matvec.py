@@ -175,6 +175,22 @@ def test_streams_and_graph():
         assert torch.equal(out, Q.asp_matvec(layer, xs)), f"replay {i}"
 
 
+@pytest.mark.parametrize("M,K,N,r,group", [(16, 4096, 528, 32, 64), (16, 1024, 272, 16, 32), (11, 8192, 80, 0, 32)])
+def test_graph_of_the_larger_forms(M, K, N, r, group):
+    """Workgroups with more than 64 KB of LDS, the parts' join, captured without a call before."""
+    layer = _layer(K, N, r, group, smooth=r > 0)
+    xs = _x(M, K)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = Q.asp_matvec(layer, xs)
+    for i in range(3):
+        xs.copy_(_x(M, K, seed=20 + i))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, Q.asp_matvec(layer, xs)), f"replay {i}"
+
+
 def test_refusals():
     layer, x = _layer(256, 64, 16), _x(2, 256)
     with pytest.raises(Q.QwamError, match="exceeds 16"):
