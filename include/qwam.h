@@ -91,7 +91,8 @@
  *
  * Rotation: hadamard == 0, or a power of two with 16 <= hadamard <= 1024
  * dividing K (QWAM_ERR_INVALID_ARG otherwise).  It affects the activation
- * calls only; qwam_pack_weights and qwam_asp_linear do not read it.
+ * calls and qwam_asp_matvec only; qwam_pack_weights and qwam_asp_linear do not
+ * read it.
  *
  * Shape limits: group == 64 or 32; K % 64 == 0, 64 <= K <= 65536; N % 16 == 0,
  * 16 <= N <= 1048576; r in {16, 32, 48, 64}; 1 <= M <= 1048576; for
@@ -339,14 +340,15 @@ int64_t qwam_aog_protected_basis_workspace(int32_t d, int32_t r);
  * Matrix-vector products with the packed 4-bit weights of a layer: for 1 to 16
  * tokens the weights' stream is what a call costs, so the activation is not
  * quantized:
- *     x~      = x * inv_smooth                 (inv_smooth NULL: x)
+ *     x~      = x * inv_smooth                 (inv_smooth NULL: x),
+ *               rotated as in the activation calls where hadamard != 0
  *     y[m, n] = bf16( sum_g ws[g][n] sum_{k in g} x~[m, k] c[n, k]
  *                     + sum_j t[m, j] L2t[n, j] + bias[n] ),  t = x~ . L1
  * with the sums and t in float32; x~ enters the matrix cores as two bf16
- * pieces (within 2^-16 of it), or as it is where inv_smooth is NULL.
+ * pieces (within 2^-16 of it), or as it is where it is x itself.
  *   L   in   packed layer: reads K, N, r, group, hadamard, wq, ws, inv_smooth,
  *            L1f, L2t, bias.  r = 0 (no branch; L1f and L2t are not read), 16,
- *            32, 48 or 64; hadamard 0
+ *            32, 48 or 64
  *   M   in   1 <= M <= 16 (QWAM_ERR_UNSUPPORTED above)
  *   x   in   bf16 [M][K]
  *   y   out  bf16 [M][N]

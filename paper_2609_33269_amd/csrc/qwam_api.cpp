@@ -350,7 +350,6 @@ qwam_status check_matvec(const char* fn, const qwam_layer* L, int32_t M) {
   if (s != QWAM_OK) return s;
   if (L->r < 0 || L->r > 64 || L->r % 16 != 0)
     return fail(QWAM_ERR_UNSUPPORTED, "%s: rank r must be 0, 16, 32, 48 or 64 (got %d)", fn, L->r);
-  if (L->hadamard != 0) return fail(QWAM_ERR_UNSUPPORTED, "%s: layers without rotation only", fn);
   if ((s = check_m(fn, M)) != QWAM_OK) return s;
   if (M > qwam::kMatvecMaxM) return fail(QWAM_ERR_UNSUPPORTED, "%s: M = %d exceeds %d", fn, M, qwam::kMatvecMaxM);
   if (static_cast<int64_t>(L->N) * (L->K / L->group) >= (int64_t(1) << 29))
@@ -462,7 +461,7 @@ extern "C" {
 int64_t qwam_asp_matvec_workspace(const qwam_layer* L, int32_t M) {
   if (check_matvec("qwam_asp_matvec_workspace", L, M) != QWAM_OK) return -1;
   ok();
-  return qwam::matvec_workspace_bytes(M, L->N, L->K, L->r);
+  return qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->hadamard);
 }
 
 qwam_status qwam_asp_matvec(const qwam_layer* L, int32_t M, const uint16_t* x, uint16_t* y, void* workspace,
@@ -482,10 +481,10 @@ qwam_status qwam_asp_matvec(const qwam_layer* L, int32_t M, const uint16_t* x, u
     return fail(QWAM_ERR_MISALIGNED, "%s: bias is not 16-byte aligned", fn);
   QWAM_REQUIRE_PTR(x);
   QWAM_REQUIRE_PTR(y);
-  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::matvec_workspace_bytes(M, L->N, L->K, L->r))) != QWAM_OK)
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::matvec_workspace_bytes(M, L->N, L->K, L->r, L->hadamard))) != QWAM_OK)
     return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;
-  return launched(fn, qwam::launch_asp_matvec(M, L->N, L->K, L->r, L->group, x, L->inv_smooth, L->L1f, L->wq, L->ws, L->L2t,
+  return launched(fn, qwam::launch_asp_matvec(M, L->N, L->K, L->r, L->group, L->hadamard, x, L->inv_smooth, L->L1f, L->wq, L->ws, L->L2t,
                                               L->bias, y, workspace, static_cast<hipStream_t>(stream)));
 }
 

@@ -106,11 +106,11 @@ hipError_t launch_group_partials_small(int M, int N, int K, int group, const uin
 // ---- a single token's step ----
 
 // y = x~ . dequantized weights + the branch + bias for M <= kMatvecMaxM tokens
-// (r = 0: no branch; inv_smooth null: x~ = x); the workspace may be null where
-// matvec_workspace_bytes is 0
+// (r = 0: no branch; inv_smooth null: x unsmoothed; B: block of the rotation or 0);
+// the workspace may be null where matvec_workspace_bytes is 0
 constexpr int kMatvecMaxM = 16;
-int64_t matvec_workspace_bytes(int M, int N, int K, int r);
-hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, const uint16_t* x, const float* inv_smooth,
+int64_t matvec_workspace_bytes(int M, int N, int K, int r, int B);
+hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, int B, const uint16_t* x, const float* inv_smooth,
                              const uint16_t* L1f, const uint8_t* wq, const float* ws, const uint16_t* L2t,
                              const uint16_t* bias, uint16_t* y, void* workspace, hipStream_t stream);
 

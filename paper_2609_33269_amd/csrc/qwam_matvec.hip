@@ -25,10 +25,13 @@
 //     reads, 18.7 us instead of 16.5 for 7 tokens at 14336 x 3072 in groups of 32.)
 //   * The pieces are staged in the wave's own part of LDS, CK channels at a time,
 //     while the codes of the next CK are on their way; no barrier until the end.
+//   * A rotated layer's x~ (hadamard) comes as pieces from a launch in front.
 //   * t comes from the same instructions (L1 in fragment order as the other
 //     operand): in the same launch where a workgroup's reading of all of L1 from
 //     L2 is cheaper than a launch, otherwise from a first launch that splits K
 //     over workgroups and leaves partial sums in the workspace.
+#include <cmath>
+
 #include "qwam_device.h"
 #include "qwam_internal.h"
 #include "qwam_mfma.h"
@@ -78,8 +81,12 @@ __device__ __forceinline__ void swap16(unsigned& a, unsigned& b) {
   b = r[1];
 }
 
+// what x holds: the tokens as they are, tokens still to be smoothed, or the two
+// pieces of each x~ (rows 2 m and 2 m + 1), as the rotation leaves them
+enum Input { kPlain, kSmooth, kPieces };
+
 // MV: vectors the instance has registers for
-template <int GS, int MV, int NT, int RB, bool SMOOTH>
+template <int GS, int MV, int NT, int RB, Input IN>
 __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a) {
   constexpr int GPU = kUnit / GS;                    // groups of a unit
   constexpr int SETS = (MV + kRows - 1) / kRows;
@@ -90,14 +97,16 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   constexpr int UPC = CK / kUnit;                    // units of a chunk
   constexpr int LPT = CK / 8;                        // lanes that stage one token's chunk, 8 channels each
   constexpr int TPI = 64 / LPT;                      // tokens staged at once
-  constexpr int PIECES = SMOOTH ? 2 : 1;             // of a token's x~
-  constexpr int NX = (MV / PIECES + TPI - 1) / TPI;           // staging steps
+  constexpr bool SMOOTH = IN == kSmooth;
+  constexpr int PIECES = IN == kPlain ? 1 : 2;       // of a token's x~
+  constexpr int NX = (MV / (SMOOTH ? 2 : 1) + TPI - 1) / TPI; // staging steps
   constexpr int TILES = NT + RB;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, c = lane >> 4;
   const int M = a.M, K = a.K, N = a.N, V = M * PIECES, waves = a.waves, pitch = a.pitch;
+  const int rows_in = SMOOTH ? M : V;                // of x
   const int tgrid = a.tsplits * a.tblocks;
   const bool branch = static_cast<int>(blockIdx.x) < tgrid;             // a workgroup of t
   const int index = branch ? blockIdx.x : blockIdx.x - tgrid, nblocks = branch ? a.tblocks : a.blocks;
@@ -125,7 +134,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   const uint32_t rows = branch ? 0u : static_cast<uint32_t>(min(NT * kCols, N - n0));
   const buf_rsrc w_rsrc = make_rsrc(a.wq + static_cast<int64_t>(n0) * KB, rows * static_cast<uint32_t>(KB));
   const buf_rsrc s_rsrc = make_rsrc(a.ws, static_cast<uint32_t>(K / GS) * static_cast<uint32_t>(N) * 4u);
-  const buf_rsrc x_rsrc = make_rsrc(a.x, static_cast<uint32_t>(M) * static_cast<uint32_t>(K) * 2u);
+  const buf_rsrc x_rsrc = make_rsrc(a.x, static_cast<uint32_t>(rows_in) * static_cast<uint32_t>(K) * 2u);
   const buf_rsrc i_rsrc = make_rsrc(a.inv, SMOOTH ? static_cast<uint32_t>(K) * 4u : 0u);
   const int rb = a.r >> 4;
   const buf_rsrc l_rsrc = make_rsrc(a.L1f, static_cast<uint32_t>(K) * (rb * 32u));
@@ -165,7 +174,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
 #pragma unroll
     for (int s = 0; s < NX; ++s) {
       const int m = s * TPI + stok;
-      if (s * TPI < M) xr[s] = buf_load16(x_rsrc, in && m < M ? (static_cast<uint32_t>(m) * K + k) * 2u : kNowhere);
+      if (s * TPI < rows_in) xr[s] = buf_load16(x_rsrc, in && m < rows_in ? (static_cast<uint32_t>(m) * K + k) * 2u : kNowhere);
     }
   };
   // vector v = token * PIECES + piece; channels past K are staged as zeros
@@ -177,9 +186,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
 #pragma unroll
     for (int s = 0; s < NX; ++s) {
       const int m = s * TPI + stok;
-      if (s * TPI >= M) break;
+      if (s * TPI >= rows_in) break;
       if constexpr (!SMOOTH) {
-        if (m < M && staged) put(m, xr[s]);
+        if (m < rows_in && staged) put(m, xr[s]);
         continue;
       }
       const uint32_t xb[4] = {xr[s].x, xr[s].y, xr[s].z, xr[s].w};
@@ -507,7 +516,7 @@ Form form_of(int M, int N, int K, int r, bool smooth) {
   return {nt, within((V > 16 ? 512 : 512 + blocks / 2) / blocks, most), most, false};
 }
 
-template <int GS, int MV, int NT, int RB, bool SMOOTH>
+template <int GS, int MV, int NT, int RB, Input IN>
 hipError_t launch(MatvecArgs a, hipStream_t stream) {
   constexpr int SETS = (MV + kRows - 1) / kRows, TILES = NT + RB, CK = chunk_channels(MV, NT);
   const int units = (a.K + kUnit - 1) / kUnit, per_split = (units + a.splits - 1) / a.splits;
@@ -518,9 +527,9 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   a.waves = per_split >= (RB == 0 ? 8 : 16) && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
   const int per = (per_split + a.waves - 1) / a.waves * kUnit;
   a.pitch = (per < CK ? per : CK) * 2 + 16;
-  const int stage = a.waves * a.M * (SMOOTH ? 2 : 1) * a.pitch, red = a.waves * TILES * SETS * kRows * kCols * 4;
+  const int stage = a.waves * a.M * (IN == kPlain ? 1 : 2) * a.pitch, red = a.waves * TILES * SETS * kRows * kCols * 4;
   const int bytes = (stage > red ? stage : red) + a.pitch + a.M * RB * 64;
-  auto kernel = matvec_kernel<GS, MV, NT, RB, SMOOTH>;
+  auto kernel = matvec_kernel<GS, MV, NT, RB, IN>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
@@ -529,39 +538,101 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int GS, int NT, int RB, bool SMOOTH>
+template <int GS, int NT, int RB, Input IN>
 hipError_t launch_vectors(const MatvecArgs& a, hipStream_t stream) {
-  const int V = a.M * (SMOOTH ? 2 : 1);
+  const int V = a.M * (IN == kPlain ? 1 : 2);
   if constexpr (NT <= 2)
-    if (V <= 4) return launch<GS, 4, NT, RB, SMOOTH>(a, stream);
-  if (V <= 16) return launch<GS, 16, NT, RB, SMOOTH>(a, stream);
-  if constexpr (SMOOTH && NT <= 2) return launch<GS, 32, NT, RB, SMOOTH>(a, stream);
+    if (V <= 4) return launch<GS, 4, NT, RB, IN>(a, stream);
+  if (V <= 16) return launch<GS, 16, NT, RB, IN>(a, stream);
+  if constexpr (IN != kPlain && NT <= 2) return launch<GS, 32, NT, RB, IN>(a, stream);
   return hipErrorInvalidValue;
 }
 
 template <int NT, int RB>
-hipError_t launch_main(const MatvecArgs& a, int group, hipStream_t stream) {
-  if (a.inv != nullptr) return group == 32 ? launch_vectors<32, NT, RB, true>(a, stream) : launch_vectors<64, NT, RB, true>(a, stream);
-  return group == 32 ? launch_vectors<32, NT, RB, false>(a, stream) : launch_vectors<64, NT, RB, false>(a, stream);
+hipError_t launch_main(const MatvecArgs& a, int group, bool pieces, hipStream_t stream) {
+  if (pieces) return group == 32 ? launch_vectors<32, NT, RB, kPieces>(a, stream) : launch_vectors<64, NT, RB, kPieces>(a, stream);
+  if (a.inv != nullptr) return group == 32 ? launch_vectors<32, NT, RB, kSmooth>(a, stream) : launch_vectors<64, NT, RB, kSmooth>(a, stream);
+  return group == 32 ? launch_vectors<32, NT, RB, kPlain>(a, stream) : launch_vectors<64, NT, RB, kPlain>(a, stream);
+}
+
+// The rotated x~ of Eq. 3 as pieces: a wave takes 64 E channels (one block, or
+// several of fewer than 64), channel 64 e + lane in value e, so that the first six
+// stages cross lanes and the others stay in registers; stages, roundings and
+// the last multiply as the activation kernels'.
+template <int E>
+__global__ __launch_bounds__(64) void matvec_rotate_kernel(const uint16_t* x, const float* inv, uint16_t* out, int K, int B, float scale) {
+  const int lane = threadIdx.x, per = K / (64 * E), m = blockIdx.x / per, k0 = blockIdx.x % per * (64 * E);
+  float v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int k = k0 + 64 * e + lane;
+    v[e] = bf16_to_f32(x[static_cast<int64_t>(m) * K + k]);
+    if (inv != nullptr) v[e] = v[e] * inv[k];
+  }
+#pragma unroll
+  for (int s = 0; s < 6; ++s)
+    if ((1 << s) < B) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float o = __shfl_xor(v[e], 1 << s);
+        v[e] = lane >> s & 1 ? o - v[e] : v[e] + o;
+      }
+    }
+#pragma unroll
+  for (int h = 1; h < E; h *= 2)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if ((e & h) == 0) {
+        const float p = v[e], q = v[e + h];
+        v[e] = p + q;
+        v[e + h] = p - q;
+      }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float y = v[e] * scale;
+    const uint32_t hi = f32_to_bf16_rne(y);
+    const int64_t at = 2 * static_cast<int64_t>(m) * K + k0 + 64 * e + lane;
+    out[at] = static_cast<uint16_t>(hi);
+    out[at + K] = static_cast<uint16_t>(f32_to_bf16_rne(y - bf16_to_f32(hi)));
+  }
+}
+
+hipError_t launch_rotate(int M, int K, int B, const uint16_t* x, const float* inv, uint16_t* out, hipStream_t stream) {
+  const int e = B <= 64 ? 1 : B / 64;
+  const dim3 grid(static_cast<unsigned>(M) * (K / (64 * e)));
+  const float scale = 1.0f / sqrtf(static_cast<float>(B));
+  auto kernel = e == 1 ? matvec_rotate_kernel<1> : e == 2 ? matvec_rotate_kernel<2> : e == 4 ? matvec_rotate_kernel<4>
+                : e == 8 ? matvec_rotate_kernel<8> : matvec_rotate_kernel<16>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, x, inv, out, K, B, scale);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t matvec_workspace_bytes(int M, int N, int K, int r) {
+// the rotated pieces, then the parts
+static int64_t rotated_bytes(int M, int K, int B) { return B == 0 ? 0 : static_cast<int64_t>(M) * K * 4; }
+
+int64_t matvec_workspace_bytes(int M, int N, int K, int r, int B) {
   const Form f = form_of(M, N, K, r, true);
-  return f.fused ? 0 : (static_cast<int64_t>(f.splits) * N + static_cast<int64_t>(f.tsplits) * r) * M * 4;
+  return rotated_bytes(M, K, B) + (f.fused ? 0 : (static_cast<int64_t>(f.splits) * N + static_cast<int64_t>(f.tsplits) * r) * M * 4);
 }
 
-hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, const uint16_t* x, const float* inv_smooth,
+hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, int B, const uint16_t* x, const float* inv_smooth,
                              const uint16_t* L1f, const uint8_t* wq, const float* ws, const uint16_t* L2t,
                              const uint16_t* bias, uint16_t* y, void* workspace, hipStream_t stream) {
-  const Form f = form_of(M, N, K, r, inv_smooth != nullptr);
-  float* const part = f.fused ? nullptr : static_cast<float*>(workspace);
+  const Form f = form_of(M, N, K, r, inv_smooth != nullptr || B != 0);
+  if (B != 0) {
+    uint16_t* const pieces = static_cast<uint16_t*>(workspace);
+    const hipError_t e = launch_rotate(M, K, B, x, inv_smooth, pieces, stream);
+    if (e != hipSuccess) return e;
+    x = pieces;
+  }
+  float* const part = f.fused ? nullptr : reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rotated_bytes(M, K, B));
   const MatvecArgs a = {x, inv_smooth, L1f, wq, ws, L2t, bias, y, part, f.fused ? nullptr : part + static_cast<int64_t>(f.splits) * M * N,
                         M, N, K, r, f.splits, 0, f.tsplits, 0, 0, 0};
-  if (f.fused && r > 0) return launch_main<1, 1>(a, group, stream);
-  const hipError_t e = f.nt == 1 ? launch_main<1, 0>(a, group, stream) : f.nt == 2 ? launch_main<2, 0>(a, group, stream)
-                                                                                   : launch_main<4, 0>(a, group, stream);
+  if (f.fused && r > 0) return launch_main<1, 1>(a, group, B != 0, stream);
+  const hipError_t e = f.nt == 1 ? launch_main<1, 0>(a, group, B != 0, stream) : f.nt == 2 ? launch_main<2, 0>(a, group, B != 0, stream)
+                                                                                           : launch_main<4, 0>(a, group, B != 0, stream);
   if (f.fused || e != hipSuccess) return e;
   hipLaunchKernelGGL(matvec_join_kernel, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>((M + 3) / 4)), dim3(256), 0, stream, a);
   return hipGetLastError();

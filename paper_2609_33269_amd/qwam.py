@@ -384,7 +384,8 @@ def _need(fn: str, nbytes: int) -> int:
 
 
 def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """qwam_asp_matvec: the packed layer on 1 to 16 tokens without quantizing them.  x bf16 [M][K] -> y bf16 [M][N].
+    """qwam_asp_matvec: the packed layer (either group, rotated or not, with or without a branch) on 1 to 16 tokens
+    without quantizing them.  x bf16 [M][K] -> y bf16 [M][N].
     `stream` is a torch.cuda.Stream (y and the workspace come from its pool)."""
     if stream is None:
         y = (_call or _native()).matvec(layer, x, out)

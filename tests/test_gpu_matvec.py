@@ -48,6 +48,8 @@ def _terms(layer, x):
     xt = f64(x.float())
     if layer.inv_smooth is not None:
         xt = xt * f64(layer.inv_smooth)
+    if layer.hadamard:
+        xt = O.rotate_exact(xt, layer.hadamard)
     y, s = xt @ w.T, np.abs(xt) @ np.abs(w).T
     if layer.r:
         L1, L2 = f64(layer.L1t.float()).T, f64(layer.L2t.float()).T
@@ -126,6 +128,22 @@ def test_wide_layers(group, smooth):
         for M in (1, 3, 5, 8, 9, 16):
             x = _x(M, 320)
             _check(layer, x, Q.asp_matvec(layer, x))
+
+
+@pytest.mark.parametrize("B", [16, 32, 64, 128, 256, 512, 1024])
+@pytest.mark.parametrize("group", [64, 32])
+def test_rotated_layers(B, group):
+    """x~ rotated: its float32 butterflies (ten roundings of 2^-24 on sums of up to 1024 terms, each at most the block's
+    root sum of squares) stay below the bound's 2^-15 of the terms, as every product's magnitude sum is at least a block's
+    root sum of squares times that of its weights."""
+    for K, N, r, M in ((1024, 272, 16, 1), (3072, 1040, 32, 5), (2048, 96, 0, 16), (5120, 144, 64, 9)):
+        layer = dataclasses.replace(_layer(K, N, r, group, bias=True, seed=B), hadamard=B)
+        x = _x(M, K)
+        _check(layer, x, Q.asp_matvec(layer, x))
+    plain = dataclasses.replace(_layer(1024, 64, 0, group, smooth=False), hadamard=B)      # without smoothing
+    for M in (1, 12):
+        x = _x(M, 1024)
+        _check(plain, x, Q.asp_matvec(plain, x))
 
 
 def test_largest_width():
@@ -207,8 +225,8 @@ def test_refusals():
         Q.asp_matvec(layer, x[:0])
     with pytest.raises(ValueError, match="y must have shape"):
         Q.asp_matvec(layer, x, out=torch.empty(2, 48, dtype=torch.bfloat16, device="cuda"))
-    with pytest.raises(Q.QwamError, match="without rotation"):
-        Q.asp_matvec(dataclasses.replace(layer, hadamard=64), x)
+    with pytest.raises(Q.QwamError, match="hadamard must be"):
+        Q.asp_matvec(dataclasses.replace(layer, hadamard=24), x)
     with pytest.raises(TypeError, match="L2t must be"):
         Q.asp_matvec(dataclasses.replace(layer, L2t=None), x)
     with pytest.raises(Q.QwamError, match="L1f is NULL"):

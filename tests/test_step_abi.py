@@ -36,7 +36,7 @@ def _matvec(lib, L, M=1, x=FAKE, y=FAKE, ws=FAKE, nbytes=1 << 40):
 def test_matvec_refusals(lib):
     assert lib.qwam_asp_matvec(None, 1, FAKE, FAKE, FAKE, 1 << 40, None) == INVALID
     for kw, st in (({"K": 96}, INVALID), ({"K": 0}, INVALID), ({"N": 24}, INVALID), ({"group": 16}, INVALID),
-                   ({"r": 8}, UNSUPPORTED), ({"r": 80}, UNSUPPORTED), ({"r": -16}, UNSUPPORTED), ({"hadamard": 64}, UNSUPPORTED),
+                   ({"r": 8}, UNSUPPORTED), ({"r": 80}, UNSUPPORTED), ({"r": -16}, UNSUPPORTED),
                    ({"hadamard": 24}, INVALID), ({"K": 131072}, UNSUPPORTED)):
         assert _matvec(lib, _layer(**kw)) == st, kw
         assert lib.qwam_asp_matvec_workspace(ctypes.byref(_layer(**kw)), 1) == -1
