@@ -469,11 +469,14 @@ Plan plan_of(const CacheParams& c, bool fp8, int q_heads, int max_len) {
   // one range where a second launch would cost as much as the waves' turns (1.1 us for
   // each 128 positions of 8 x 3 heads of 128; 64 sequences of 500: 13.5 us, in two ranges 18.6)
   if (max_len <= kOneRange) return {static_cast<int>(up(max_len, 32)), 1};
-  // enough workgroups for every CU four times; no more than 256 ranges to join, and
-  // their partial results at most 1/16 of what they read
-  const int64_t heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16;
-  int64_t n = (rows * max_len + 1023) / 1024;
-  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 64 * heads / (fp8 ? 1 : 2), int64_t(128)})
+  // Workgroups for every CU four times, of half as wide values twice (ranges of as many
+  // bytes: 8 x 3 heads of 128 over 131072 positions in fp8 66 us, with 1024 workgroups 74; 16 x 8 x 3 over
+  // 4096 in bf16 18.0 us, with 512 26.0); no more than 256 ranges to join, their partial results
+  // at most 1/16 of what they read, and no range of one turn of the waves in a long context
+  // (4 x 2 x 2 heads of 80 over 16197 positions 12.4 us, with ranges of 128 15.0)
+  const int64_t heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16, want = fp8 ? 512 : 1024;
+  int64_t n = (rows * max_len + want - 1) / want;
+  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 64 * heads / (fp8 ? 1 : 2), int64_t(max_len > 4096 ? 256 : 128)})
     n = n < least ? least : n;
   n = up(n, 128) > kMaxChunk ? kMaxChunk : up(n, 128);
   return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n)};
