@@ -497,29 +497,32 @@ struct Form {
   bool fused;
 };
 
-// (a layer with a branch is taken as smoothed: the workspace query does not read inv_smooth)
+// (in parts, every layer is taken as smoothed: the workspace query does not read inv_smooth)
 Form form_of(int M, int N, int K, int r, bool smooth) {
   const int units = (K + kUnit - 1) / kUnit, tiles = N / kCols;
   // t once per workgroup is cheaper than a launch while all of them together read little of L1: 8 MB (1024 x 4096,
   // rank 16) 4.7 us against 8.1 with a join, 38 MB (3072 x 3072, rank 32) 6.4 against 8.0 and for 16 tokens 11.1 against
   // 11.0, 57 MB (3072 x 9216, rank 16) 10.4 against 10.2 and for 4 tokens 14.3 against 11.2; and while there are no more
   // of these narrow workgroups than the CUs hold: 192 x 28656, 11 tokens, rank 32 22.7 against 10.9
-  const bool fused = r == 0 || (r <= 32 && tiles <= 768 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(48) << 20));
-  const int V = M * (r > 0 || smooth ? 2 : 1);
+  // long rows of few workgroups go in parts with or without a branch: 16384 x 1024, plain, one token 7.0 us against 7.9
+  // in one, 16 tokens 9.8 against 14.2, 14336 x 1024, rank 16 8.8 against 12.3; but 16384 x 2048, plain 10.3 against 8.0
+  const bool alone = units <= 64 || tiles > 96;
+  const bool fused = r == 0 ? alone : (alone && r <= 32 && tiles <= 768 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(48) << 20));
   // Wider workgroups stage x for more channels; the widest hold fewer waves.  4096 x 28672, plain, one token 14.5 us with
   // one tile and 15.6 with two, 8 tokens 22.5 and 18.2, 16 tokens 20.7 with two and 19.6 with four.
   if (fused) {
+    const int V = M * (smooth ? 2 : 1);
     int nt = r > 0 || V <= 4 ? 1 : V <= 8 || V > 16 ? 2 : 4;      // (two sets of four tiles spill)
     while (nt > 1 && tiles < 256 * nt) nt /= 2;
     return {nt, 1, 0, true};
   }
   // 3072 x 9216, rank 32, one token 10.5 us with one tile and 11.7 with two (fewer channels: the same)
-  const int nt = V <= 4 && tiles >= 512 ? 1 : 2, blocks = (tiles + nt - 1) / nt;
+  const int nt = M <= 2 && tiles >= 512 ? 1 : 2, blocks = (tiles + nt - 1) / nt;
   auto within = [](int v, int most) { return v < 1 ? 1 : v < most ? v : most; };
   const int most = within((units + kWaves - 1) / kWaves, kMaxSplits);
   // about 512 workgroups, and no more of the largest, of which a CU holds two: 14336 x 3072, 16 tokens, 18.4 us in five
   // parts, 20.9 in four, 22.4 in eight; 3072 x 9216, 4 tokens, 13.2 us in one and 11.5 in two, 16 tokens 17.9 and 19.7
-  return {nt, within((V > 16 ? 512 : 512 + blocks / 2) / blocks, most), most, false};
+  return {nt, within((M > 8 ? 512 : 512 + blocks / 2) / blocks, most), most, false};
 }
 
 template <int GS, int MV, int NT, int RB, Input IN>

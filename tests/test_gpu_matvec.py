@@ -130,6 +130,18 @@ def test_wide_layers(group, smooth):
             _check(layer, x, Q.asp_matvec(layer, x))
 
 
+@pytest.mark.parametrize("smooth", [False, True])
+def test_long_rows_of_few_channels(smooth):
+    """K in parts without a branch, and with one."""
+    for K, N, r, group in ((16448, 48, 0, 64), (12352, 528, 0, 32), (9216, 16, 32, 64)):
+        layer = _layer(K, N, r, group, smooth=smooth or r > 0, bias=N == 528)
+        if not smooth:
+            layer = dataclasses.replace(layer, inv_smooth=None)
+        for M in (1, 2, 3, 9, 16):
+            x = _x(M, K)
+            _check(layer, x, Q.asp_matvec(layer, x))
+
+
 @pytest.mark.parametrize("B", [16, 32, 64, 128, 256, 512, 1024])
 @pytest.mark.parametrize("group", [64, 32])
 def test_rotated_layers(B, group):
