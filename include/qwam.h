@@ -407,7 +407,8 @@ qwam_status qwam_block_norm(const qwam_norm *p, const void *x, const uint16_t *b
  * and, for every parameter whose pointer is set, its sum over the rows it
  * serves, in float32 and in an order that does not change from call to call:
  * dgate, dscale, dshift [S][D], dpost_weight, dweight [D].  With branch NULL,
- * dx = d and dbranch, dgate and dpost_weight must be NULL.
+ * dx = d and dbranch, dgate and dpost_weight must be NULL.  S * ceil(D / 64) is
+ * at most 2^21 (QWAM_ERR_UNSUPPORTED above).
  *   workspace  as for qwam_asp_matvec, qwam_block_norm_backward_workspace(p) bytes
  */
 qwam_status qwam_block_norm_backward(const qwam_norm *p, const void *dx_out, const uint16_t *dh,

@@ -382,6 +382,13 @@ qwam_status check_norm_shape(const char* fn, const qwam_norm* p) {
   return QWAM_OK;
 }
 
+// the gradients' sums over rows: one launch has a workgroup for each sample and 64 channels
+qwam_status check_norm_samples(const char* fn, const qwam_norm* p) {
+  if (static_cast<int64_t>(p->S) * ((p->D + 63) / 64) > (1 << 21))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: S * ceil(D / 64) must be at most 2^21", fn);
+  return QWAM_OK;
+}
+
 qwam_status check_norm(const char* fn, const qwam_norm* p, qwam::NormParams* out) {
   qwam_status s = check_norm_shape(fn, p);
   if (s != QWAM_OK) return s;
@@ -507,7 +514,8 @@ qwam_status qwam_block_norm(const qwam_norm* p, const void* x, const uint16_t* b
 }
 
 int64_t qwam_block_norm_backward_workspace(const qwam_norm* p) {
-  if (check_norm_shape("qwam_block_norm_backward_workspace", p) != QWAM_OK) return -1;
+  const char* fn = "qwam_block_norm_backward_workspace";
+  if (check_norm_shape(fn, p) != QWAM_OK || check_norm_samples(fn, p) != QWAM_OK) return -1;
   ok();
   return qwam::block_norm_bwd_workspace_bytes(p->T, p->D, p->S);
 }
@@ -534,6 +542,7 @@ qwam_status qwam_block_norm_backward(const qwam_norm* p, const void* dx_out, con
   QWAM_OPTIONAL_ELEM(dweight, 4);
   if (branch == nullptr && (dbranch != nullptr || dgate != nullptr || dpost_weight != nullptr))
     return fail(QWAM_ERR_INVALID_ARG, "%s: dbranch, dgate or dpost_weight without a branch", fn);
+  if ((s = check_norm_samples(fn, p)) != QWAM_OK) return s;
   if (!np.post && dpost_weight != nullptr)
     return fail(QWAM_ERR_INVALID_ARG, "%s: dpost_weight without a post-norm", fn);
   if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::block_norm_bwd_workspace_bytes(p->T, p->D, p->S))) != QWAM_OK)

@@ -471,13 +471,13 @@ constexpr int kSumAhead = 8;             // rows requested by a wave before the 
 }  // namespace
 
 // The samples' partial rows added in order: 64 channels a workgroup, the waves
-// dealt out over `here` samples (1: blockIdx.y says which, or all of at most 16)
-// and then over the rows of each.
+// dealt out over `here` samples (all of at most 16, or one a workgroup) and then
+// over the rows of each.
 __global__ __launch_bounds__(64 * kSumWaves) void block_norm_sums_kernel(NormParams p, const float* part, int blocks, int here,
                                                                          ParamGrads o) {
   __shared__ float red[kSumWaves][3][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
-  const int per = kSumWaves / here, si = wave / per, s = blockIdx.y * here + si;
+  const int cols = (p.D + 63) / 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x % cols * 64 + lane;
+  const int per = kSumWaves / here, si = wave / per, s = blockIdx.x / cols * here + si;
   float a = 0.0f, b = 0.0f, c = 0.0f;
   if (i < p.D && si < here)
     for (int j0 = wave % per; j0 < blocks; j0 += per * kSumAhead) {
@@ -644,7 +644,7 @@ hipError_t launch_block_norm_bwd(const NormParams& p, int T, const void* dxo, co
     const unsigned cols = static_cast<unsigned>((D + 63) / 64);
     const bool together = S > 1 && S <= kSumWaves;      // (by S alone: the order of a sum does not depend on what else is wanted)
     const ParamGrads o = {dgate, dscale, dshift, dpost_weight, dweight, weights && S > kSumWaves ? sums : nullptr};
-    hipLaunchKernelGGL(block_norm_sums_kernel, dim3(cols, together ? 1 : S), dim3(64 * kSumWaves), 0, stream, p, part, blocks,
+    hipLaunchKernelGGL(block_norm_sums_kernel, dim3(cols * (together ? 1u : static_cast<unsigned>(S))), dim3(64 * kSumWaves), 0, stream, p, part, blocks,
                        together ? S : 1, o);
     if (o.sums != nullptr) hipLaunchKernelGGL(block_norm_weights_kernel, dim3(cols), dim3(64 * kSumWaves), 0, stream, D, S, o);
   }

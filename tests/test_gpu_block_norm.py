@@ -244,6 +244,13 @@ def test_backward_optional_parameters(given):
         _backward_check({**_keep(p, given), "branch": None}, dh, dxo, norm, False)
 
 
+@pytest.mark.parametrize("T,S", [(17, 17), (34, 17), (70000, 70000), (48, 16)])
+def test_backward_many_samples(T, S):
+    """A gate, scale and shift per row, more samples than a grid's second dimension holds."""
+    p, dh, dxo = _inputs(T, 72, S, seed=S)
+    _backward_check(p, dh, dxo, "rms", True)
+
+
 def test_backward_sums_do_not_change():
     p, dh, dxo = _inputs(2048, 520, 2)
     dxo = dxo.bfloat16().cuda()

@@ -102,6 +102,8 @@ def test_norm_refusals(lib):
     assert _bwd(lib, _norm(post=1), ws=FAKE + 8) == MISALIGNED
     assert _bwd(lib, _norm(post=1), nbytes=need - 1) == INVALID
     assert lib.qwam_block_norm_backward_workspace(ctypes.byref(_norm(T=5))) == -1
+    many = _norm(T=1 << 20, S=1 << 20, D=256, post=1)                # 2^22 workgroups for the sums
+    assert _bwd(lib, many) == UNSUPPORTED and lib.qwam_block_norm_backward_workspace(ctypes.byref(many)) == -1
 
 
 def _cache(**kw):
