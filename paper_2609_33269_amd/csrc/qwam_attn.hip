@@ -48,7 +48,9 @@ __device__ __forceinline__ uint32_t fp8x4(float a, float b, float c, float d) {
 
 }  // namespace
 
-// one thread per 8 keys and the 8 values beside them (at most 2^29 threads, so that indexes are divided in 32 bits)
+// One thread per 8 keys and the 8 values beside them (at most 2^29 threads, so that indexes are divided in 32 bits).
+// Bound by the chain position - table - store (16 tokens 3.7 us in a graph) and, for prompts in fp8, by that and the
+// divisions: 2200 tokens 7.0 us (2.7 TB/s), with 16 channels a thread 7.7.
 template <bool FP8>
 __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t threads, const uint16_t* k, int64_t k_stride,
                                                         const uint16_t* v, int64_t v_stride, const int32_t* seq,
