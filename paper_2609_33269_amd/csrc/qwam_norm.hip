@@ -375,8 +375,9 @@ __global__ __launch_bounds__(TPR > kBwdThreads ? TPR : kBwdThreads) void block_n
         q[3] = __builtin_fmaf(b, b, q[3]);
       }
     row_sums<TPR>(q, red, turn);
-    const float rx = 1.0f / sqrtf(q[0] * inv_d + p.eps), mp = p.layer ? q[1] * inv_d : 0.0f, mpz = q[2] * rx * inv_d;
-    const float rb = post ? 1.0f / sqrtf(q[3] * inv_d + p.eps) : 1.0f;
+    // a group without a row left adds nothing: its zeros' 1 / deviation is infinite where eps is 0
+    const float rx = real ? 1.0f / sqrtf(q[0] * inv_d + p.eps) : 0.0f, mp = p.layer ? q[1] * inv_d : 0.0f, mpz = q[2] * rx * inv_d;
+    const float rb = !real ? 0.0f : post ? 1.0f / sqrtf(q[3] * inv_d + p.eps) : 1.0f;
 
     // d, the column sums, dx
     float d[NV][8];
