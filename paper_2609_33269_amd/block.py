@@ -114,7 +114,8 @@ class _BlockNorm(torch.autograd.Function):
                                 residual_scale=residual_scale, gate=gate, post_norm=post_norm, post_weight=post_weight,
                                 weight=weight, scale=scale, shift=shift,
                                 wanted=tuple("d" + n for n, w in need.items() if w))
-        like = lambda n, t: g["d" + n].to(t.dtype) if need[n] and t is not None else None  # noqa: E731
+        # (None too for a gate or post_weight that a norm without a branch does not read)
+        like = lambda n, t: g["d" + n].to(t.dtype) if need[n] and g["d" + n] is not None else None  # noqa: E731
         return (g["dx"] if need["x"] else None, g.get("dbranch"), like("gate", gate), like("post_weight", post_weight),
                 like("weight", weight), like("scale", scale), like("shift", shift), None, None, None, None)
 

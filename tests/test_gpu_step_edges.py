@@ -3,6 +3,7 @@
 import pytest
 import torch
 
+import paper_2609_33269_amd as P
 from paper_2609_33269_amd import qwam as Q
 from test_gpu_block_norm import _backward_check, _inputs
 
@@ -25,3 +26,23 @@ def test_backward_without_eps(T, S, D):
     for norm, post, f32 in (("rms", True, False), ("rms", False, True), ("layer", True, True), ("layer", False, False)):
         p, dh, dxo = _inputs(T, D, S, f32, seed=D + T)
         _backward_check(p, dh, dxo, norm, post, eps=0.0)
+
+
+# ---- block_norm under autograd ----
+
+@pytest.mark.parametrize("post", [False, True])
+def test_unread_parameters_without_a_branch(post):
+    """The norm in front of the first block reads neither gate nor post_weight: they get no gradient, the others theirs."""
+    p, dh, _ = _inputs(6, 72, 2)
+    if not post:
+        p["post_weight"] = None
+    leaf = {n: t.clone().requires_grad_() for n, t in p.items() if t is not None and n != "branch"}
+    kw = {n: leaf.get(n) for n in ("gate", "post_weight", "weight", "scale", "shift")}
+    _, h = P.block_norm(leaf["x"], post_norm=post, **kw)
+    h.backward(dh)
+    want = P.block_norm_backward(None, dh, p["x"], post_norm=post, **{n: p[n] for n in kw})
+    for n, t in leaf.items():
+        if n in ("gate", "post_weight"):
+            assert t.grad is None, n
+        else:
+            assert torch.equal(t.grad, want["d" + n].to(torch.bfloat16)), n
