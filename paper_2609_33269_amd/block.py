@@ -100,6 +100,7 @@ class _BlockNorm(torch.autograd.Function):
         xo, h = _forward(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift, None, None)
         ctx.save_for_backward(x if branch is None else xo, branch, gate, post_weight, weight, scale, shift)
         ctx.kept = (norm, eps, residual_scale, post_norm)
+        ctx.set_materialize_grads(False)      # the gradient of an unused output is None, not T x D zeros
         return xo, h
 
     @staticmethod

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2609_33269_amd as P
+from paper_2609_33269_amd import block
 from paper_2609_33269_amd import qwam as Q
 from test_gpu_block_norm import _backward_check, _inputs
 
@@ -46,3 +47,25 @@ def test_unread_parameters_without_a_branch(post):
             assert t.grad is None, n
         else:
             assert torch.equal(t.grad, want["d" + n].to(torch.bfloat16)), n
+
+
+@pytest.mark.parametrize("used", ["x", "h"])
+def test_unused_outputs_have_no_gradient_tensor(used, monkeypatch):
+    """A last block uses one output only: the other's gradient is taken as none, not as a tensor of zeros."""
+    p, dh, dxo = _inputs(10, 72, 2)
+    d = dxo.bfloat16().cuda()
+    kw = {n: p[n] for n in ("gate", "weight", "scale", "shift")}
+    x, b = (p[n].clone().requires_grad_() for n in ("x", "branch"))
+    seen = []
+    call = block.block_norm_backward
+    monkeypatch.setattr(block, "block_norm_backward", lambda *a, **k: seen.append(a[0]) or call(*a, **k))
+    xo, h = P.block_norm(x, b, residual_scale=0.5, **kw)
+    if used == "x":
+        xo.backward(d)
+        assert torch.equal(x.grad, (0.5 * d.float()).bfloat16())
+        assert torch.equal(b.grad, (d.float() * kw["gate"].float().repeat_interleave(5, 0)).bfloat16())
+    else:
+        h.backward(dh)
+        assert seen == [None]
+        want = call(None, dh, xo.detach(), p["branch"], residual_scale=0.5, **kw)
+        assert torch.equal(x.grad, want["dx"]) and torch.equal(b.grad, want["dbranch"])
