@@ -472,7 +472,8 @@ qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *
  *   lengths  in  int32 [seqs], taken as at most max_len and the table's reach,
  *                and below 0 as 0
  *   starts   in  int32 [seqs], or NULL for 0
- *   max_len  in  1 .. table_width * page_size: the call's work is laid out for it
+ *   max_len  in  1 .. table_width * page_size, at most 2^31 - 4096
+ *                (QWAM_ERR_UNSUPPORTED above): the call's work is laid out for it
  *   out      out bf16 [seqs][q_heads][dim]
  *   workspace  as for qwam_asp_matvec, qwam_paged_attention_workspace bytes
  */

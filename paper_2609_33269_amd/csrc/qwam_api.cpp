@@ -456,6 +456,9 @@ qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::Cac
     return fail(QWAM_ERR_UNSUPPORTED, "%s: seqs * q_heads must be at most 2^22", fn);
   if (max_len < 1 || max_len > static_cast<int64_t>(c->table_width) * c->page_size)
     return fail(QWAM_ERR_INVALID_ARG, "%s: max_len must be in [1, table_width * page_size] (got %d)", fn, max_len);
+  // the kernels count positions in 32 bits, up to a range past the last
+  if (static_cast<int64_t>(max_len) + qwam::kMaxChunk > (int64_t(1) << 31))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: max_len = %d exceeds 2^31 - %d", fn, max_len, qwam::kMaxChunk);
   if (!qwam::paged_attention_fits(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len))
     return fail(QWAM_ERR_UNSUPPORTED, "%s: too many sequences and heads of too long a max_len for one launch", fn);
   return QWAM_OK;

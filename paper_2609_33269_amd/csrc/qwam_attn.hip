@@ -88,7 +88,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t 
 namespace {
 
 constexpr int kAttnWaves = 4;
-constexpr int kMaxChunk = 4096;     // positions of a workgroup, the pages of 16 in each lane
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttnArgs {
@@ -102,7 +101,7 @@ struct AttnArgs {
   float scale;
 };
 
-// visible positions of a sequence: [first, len), and where its ranges start
+// visible positions of a sequence: [first, len), and where its ranges start (all 32 bits: len + kMaxChunk does not pass 2^31)
 struct Span {
   int first, len, base, count;    // count: ranges
 };

@@ -141,6 +141,7 @@ struct CacheParams {
   const int32_t* table;
 };
 constexpr int kMaxHeadGroup = 64;      // query heads per key head
+constexpr int kMaxChunk = 4096;        // positions of a workgroup of the attention, the pages of 16 in each lane
 hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream);
 bool paged_attention_fits(const CacheParams& c, bool fp8, int q_heads, int max_len);      // one launch's workgroups
