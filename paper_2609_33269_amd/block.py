@@ -210,6 +210,9 @@ class PagedCache:
     k_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
 
+    def _values(self) -> dict:
+        return {"cache.k": self.k, "cache.v": self.v, "cache.k_scale": self.k_scale, "cache.v_scale": self.v_scale}
+
     def c_struct(self) -> "_q.QwamCacheC":
         for t, name in ((self.k, "k"), (self.v, "v")):
             if not isinstance(t, torch.Tensor):
@@ -260,7 +263,8 @@ def _rows(t: torch.Tensor, name: str, shape) -> int:
 
 def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None) -> None:
     """qwam_kv_append: k, v bf16 [tokens][heads][dim] to position pos[t] of sequence seq[t] (int32 [tokens]), rounded to
-    float8 where the pages are.  Tokens without a place (pos < 0, no page) are not stored."""
+    float8 where the pages are.  Tokens without a place (pos < 0, no page) are not stored.  There is no gradient: tensors
+    that require one are refused where autograd records."""
     if stream is None:
         st = (_q._call or _q._native()).append(cache, k, v, seq, pos)
         if st is not None:
@@ -270,6 +274,7 @@ def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Te
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor of three dimensions (tokens, heads, dim)")
     n = k.shape[0]
+    _q._no_gradient("kv_append", k=k, v=v, **cache._values())
     st = _q.lib().qwam_kv_append(ctypes.byref(c), n, _rows(k, "k", (n, c.heads, c.dim)), k.stride(0) if n > 1 else 0,
                                  _rows(v, "v", (n, c.heads, c.dim)), v.stride(0) if n > 1 else 0,
                                  _q._req(seq, "seq", torch.int32, (n,)), _q._req(pos, "pos", torch.int32, (n,)),
@@ -283,7 +288,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
     """qwam_paged_attention: one new token per sequence, q bf16 [sequences][q_heads][dim] -> out bf16 of the same shape.
     Sequence b sees positions starts[b] (0) to lengths[b] (int32 [sequences]); one that sees none gives zeros.  `scale`
     is dim ** -0.5 unless given.  `max_len` bounds the lengths (the table's reach unless given): the work is laid out
-    for it, and positions past it are not seen."""
+    for it, and positions past it are not seen.  There is no gradient, as for kv_append."""
     if stream is None:
         o = (_q._call or _q._native()).attention(cache, q, lengths, starts, scale, max_len, out)
         if o is not None:
@@ -296,6 +301,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
     Hq = q.shape[1]
     shape = (c.seqs, Hq, c.dim)
     pq = _rows(q, "q", shape)
+    _q._no_gradient("paged_attention", q=q, **cache._values())
     if max_len is None:
         max_len = c.table_width * c.page_size
     need = _q._need("qwam_paged_attention", _q.lib().qwam_paged_attention_workspace(ctypes.byref(c), Hq, max_len))

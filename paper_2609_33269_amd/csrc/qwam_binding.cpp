@@ -270,6 +270,18 @@ at::Tensor workspace_of(int64_t need, const at::Tensor& like) {
   return need > 0 ? at::empty({need}, like.options().dtype(at::kByte)) : at::Tensor();
 }
 
+// whether autograd follows this argument (a tensor, or None): backwards, or forwards through a tangent
+bool tracked(PyObject* o) {
+  if (!THPVariable_Check(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return (t.requires_grad() && c10::GradMode::is_enabled()) || t._fw_grad(0).defined();
+}
+bool tracked(std::initializer_list<PyObject*> objects) {
+  for (PyObject* o : objects)
+    if (tracked(o)) return true;
+  return false;
+}
+
 // matvec(layer, x, out) -> y
 PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
@@ -278,6 +290,7 @@ PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t M = rows_of(args[1]);
   void *x, *py;
   if (M < 0 || !L.load(args[0], true) || !data_of(args[1], at::kBFloat16, {M, L.c.K}, &x)) return none_or_error();
+  if (tracked({args[1], L.held[kWs], L.held[kInv], L.held[kL1t], L.held[kL2t], L.held[kBias], L.held[kL1f]})) Py_RETURN_NONE;
   const at::Tensor& xt = THPVariable_Unpack(args[1]);
   Held y;
   if (!output(args[2], xt, at::kBFloat16, M, L.c.N, &y.o, &py)) return none_or_error();
@@ -344,8 +357,6 @@ bool norm_of(PyObject* const* a, int64_t T, int64_t D, bool f32, qwam_norm& p) {
          (p.post_weight == nullptr || p.post != 0);
 }
 
-bool needs_grad(PyObject* o) { return o != Py_None && THPVariable_Unpack(o).requires_grad(); }
-
 // norm(x, branch, <norm_of's>) -> (x', h); None under autograd too
 PyObject* py_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
@@ -359,11 +370,7 @@ PyObject* py_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   void* branch = nullptr;
   if (!norm_of(args + 2, T, D, f32, p) || (args[1] != Py_None && !data_of(args[1], at::kBFloat16, {T, D}, &branch)))
     return none_or_error();
-  if (c10::GradMode::is_enabled()) {
-    if (x->requires_grad() || needs_grad(args[1])) Py_RETURN_NONE;
-    for (const int i : {3, 5, 6, 7, 8})
-      if (needs_grad(args[2 + i])) Py_RETURN_NONE;
-  }
+  if (tracked({args[0], args[1], args[5], args[7], args[8], args[9], args[10]})) Py_RETURN_NONE;
   const at::Tensor h = at::empty({T, D}, x->options().dtype(at::kBFloat16));
   const at::Tensor xo = branch != nullptr ? at::empty({T, D}, x->options()) : at::Tensor();
   const qwam_status st = g_norm(&p, x->data_ptr(), static_cast<const uint16_t*>(branch), branch != nullptr ? xo.data_ptr() : nullptr,
@@ -470,6 +477,7 @@ struct Cache {
     c.v_scale = static_cast<const float*>(vs);
     return true;
   }
+  bool followed() const { return tracked({held[kCacheK], held[kCacheV], held[kCacheKScale], held[kCacheVScale]}); }
 };
 
 // a bf16 [rows][heads][dim] whose rows may be apart
@@ -494,6 +502,7 @@ PyObject* py_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (v == nullptr || rows3_of(args[1], n, C.c.heads, C.c.dim) == nullptr || !data_of(args[3], at::kInt, {n}, &seq) ||
       !data_of(args[4], at::kInt, {n}, &pos))
     return none_or_error();
+  if (C.followed() || tracked({args[1], args[2]})) Py_RETURN_NONE;
   return PyLong_FromLong(g_append(&C.c, static_cast<int32_t>(n), static_cast<const uint16_t*>(k->data_ptr()), n > 1 ? k->stride(0) : 0,
                                   static_cast<const uint16_t*>(v->data_ptr()), n > 1 ? v->stride(0) : 0,
                                   static_cast<const int32_t*>(seq), static_cast<const int32_t*>(pos), current_stream()));
@@ -509,6 +518,7 @@ PyObject* py_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (q == nullptr || q->dim() != 3 || q->size(1) > INT32_MAX || !C.load(args[0]) ||
       rows3_of(args[1], C.c.seqs, q->size(1), C.c.dim) == nullptr)
     return none_or_error();
+  if (C.followed() || tracked(args[1])) Py_RETURN_NONE;
   const int32_t heads = static_cast<int32_t>(q->size(1));
   void *lengths, *starts = nullptr, *po;
   if (!data_of(args[2], at::kInt, {C.c.seqs}, &lengths) || (args[3] != Py_None && !data_of(args[3], at::kInt, {C.c.seqs}, &starts)))

@@ -383,10 +383,24 @@ def _need(fn: str, nbytes: int) -> int:
     return int(nbytes)
 
 
+def _tangent(t: Optional[torch.Tensor]) -> bool:
+    return isinstance(t, torch.Tensor) and torch.autograd.forward_ad.unpack_dual(t).tangent is not None
+
+
+def _no_gradient(fn: str, **tensors) -> None:
+    """For a call without a derivative: refuses arguments that autograd follows, whose gradient would be lost."""
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which {fn} does not have: detach it, or call under torch.no_grad()")
+        if _tangent(t):
+            raise ValueError(f"{name} carries a tangent, which {fn} does not take on")
+
+
 def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """qwam_asp_matvec: the packed layer (either group, rotated or not, with or without a branch) on 1 to 16 tokens
     without quantizing them.  x bf16 [M][K] -> y bf16 [M][N].
-    `stream` is a torch.cuda.Stream (y and the workspace come from its pool)."""
+    `stream` is a torch.cuda.Stream (y and the workspace come from its pool).  There is no gradient: an x or a layer that
+    requires one is refused where autograd records."""
     if stream is None:
         y = (_call or _native()).matvec(layer, x, out)
         if y is not None:
@@ -396,6 +410,8 @@ def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] 
     M = x.shape[0]
     c = layer.c_struct(matvec=True)
     px = _req(x, "x", torch.bfloat16, (M, layer.K))
+    _no_gradient("asp_matvec", x=x, ws=layer.ws, inv_smooth=layer.inv_smooth, L1t=layer.L1t, L2t=layer.L2t, bias=layer.bias,
+                 L1f=layer.L1f)
     need = _need("qwam_asp_matvec", lib().qwam_asp_matvec_workspace(ctypes.byref(c), M))
     y = _empty((M, layer.N), torch.bfloat16, x.device, stream) if out is None else out
     ws = _workspace(need, x.device, stream)

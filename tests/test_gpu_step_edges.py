@@ -7,6 +7,8 @@ import paper_2609_33269_amd as P
 from paper_2609_33269_amd import block
 from paper_2609_33269_amd import qwam as Q
 from test_gpu_block_norm import _backward_check, _inputs
+from test_gpu_matvec import _layer, _x
+from test_gpu_paged_attention import _cache, _q
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +71,51 @@ def test_unused_outputs_have_no_gradient_tensor(used, monkeypatch):
         assert seen == [None]
         want = call(None, dh, xo.detach(), p["branch"], residual_scale=0.5, **kw)
         assert torch.equal(x.grad, want["dx"]) and torch.equal(b.grad, want["dbranch"])
+
+
+# ---- operators without a gradient ----
+
+def _tracked_calls():
+    """(call, tensors of it that a gradient could be asked of), fresh tensors."""
+    layer = _layer(256, 64, 16, bias=True)
+    x = _x(2, 256)
+    yield "asp_matvec", lambda: P.asp_matvec(layer, x), [x, layer.L2t, layer.L1f, layer.bias, layer.ws, layer.inv_smooth]
+    yield "asp_matvec", lambda: P.asp_matvec(layer, x, stream=torch.cuda.current_stream()), [x]
+    for fp8 in (False, True):
+        cache = _cache([30, 40], 2, 64, 16, fp8=fp8)
+        q, L = _q(2, 4, 64), torch.tensor([30, 40], dtype=torch.int32, device="cuda")
+        held = [cache.k_scale, cache.v_scale] if fp8 else [cache.k, cache.v]
+        yield "paged_attention", lambda: P.paged_attention(cache, q, L), [q] + held
+        k, v = _q(2, 2, 64, 3), _q(2, 2, 64, 4)
+        seq = torch.arange(2, dtype=torch.int32, device="cuda")
+        yield "kv_append", lambda: P.kv_append(cache, k, v, seq, L), [k, v] + held
+
+
+def test_no_gradient_vanishes():
+    """They have none: an input that requires one is refused, and taken where no gradient is recorded."""
+    for name, call, tensors in _tracked_calls():
+        for t in tensors:
+            call()
+            t.requires_grad_()
+            with pytest.raises(ValueError, match=f"requires a gradient, which {name} does not have"):
+                call()
+            with torch.no_grad():
+                call()
+            t.requires_grad_(False)
+
+
+def test_no_tangent_vanishes():
+    import torch.autograd.forward_ad as fwd
+    layer, x = _layer(256, 64, 16), _x(2, 256)
+    cache = _cache([30, 40], 2, 64, 16)
+    q, k, L = _q(2, 4, 64), _q(2, 2, 64, 3), torch.tensor([30, 40], dtype=torch.int32, device="cuda")
+    with fwd.dual_level():
+        dual = lambda t: fwd.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for name, call in (("asp_matvec", lambda: P.asp_matvec(layer, dual(x))),
+                           ("paged_attention", lambda: P.paged_attention(cache, dual(q), L)),
+                           ("kv_append", lambda: P.kv_append(cache, dual(k), k, L * 0, L)),
+                           ("kv_append", lambda: P.kv_append(cache, k, dual(k), L * 0, L))):
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(ValueError, match=f"carries a tangent, which {name} does not"):
+                    call()
+        P.asp_matvec(layer, x)
