@@ -133,7 +133,7 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
     x bf16 or float32 [T][D], branch bf16 [T][D]; gate, scale, shift bf16 [S][D] for S samples of T / S consecutive rows
     (their rows may be apart: a slice of a modulation's wider output); post_weight, weight bf16 [D].  Each of them may be
     None.  Returns (x' as x, h bf16); without a branch (the norm in front of the first block), (None, h) with x' = x.
-    `out` = (x', h) gives the outputs; x' may be x itself."""
+    `out` = (x', h) gives the outputs; x' may be x itself.  Gradients as block_norm_backward's; no forward-mode tangents."""
     if stream is None and out is None:
         done = (_q._call or _q._native()).norm(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale,
                                                shift)
@@ -141,6 +141,7 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
             if type(done) is int:
                 _q._check("qwam_block_norm", done)
             return done
+    _q._no_tangent("block_norm", x=x, branch=branch, gate=gate, post_weight=post_weight, weight=weight, scale=scale, shift=shift)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (x, branch, gate, post_weight, weight, scale, shift)):
         if out is not None or stream is not None:
@@ -157,7 +158,7 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
     """qwam_block_norm_backward: the gradients of block_norm at the stored x' (without a branch: x), from those of x'
     (None: none) and of h.  Returns a dict with dx (as x'), dbranch (bf16), and float32 dgate, dscale, dshift [S][D] and
     dpost_weight, dweight [D] for the parameters given (None for the others).  `wanted` limits the parameters' and the
-    branch's gradients to those named."""
+    branch's gradients to those named.  What it returns is not differentiable further."""
     if stream is None and wanted is None:
         done = (_q._call or _q._native()).norm_backward(dx_out, dh, x_out, branch, norm, eps, residual_scale, gate, post_norm,
                                                         post_weight, weight, scale, shift)
@@ -165,6 +166,8 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
             if type(done) is int:
                 _q._check("qwam_block_norm_backward", done)
             return done
+    _q._no_tangent("block_norm_backward", dx_out=dx_out, dh=dh, x_out=x_out, branch=branch, gate=gate, post_weight=post_weight,
+                   weight=weight, scale=scale, shift=shift)
     T, D = x_out.shape
     c = _norm_struct(x_out, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift)
     dev = x_out.device

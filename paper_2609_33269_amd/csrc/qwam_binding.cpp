@@ -270,11 +270,11 @@ at::Tensor workspace_of(int64_t need, const at::Tensor& like) {
   return need > 0 ? at::empty({need}, like.options().dtype(at::kByte)) : at::Tensor();
 }
 
+bool tangent(PyObject* o) { return THPVariable_Check(o) && THPVariable_Unpack(o)._fw_grad(0).defined(); }
+
 // whether autograd follows this argument (a tensor, or None): backwards, or forwards through a tangent
 bool tracked(PyObject* o) {
-  if (!THPVariable_Check(o)) return false;
-  const at::Tensor& t = THPVariable_Unpack(o);
-  return (t.requires_grad() && c10::GradMode::is_enabled()) || t._fw_grad(0).defined();
+  return tangent(o) || (THPVariable_Check(o) && c10::GradMode::is_enabled() && THPVariable_Unpack(o).requires_grad());
 }
 bool tracked(std::initializer_list<PyObject*> objects) {
   for (PyObject* o : objects)
@@ -397,6 +397,8 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (!norm_of(args + 4, T, D, f32, p) || (args[0] != Py_None && !data_of(args[0], x->scalar_type(), {T, D}, &dxo)) ||
       !data_of(args[1], at::kBFloat16, {T, D}, &dh) || (args[3] != Py_None && !data_of(args[3], at::kBFloat16, {T, D}, &branch)))
     return none_or_error();
+  for (Py_ssize_t i = 0; i < nargs; ++i)
+    if (tangent(args[i])) Py_RETURN_NONE;      // (false of what is no tensor)
   const int64_t need = g_norm_workspace(&p);
   if (need < 0) Py_RETURN_NONE;
   at::Tensor g[kGrads];

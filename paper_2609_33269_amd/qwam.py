@@ -387,13 +387,18 @@ def _tangent(t: Optional[torch.Tensor]) -> bool:
     return isinstance(t, torch.Tensor) and torch.autograd.forward_ad.unpack_dual(t).tangent is not None
 
 
+def _no_tangent(fn: str, **tensors) -> None:
+    for name, t in tensors.items():
+        if _tangent(t):
+            raise ValueError(f"{name} carries a tangent, which {fn} does not take on")
+
+
 def _no_gradient(fn: str, **tensors) -> None:
     """For a call without a derivative: refuses arguments that autograd follows, whose gradient would be lost."""
     for name, t in tensors.items():
         if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{name} requires a gradient, which {fn} does not have: detach it, or call under torch.no_grad()")
-        if _tangent(t):
-            raise ValueError(f"{name} carries a tangent, which {fn} does not take on")
+    _no_tangent(fn, **tensors)
 
 
 def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:

@@ -119,3 +119,18 @@ def test_no_tangent_vanishes():
                 with torch.set_grad_enabled(grad), pytest.raises(ValueError, match=f"carries a tangent, which {name} does not"):
                     call()
         P.asp_matvec(layer, x)
+
+
+def test_block_norm_refuses_tangents():
+    """It has a gradient but no forward-mode derivative."""
+    import torch.autograd.forward_ad as fwd
+    p, dh, _ = _inputs(6, 72, 2)
+    with fwd.dual_level():
+        for name in p:
+            kw = {n: (fwd.make_dual(t, torch.ones_like(t)) if n == name else t) for n, t in p.items()}
+            x, b = kw.pop("x"), kw.pop("branch")
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(ValueError, match=f"{name} carries a tangent, which block_norm does not"):
+                    P.block_norm(x, b, post_norm=True, **kw)
+            with pytest.raises(ValueError, match=f"{'x_out' if name == 'x' else name} carries a tangent, which block_norm_backward"):
+                P.block_norm_backward(None, dh, x, b, post_norm=True, **kw)
