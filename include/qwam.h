@@ -345,7 +345,9 @@ int64_t qwam_aog_protected_basis_workspace(int32_t d, int32_t r);
  *     y[m, n] = bf16( sum_g ws[g][n] sum_{k in g} x~[m, k] c[n, k]
  *                     + sum_j t[m, j] L2t[n, j] + bias[n] ),  t = x~ . L1
  * with the sums and t in float32; x~ enters the matrix cores as two bf16
- * pieces (within 2^-16 of it), or as it is where it is x itself.
+ * pieces (within 2^-16 of it), or as it is where it is x itself.  Nothing need
+ * be finite: infinities and NaN give in their token's row what the formula
+ * gives in float32, and have no effect on the others.
  *   L   in   packed layer: reads K, N, r, group, hadamard, wq, ws, inv_smooth,
  *            L1f, L2t, bias.  r = 0 (no branch; L1f and L2t are not read), 16,
  *            32, 48 or 64

@@ -1,5 +1,8 @@
 """Edges of a single token's step on the GPU."""
 
+import dataclasses
+
+import numpy as np
 import pytest
 import torch
 
@@ -7,7 +10,7 @@ import paper_2609_33269_amd as P
 from paper_2609_33269_amd import block
 from paper_2609_33269_amd import qwam as Q
 from test_gpu_block_norm import _backward_check, _inputs
-from test_gpu_matvec import _layer, _x
+from test_gpu_matvec import _layer, _terms, _x
 from test_gpu_paged_attention import _cache, _q
 
 pytestmark = pytest.mark.gpu
@@ -134,3 +137,39 @@ def test_block_norm_refuses_tangents():
                     P.block_norm(x, b, post_norm=True, **kw)
             with pytest.raises(ValueError, match=f"{'x_out' if name == 'x' else name} carries a tangent, which block_norm_backward"):
                 P.block_norm_backward(None, dh, x, b, post_norm=True, **kw)
+
+
+# ---- infinities ----
+
+@pytest.mark.parametrize("group", [64, 32])
+@pytest.mark.parametrize("smooth", [False, True])
+@pytest.mark.parametrize("K,N", [(320, 272), (12352, 48)])
+def test_matvec_of_infinities(K, N, smooth, group):
+    """An infinite or NaN channel gives what the definition gives, in that token alone: infinities of their sign, NaN
+    where its code is 0 or two of them meet."""
+    layer = _layer(K, N, 0, group, smooth=smooth, bias=True)
+    inf = float("inf")
+    for M in (1, 2, 4, 7, 8, 16):
+        x = _x(M, K)
+        finite = P.asp_matvec(layer, x)
+        for bad in ([(17, inf)], [(0, -inf), (K - 1, -inf)], [(40, inf), (41, -inf)], [(3, float("nan"))]):
+            m = (M - 1) // 2
+            y = x.clone()
+            for k, v in bad:
+                y[m, k] = v
+            with np.errstate(invalid="ignore"):
+                want = torch.from_numpy(_terms(layer, y[m:m + 1])[0][0])
+            got = P.asp_matvec(layer, y)
+            assert torch.equal(got[m].double().cpu().nan_to_num(nan=7.0), want.nan_to_num(nan=7.0)), f"{M} tokens, {bad}"
+            others = [i for i in range(M) if i != m]
+            assert torch.equal(got[others], finite[others])
+
+
+def test_rotated_matvec_of_infinities():
+    """A rotation spreads one over its block: the token is NaN, the others are what they were."""
+    layer = dataclasses.replace(_layer(512, 64, 16), hadamard=64)
+    x = _x(5, 512)
+    want = P.asp_matvec(layer, x)
+    x[3, 100] = float("inf")
+    got = P.asp_matvec(layer, x)
+    assert got[3].isnan().all() and torch.equal(got[[0, 1, 2, 4]], want[[0, 1, 2, 4]])
