@@ -468,6 +468,9 @@ qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *
  * there are none.  Scores, the softmax's maximum and sum, and o in float32;
  * its weights enter the product with V as two bf16 pieces; o is rounded once.
  * Values outside the visible positions (NaN, infinities) have no effect.
+ * Visible scores of -inf have weight 0, and where all are -inf o is zeros; one
+ * of +inf or NaN makes o[b][h] NaN.  An infinite or NaN value makes its channel
+ * of its heads' o infinite or NaN (which of the two is not specified).
  *   q        in  bf16, sequence b's q_heads x dim values at b * q_stride,
  *                16-byte aligned, q_stride % 8 == 0
  *   q_heads  in  a multiple of heads, at most 64 per key head, seqs * q_heads <= 2^22

@@ -11,7 +11,7 @@ from paper_2609_33269_amd import block
 from paper_2609_33269_amd import qwam as Q
 from test_gpu_block_norm import _backward_check, _inputs
 from test_gpu_matvec import _layer, _terms, _x
-from test_gpu_paged_attention import _cache, _q
+from test_gpu_paged_attention import _cache, _check, _q
 
 pytestmark = pytest.mark.gpu
 
@@ -173,3 +173,48 @@ def test_rotated_matvec_of_infinities():
     x[3, 100] = float("inf")
     got = P.asp_matvec(layer, x)
     assert got[3].isnan().all() and torch.equal(got[[0, 1, 2, 4]], want[[0, 1, 2, 4]])
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("length", [40, 700, 5000])
+def test_attention_of_infinite_scores(length, D):
+    """Scores of -inf have weight 0; where all of them are, the result is zeros; one of +inf makes it NaN, as a softmax."""
+    cache = _cache([length] * 2, 2, D, 64)
+    q = _q(2, 6, D).abs() + 0.125
+    L = torch.full((2,), length, dtype=torch.int32, device="cuda")
+    want = P.paged_attention(cache, q, L)
+    row = lambda b, p: (int(cache.table[b, p // 64]), slice(None), p % 64)  # noqa: E731
+    gone = list(range(0, length, 3))
+    for p in gone:
+        cache.k[row(0, p)] = -float("inf")
+    got = P.paged_attention(cache, q, L)
+    assert torch.equal(got[1], want[1]) and torch.isfinite(got).all()
+    # the same as without these positions
+    keep = [p for p in range(length) if p % 3]
+    packed = _cache([len(keep)], 2, D, 64)
+    for i, p in enumerate(keep):
+        for c, o in ((packed.k, cache.k), (packed.v, cache.v)):
+            c[int(packed.table[0, i // 64]), :, i % 64] = o[row(0, p)]
+    _check(packed, q[:1], [len(keep)], got[:1])
+    cache.k[row(1, length // 2)] = float("inf")
+    got = P.paged_attention(cache, q, L)
+    assert got[1].isnan().all() and torch.isfinite(got[0]).all()
+    for p in range(length):
+        cache.k[row(0, p)] = -float("inf")
+    assert (P.paged_attention(cache, q, L)[0] == 0).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("length", [40, 5000])
+def test_attention_of_values_that_are_not_finite(length, fp8):
+    """They reach their channel of their heads' results only, where these are not finite."""
+    cache = _cache([length] * 2, 2, 128, 64, fp8=fp8)
+    q, L = _q(2, 6, 128), torch.full((2,), length, dtype=torch.int32, device="cuda")
+    want = P.paged_attention(cache, q, L)
+    for bad in (float("nan"),) if fp8 else (float("nan"), float("inf"), -float("inf")):
+        v = cache.v.clone().view(torch.uint8 if fp8 else torch.bfloat16)
+        v[int(cache.table[1, 0]), 1, 5, 77] = 0x7F if fp8 else bad
+        got = P.paged_attention(P.PagedCache(cache.k, v.view(cache.v.dtype), cache.table, cache.k_scale, cache.v_scale), q, L)
+        assert not torch.isfinite(got[1, 3:, 77]).any()
+        got[1, 3:, 77] = want[1, 3:, 77]
+        assert torch.equal(got, want)
