@@ -218,3 +218,27 @@ def test_attention_of_values_that_are_not_finite(length, fp8):
         assert not torch.isfinite(got[1, 3:, 77]).any()
         got[1, 3:, 77] = want[1, 3:, 77]
         assert torch.equal(got, want)
+
+
+# ---- a table wider than the contexts ----
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_graph_over_a_wide_table(fp8):
+    """A program records its step with a table for the longest context it will allow, and replays it from the first
+    token on: the ranges are laid out for the table, the sequences fill few of them."""
+    H, D, page, width = 2, 128, 64, 1024
+    lengths = [0, 1, 100, 700, 9000, 5]
+    cache = _cache([n + 1 for n in lengths], H, D, page, fp8=fp8, width=width)
+    q = _q(len(lengths), 3 * H, D)
+    L = torch.zeros(len(lengths), dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = P.paged_attention(cache, q, L)
+    for now in ([0] * 6, [min(n, 1) for n in lengths], lengths, [n // 2 for n in lengths], [lengths[4 - i] if i < 5 else 5 for i in range(6)]):
+        now = [min(n, m + 1) for n, m in zip(now, lengths)]
+        L.copy_(torch.tensor(now, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, P.paged_attention(cache, q, L)), f"lengths {now}"
+        _check(cache, q, now, out)
