@@ -92,6 +92,12 @@ __device__ __forceinline__ float finite_part(float v) {
   return __builtin_amdgcn_fmed3f(v, -kBf16Max, kBf16Max);
 }
 
+// orders LDS accesses of a wave's lanes to each other's places: the hardware takes a wave's in order, the compiler must too
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // what x holds: the tokens as they are, tokens still to be smoothed, or the two
 // pieces of each x~ (rows 2 m and 2 m + 1), as the rotation leaves them
 enum Input { kPlain, kSmooth, kPieces };
@@ -355,7 +361,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
       Branch l;
       load_x(chunk);
       load_branch(lo + chunk * UPC, l);
+      wave_order();
       store_x();
+      wave_order();
 #pragma unroll 1
       for (int u = 0; u < UPC; ++u) {
         const int unit = lo + chunk * UPC + u;
@@ -380,7 +388,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
     }
     __syncthreads();
     auto step = [&](int chunk, const Codes& b, Codes& ahead) __attribute__((always_inline)) {
+      wave_order();                // the chunk before has been read
       store_x();
+      wave_order();
       if (chunk + 1 < chunks) {
         load_x(chunk + 1);
         load_codes(chunk + 1, ahead);
