@@ -45,21 +45,23 @@ def _per_sample(t: Optional[torch.Tensor], name: str, S: int, D: int):
 
 
 def _samples(gate, scale, shift) -> int:
-    for t in (gate, scale, shift):
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
         if t is not None:
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch.Tensor")
             if t.dim() != 2:
                 raise ValueError("gate, scale and shift have two dimensions (samples, width)")
             return t.shape[0]
     return 1
 
 
-def _norm_struct(x, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift):
+def _norm_struct(x, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift, x_name="x"):
     if norm not in NORM_KINDS:
         raise ValueError(f"norm must be one of {sorted(NORM_KINDS)} (got {norm!r})")
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise ValueError("x must be a tensor of two dimensions (rows, width)")
+        raise ValueError(f"{x_name} must be a tensor of two dimensions (rows, width)")
     if x.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"x must be {torch.bfloat16} or {torch.float32} (got {x.dtype})")
+        raise TypeError(f"{x_name} must be {torch.bfloat16} or {torch.float32} (got {x.dtype})")
     if post_weight is not None and not post_norm:
         raise ValueError("post_weight without post_norm")
     T, D = x.shape
@@ -76,8 +78,8 @@ def _norm_struct(x, norm, eps, residual_scale, gate, post_norm, post_weight, wei
 
 
 def _forward(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift, out, stream):
-    T, D = x.shape
     c = _norm_struct(x, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift)
+    T, D = x.shape
     px = _q._req(x, "x", x.dtype, (T, D))
     pb = None if branch is None else _q._req(branch, "branch", torch.bfloat16, (T, D))
     xo, h = (None, None) if out is None else out
@@ -142,7 +144,7 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
                 _q._check("qwam_block_norm", done)
             return done
     _q._no_tangent("block_norm", x=x, branch=branch, gate=gate, post_weight=post_weight, weight=weight, scale=scale, shift=shift)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
                                        for t in (x, branch, gate, post_weight, weight, scale, shift)):
         if out is not None or stream is not None:
             raise ValueError("block_norm under autograd takes neither out nor stream")
@@ -168,8 +170,8 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
             return done
     _q._no_tangent("block_norm_backward", dx_out=dx_out, dh=dh, x_out=x_out, branch=branch, gate=gate, post_weight=post_weight,
                    weight=weight, scale=scale, shift=shift)
+    c = _norm_struct(x_out, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift, "x_out")
     T, D = x_out.shape
-    c = _norm_struct(x_out, norm, eps, residual_scale, gate, post_norm, post_weight, weight, scale, shift)
     dev = x_out.device
     pd = None if dx_out is None else _q._req(dx_out, "dx_out", x_out.dtype, (T, D))
     ph = _q._req(dh, "dh", torch.bfloat16, (T, D))
