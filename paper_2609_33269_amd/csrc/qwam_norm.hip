@@ -328,7 +328,7 @@ __global__ __launch_bounds__(TPR > kBwdThreads ? TPR : kBwdThreads) void block_n
   if constexpr (AHEAD) load(block * GROUPS + group, ahead);
   // every group of the workgroup goes round as often as the first, for the barriers
   for (int r0 = block * GROUPS; r0 < p.rows; r0 += g.blocks * GROUPS) {
-    const bool real = r0 + group < p.rows;
+    const bool real = GROUPS == 1 || r0 + group < p.rows;
     const int n = real ? D : 0;
     const int64_t at = (static_cast<int64_t>(s) * p.rows + r0 + group) * D;
     Row r;
