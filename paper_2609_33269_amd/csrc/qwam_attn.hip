@@ -59,19 +59,18 @@ __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t 
   if (i >= threads) return;
   const uint32_t per_head = c.dim / 8, row = i / per_head, t = row / c.heads, head = row - t * c.heads, d = (i - row * per_head) * 8;
   const int s = seq[t], q = pos[t];
-  const uint4 in[2] = {*reinterpret_cast<const uint4*>(k + t * k_stride + head * c.dim + d),
-                       *reinterpret_cast<const uint4*>(v + t * v_stride + head * c.dim + d)};
+  const uint4 ki = *reinterpret_cast<const uint4*>(k + t * k_stride + head * c.dim + d);
+  const uint4 vi = *reinterpret_cast<const uint4*>(v + t * v_stride + head * c.dim + d);
   if (s < 0 || s >= c.seqs || q < 0 || (q >> c.page_bits) >= c.table_width) return;
   const int page = c.table[static_cast<int64_t>(s) * c.table_width + (q >> c.page_bits)];
   if (page < 0 || page >= c.pages) return;
   const int64_t at = page * c.page_stride + head * c.head_stride + (q & ((1 << c.page_bits) - 1)) * c.row_stride + d;
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    void* const base = w == 0 ? c.k : c.v;
+  // (called twice rather than a loop over the two, which was not unrolled in bf16 and took them through LDS)
+  auto put = [&](const uint4& in, void* base, const float* scales) __attribute__((always_inline)) {
     if constexpr (FP8) {
-      const float scale = (w == 0 ? c.k_scale : c.v_scale)[head];
+      const float scale = scales[head];
       float f[8];
-      const uint32_t u[4] = {in[w].x, in[w].y, in[w].z, in[w].w};
+      const uint32_t u[4] = {in.x, in.y, in.z, in.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = bf16_to_f32((u[e >> 1] >> (16 * (e & 1))) & 0xFFFFu) / scale;
@@ -80,9 +79,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t 
       *reinterpret_cast<uint2*>(static_cast<uint8_t*>(base) + at) =
           make_uint2(fp8x4(f[0], f[1], f[2], f[3]), fp8x4(f[4], f[5], f[6], f[7]));
     } else {
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) = in[w];
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) = in;
     }
-  }
+  };
+  put(ki, c.k, c.k_scale);
+  put(vi, c.v, c.v_scale);
 }
 
 namespace {
