@@ -5,8 +5,10 @@ checked here, every step runs in the library's HIP kernels, and there is no
 fallback.
 
 block_norm is differentiable: with an input that requires a gradient it records
-block_norm_backward (calibration back-propagates its probe vectors through the
-norms between two layers); that needs gradients of bf16 and float32 tensors only.
+block_norm_backward, so probe vectors can be back-propagated through the norms
+between two layers (those through the layers themselves are the caller's, by
+the float weights).  asp_matvec and the cache's calls have no gradient and
+refuse inputs that require one.
 """
 
 from __future__ import annotations

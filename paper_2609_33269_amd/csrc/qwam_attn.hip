@@ -2,9 +2,9 @@
 // (qwam_kv_append), and the attention of one new token per sequence
 // (qwam_paged_attention):
 //   o[h] = sum_p softmax_p(scale q[h] . K[p]) V[p], the G = q_heads / heads query heads of a key head together.
-// Every key and value is read once from HBM and serves G heads; with G <= 16 that
-// is far below what the matrix cores need to be busy, so the stream of the pages
-// is the bound and everything below is laid out for it:
+// Every key and value is read once for each 16 query heads of its key head (once
+// for G <= 16) and serves those; that is far below what the matrix cores need to be
+// busy, so the stream of the pages is the bound and everything below is laid out for it:
 //
 //   * A workgroup takes one key head (and up to 16 query heads) of one sequence
 //     over a range of its positions, its waves 32 of them in turn.  Ranges of up to
@@ -27,9 +27,11 @@
 //     handed out by readlane, so that addresses are scalar.
 //   * Positions outside [start, length) or without a page get weight 0, and their
 //     values are replaced by 0 before the product (0 * NaN is not 0).
-// Measured: two contexts up to 131072 in fp8, 8 x 3 heads of 128, 65.8 us (5.1 TB/s); one of
-// 65536 in bf16 53 us (5.0 TB/s); 16 ragged ones up to 4096 18.0 us (2.7 TB/s: few turns a wave,
-// each 1.1 us of dependent products and exponentials); one of 77 3.9 us.
+// Measured, 8 x 3 heads of 128: two contexts up to 131072 in fp8 66 us (5.1 TB/s); one of 65536 in bf16
+// 53.6 us (5.0 TB/s); 32 of 512 13.1 us (5.2 TB/s); 16 ragged ones up to 4096 18.0 us (2.7 TB/s: 256 workgroups
+// of one to four turns of their waves, a turn 1.2 us of dependent loads, products and exponentials when alone);
+// one of 4096 10.0 us, in a table that reaches 131072 17.0 (ranges go by the reach).  8 x 8 x G heads over 4096:
+// G = 16 31.6 us, 32 (two tiles of heads, each reading the pages) 49.5.  One of 77, 16 heads of 64, 3.9 us in a graph.
 #include <initializer_list>
 
 #include "qwam_device.h"
@@ -49,8 +51,9 @@ __device__ __forceinline__ uint32_t fp8x4(float a, float b, float c, float d) {
 }  // namespace
 
 // One thread per 8 keys and the 8 values beside them (at most 2^29 threads, so that indexes are divided in 32 bits).
-// Bound by the chain position - table - store (16 tokens 3.7 us in a graph) and, for prompts in fp8, by that and the
-// divisions: 2200 tokens 7.0 us (2.7 TB/s), with 16 channels a thread 7.7.
+// Bound by the chain position - table - store (16 tokens in bf16 2.1 us in a graph) and, for prompts in fp8, by that and
+// the divisions: 3098 tokens 6.9 us (2.8 TB/s; 1.3 of it the divisions, 0.2 the scales' place behind the table), with 16
+// channels a thread 7.7; in bf16 6.4 us (4.0 TB/s).
 template <bool FP8>
 __global__ __launch_bounds__(256) void kv_append_kernel(CacheParams c, uint32_t threads, const uint16_t* k, int64_t k_stride,
                                                         const uint16_t* v, int64_t v_stride, const int32_t* seq,
@@ -197,8 +200,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
   };
 
   uint4 kr[2][NK];
-  // heads of 64: V comes a tile ahead too (in wider ones its registers cost more waves than that gains: 4 x 16
-  // heads of 64 over 16384 positions 32.6 -> 27.6 us, 16 x 8 x 3 of 128 over 4096 18.2 -> 19.2)
+  // heads of 64: V comes a tile ahead too (in wider ones its registers cost more waves than that gains: 4 ragged
+  // contexts up to 16384, 16 heads of 64, 32.4 -> 27.6 us, one alone 17.0 -> 17.7; 16 up to 4096, 8 x 3 of 128, 18.0 -> 19.2)
   constexpr bool V_AHEAD = DP == 64;
   uint32_t va[8][NV], vb[8][NV];
   int id[2], idn[2];
@@ -472,13 +475,13 @@ Plan plan_of(const CacheParams& c, bool fp8, int q_heads, int max_len) {
   auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
   const int64_t rows = rows_of(c, q_heads);
   // one range where a second launch would cost as much as the waves' turns (1.1 us for
-  // each 128 positions of 8 x 3 heads of 128; 64 sequences of 500: 13.5 us, in two ranges 18.6)
+  // each 128 positions of 8 x 3 heads of 128; 64 sequences up to 500: 13.8 us, in two ranges 18.3)
   if (max_len <= kOneRange) return {static_cast<int>(up(max_len, 32)), 1};
   // Workgroups for every CU four times, of half as wide values twice (ranges of as many
-  // bytes: 8 x 3 heads of 128 over 131072 positions in fp8 66 us, with 1024 workgroups 74; 16 x 8 x 3 over
-  // 4096 in bf16 18.0 us, with 512 26.0); no more than 256 ranges to join, their partial results
+  // bytes: two contexts up to 131072, 8 x 3 heads of 128 in fp8 66 us, with 1024 workgroups 74; 16 up to
+  // 4096 in bf16 18.0 us, with 512 26.0, with 2048 21.3); no more than 256 ranges to join, their partial results
   // at most 1/16 of what they read, and no range of one turn of the waves in a long context
-  // (4 x 2 x 2 heads of 80 over 16197 positions 12.4 us, with ranges of 128 15.0)
+  // (4 ragged ones up to 16197, 2 x 2 heads of 80, 12.4 us, with ranges of 128 15.0)
   const int64_t heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16, want = fp8 ? 512 : 1024;
   int64_t n = (rows * max_len + want - 1) / want;
   for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 64 * heads / (fp8 ? 1 : 2), int64_t(max_len > 4096 ? 256 : 128)})

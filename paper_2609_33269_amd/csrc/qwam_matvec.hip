@@ -15,14 +15,15 @@
 //   * x~ = x * inv_smooth is not a bf16 number.  It enters as two, hi = bf16(x~)
 //     and lo = bf16(x~ - hi), within 2^-17 of x~: each piece is a row of its own
 //     (few tokens leave most of the 16 rows empty anyway).  hi is kept finite, so that an
-//     infinite x~ is inf in lo alone (one more instruction a value: 7 tokens at 14336 x 3072 16.7 us, without 16.5).
+//     infinite x~ is inf in lo alone (one more instruction a value: 7 tokens at 14336 x 3072 16.7 us, without 16.5;
+//     16 at 3072 x 9216 18.6 and 17.9).
 //   * A wave's 16 bytes per lane are 32 consecutive codes of a row, so its four
 //     quarters hold 128 channels: two groups of 64 or four of 32, each with its own
 //     scale, while an MFMA sums over the quarters.  Up to four vectors have a row per
 //     group, which holds zeros outside it.  For more, half-wave and 16-lane swaps
 //     (eight or sixteen instructions a step) first give every quarter its share of
 //     each group, and a vector has one row.  (The swaps for all: one token at 4096 x 28672 14.6 us
-//     instead of 14.0.  Rows per group for all: two to four times the MFMAs and LDS
+//     instead of 13.9.  Rows per group for all: two to four times the MFMAs and LDS
 //     reads, 18.7 us instead of 16.5 for 7 tokens at 14336 x 3072 in groups of 32.)
 //   * The pieces are staged in the wave's own part of LDS, CK channels at a time,
 //     while the codes of the next CK are on their way; no barrier until the end.
@@ -32,8 +33,9 @@
 //     than a launch; otherwise in workgroups of its own, K in parts for them and for
 //     y, and a second launch joins the parts.
 // Measured: 4096 x 28672 without a branch, one token 13.8 us (4.8 TB/s; with a workgroup's eight
-// waves 17.6); 1024 x 1024, rank 16, one token 4.6 us; 14336 x 3072, group 32, rank 32, one token
-// 12.2 and seven 16.5 us, of them 4 for the join; 16 tokens at 4096 x 28672 19.6 us.
+// waves 16.1); 1024 x 1024, rank 16, one token 4.6 us; 14336 x 3072, group 32, rank 32, one token
+// 12.8 and seven 16.7 us, of them 4 for the join; 16 tokens at 4096 x 28672 19.6 us.  Rotated: 1024 x 1024,
+// rank 16, block 64, one token 8.2 us (6.2 in a graph, without the rotation 4.3); 14336 x 3072, block 512, seven 22.7 us.
 #include <cmath>
 
 #include "qwam_device.h"
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void matvec_kernel(MatvecArgs a)
   constexpr int SETS = (MV + kRows - 1) / kRows;
   constexpr int CK = chunk_channels(MV, NT);         // channels staged at a time
   // row 4 g + v is vector v within group g of a unit; not with t beside y, whose fragments of L1 then come in
-  // smaller pieces (1024 x 1024 4.9 us instead of 4.6)
+  // smaller pieces (1024 x 1024 5.0 us instead of 4.6)
   constexpr bool GROUP_ROWS = MV == 4 && RB == 0;
   constexpr int UPC = CK / kUnit;                    // units of a chunk
   constexpr int LPT = CK / 8;                        // lanes that stage one token's chunk, 8 channels each
@@ -519,27 +521,28 @@ struct Form {
 Form form_of(int M, int N, int K, int r, bool smooth) {
   const int units = (K + kUnit - 1) / kUnit, tiles = N / kCols;
   // t once per workgroup is cheaper than a launch while all of them together read little of L1: 8 MB (1024 x 4096,
-  // rank 16) 4.7 us against 8.1 with a join, 38 MB (3072 x 3072, rank 32) 6.4 against 8.0 and for 16 tokens 11.1 against
-  // 11.0, 57 MB (3072 x 9216, rank 16) 10.4 against 10.2 and for 4 tokens 14.3 against 11.2; and while there are no more
-  // of these narrow workgroups than the CUs hold: 192 x 28656, 11 tokens, rank 32 22.7 against 10.9
-  // long rows of few workgroups go in parts with or without a branch: 16384 x 1024, plain, one token 7.0 us against 7.9
-  // in one, 16 tokens 9.8 against 14.2, 14336 x 1024, rank 16 8.8 against 12.3; but 16384 x 2048, plain 10.3 against 8.0
+  // rank 16) 4.7 us against 7.3 with a join, 38 MB (3072 x 3072, rank 32) 6.4 against 7.5 and for 16 tokens 11.4 against
+  // 11.3, 57 MB (3072 x 9216, rank 16) 10.4 against 10.2 and for 4 tokens 14.5 against 11.4; and while there are no more
+  // of these narrow workgroups than the CUs hold: 192 x 28656, 11 tokens, rank 32 22.8 against 11.0
+  // long rows of few workgroups go in parts with or without a branch: 16384 x 1024, plain, one token in a graph 6.6 us
+  // against 7.9 in one (call by call the host takes as long: 7.6 to 8.2 and 7.9), 16 tokens 9.7 against 14.3, 14336 x 1024,
+  // rank 16 8.8 against 12.3; but 16384 x 2048, plain 10.1 against 8.0
   const bool alone = units <= 64 || tiles > 96;
   const bool fused = r == 0 ? alone : (alone && r <= 32 && tiles <= 768 && static_cast<int64_t>(tiles) * K * r * 2 <= (int64_t(48) << 20));
-  // Wider workgroups stage x for more channels; the widest hold fewer waves.  4096 x 28672, plain, one token 14.5 us with
-  // one tile and 15.6 with two, 8 tokens 22.5 and 18.2, 16 tokens 20.7 with two and 19.6 with four.
+  // Wider workgroups stage x for more channels; the widest hold fewer waves.  4096 x 28672, plain, one token 13.9 us with
+  // one tile and 14.4 with two, 8 tokens 22.3 and 18.3 (with four 17.5), 16 tokens 20.7 with two and 19.6 with four.
   if (fused) {
     const int V = M * (smooth ? 2 : 1);
     int nt = r > 0 || V <= 4 ? 1 : V <= 8 || V > 16 ? 2 : 4;      // (two sets of four tiles spill)
     while (nt > 1 && tiles < 256 * nt) nt /= 2;
     return {nt, 1, 0, true};
   }
-  // 3072 x 9216, rank 32, one token 10.5 us with one tile and 11.7 with two (fewer channels: the same)
+  // 3072 x 9216, rank 32, one token 10.4 us with one tile and 10.6 with two (fewer channels: the same)
   const int nt = M <= 2 && tiles >= 512 ? 1 : 2, blocks = (tiles + nt - 1) / nt;
   auto within = [](int v, int most) { return v < 1 ? 1 : v < most ? v : most; };
   const int most = within((units + kWaves - 1) / kWaves, kMaxSplits);
-  // about 512 workgroups, and no more of the largest, of which a CU holds two: 14336 x 3072, 16 tokens, 18.4 us in five
-  // parts, 20.9 in four, 22.4 in eight; 3072 x 9216, 4 tokens, 13.2 us in one and 11.5 in two, 16 tokens 17.9 and 19.7
+  // about 512 workgroups, and no more of the largest, of which a CU holds two: 14336 x 3072, group 32, 16 tokens, 20.1 us in five
+  // parts, 23.4 in four, 24.0 in eight; 3072 x 9216, 4 tokens, 13.3 us in one and 11.7 in two, 16 tokens 18.6 and 20.1
   return {nt, within((M > 8 ? 512 : 512 + blocks / 2) / blocks, most), most, false};
 }
 
@@ -551,8 +554,8 @@ hipError_t launch(MatvecArgs a, hipStream_t stream) {
   a.tblocks = (a.r / 16 + NT - 1) / NT;
   const int grid = a.blocks * a.splits + a.tblocks * a.tsplits;
   // A wave has a unit at least; the fused t also a thread for each output.  Eight waves where the workgroups are few and
-  // the rows long enough for a unit or two in each: 8192 x 1024, one token 5.6 us, with four 6.3; with t beside it
-  // 4096 x 1024 6.0 and 6.5, but 1024 x 1024 5.0 and 4.9
+  // the rows long enough for a unit or two in each: 8192 x 1024, one token 5.6 us, with four 6.1; with t beside it
+  // 4096 x 1024 5.8 and 6.4, but 1024 x 1024 4.8 and 4.7
   a.waves = per_split >= (RB == 0 ? 8 : 16) && grid <= 256 ? kMaxWaves : per_split >= 3 || RB > 0 ? kWaves : per_split;
   const int per = (per_split + a.waves - 1) / a.waves * kUnit;
   a.pitch = (per < CK ? per : CK) * 2 + 16;
