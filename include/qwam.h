@@ -474,6 +474,8 @@ qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *
  *   q        in  bf16, sequence b's q_heads x dim values at b * q_stride,
  *                16-byte aligned, q_stride % 8 == 0
  *   q_heads  in  a multiple of heads, at most 64 per key head, seqs * q_heads <= 2^22
+ *                (tokens of a sequence that all see the same positions can be passed
+ *                as further query heads beside each other of every key head)
  *   lengths  in  int32 [seqs], taken as at most max_len and the table's reach,
  *                and below 0 as 0
  *   starts   in  int32 [seqs], or NULL for 0
