@@ -428,30 +428,38 @@ int64_t qwam_block_norm_backward_workspace(const qwam_norm *p);
  * page: nothing is stored there and attention does not see its positions. */
 #define QWAM_CACHE_BF16 0
 #define QWAM_CACHE_FP8 1        /* e4m3 (finite, no infinities); value = code * scale[head]  */
+#define QWAM_CACHE_FP4 4        /* e2m1, two channels to a byte, the lower one in the lower half: codes 0, .5, 1, 1.5,  */
+                                /* 2, 3, 4, 6 and a sign bit above; value = code * 2^(E - 127), E the byte of its       */
+                                /* position and group of 32 channels, 255 for NaN                                      */
 typedef struct qwam_cache {
     int32_t pages;              /* pages in k and v                                     */
     int32_t page_size;          /* positions of a page: a power of two, 16 .. 4096      */
     int32_t heads;              /* key heads                                            */
-    int32_t dim;                /* head width, % 8 == 0 (fp8: % 16), 8 .. 256           */
-    int32_t type;               /* QWAM_CACHE_BF16 or QWAM_CACHE_FP8                    */
+    int32_t dim;                /* head width, % 8 == 0 (fp8: % 16, fp4: % 32), 8 .. 256 */
+    int32_t type;               /* QWAM_CACHE_BF16, QWAM_CACHE_FP8 or QWAM_CACHE_FP4    */
     int32_t seqs;               /* rows of the table                                    */
     int32_t table_width;        /* entries of a row; the first table_width * page_size  */
                                 /* positions of a sequence exist (below 2^31)           */
     int32_t reserved;           /* 0                                                    */
-    int64_t page_stride, head_stride, row_stride;   /* elements between pages, heads and rows;  */
-                                /* multiples of 8 (fp8: 16), the same for k and v;       */
-                                /* |row_stride| < 2^26                                  */
+    int64_t page_stride, head_stride, row_stride;   /* elements (fp4: bytes) between pages, heads and   */
+                                /* rows; multiples of 8 (fp8, fp4: 16), the same for k  */
+                                /* and v; |row_stride| < 2^26                           */
     void *k, *v;                /* 16-byte aligned                                      */
-    const float *k_scale, *v_scale;                 /* float [heads] (fp8), else not read   */
+    const void *k_scale, *v_scale;                  /* fp8: float [heads].  fp4: uint8          */
+                                /* [pages][heads][dim / 32][page_size], 16-byte         */
+                                /* aligned, which qwam_kv_append writes.  bf16: not read */
     const int32_t *table;       /* [seqs][table_width]                                  */
 } qwam_cache;
 
 /*
  * New keys and values into the pages: token t goes to position pos[t] of
  * sequence seq[t].  fp8: code = e4m3(clamp(x / scale[head], -448, 448)), to
- * nearest, ties to even.  A token whose sequence or position does not exist,
- * or whose page does not, is not stored (a negative pos marks padding).  Two
- * tokens of one call must not share a slot.
+ * nearest, ties to even.  fp4: E - 127 is the least e in [-123, 125] with
+ * absmax <= 7 * 2^e over the group, code = e2m1(x / 2^e), to nearest, ties to the
+ * even code, 6 at most; a group with an infinity or NaN gets E = 255.  A token
+ * whose sequence or position does not exist, or whose page does not, is not
+ * stored (a negative pos marks padding).  Two tokens of one call must not share
+ * a slot.
  *   tokens   in  >= 1, tokens * heads * dim <= 2^32
  *   k, v     in  bf16, token t's heads x dim values at t * k_stride (v_stride),
  *                16-byte aligned, strides % 8 == 0
@@ -460,6 +468,18 @@ typedef struct qwam_cache {
 qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *k, int64_t k_stride,
                            const uint16_t *v, int64_t v_stride, const int32_t *seq,
                            const int32_t *pos, void *stream);
+
+/*
+ * Stored keys and values back as bf16: token t gets those of position pos[t] of
+ * sequence seq[t], the value rounded once (bf16 and fp4: exactly the value), and
+ * zeros where qwam_kv_append would not store.
+ *   tokens   in  as for qwam_kv_append
+ *   seq, pos in  int32 [tokens]
+ *   k, v     out bf16, laid out as qwam_kv_append's; with more than one token
+ *                |k_stride|, |v_stride| >= heads * dim
+ */
+qwam_status qwam_kv_read(const qwam_cache *c, int32_t tokens, const int32_t *seq, const int32_t *pos, uint16_t *k,
+                         int64_t k_stride, uint16_t *v, int64_t v_stride, void *stream);
 
 /*
  * Attention of one new token per sequence over its pages:
@@ -492,6 +512,39 @@ qwam_status qwam_paged_attention(const qwam_cache *c, int32_t q_heads, const uin
 /* Bytes of workspace of qwam_paged_attention; -1 if not supported.  Reads
  * the cache's integers only. */
 int64_t qwam_paged_attention_workspace(const qwam_cache *c, int32_t q_heads, int32_t max_len);
+
+/* Rotary positions over one or several axes (time, height, width): pair i of
+ * every head turns by the token's position on the pair's axis times its
+ * frequency. */
+typedef struct qwam_rope_plan {
+    int32_t heads, dim;         /* dim <= 4096                                          */
+    int32_t pairs;              /* 1 .. dim / 2; channels from 2 * pairs on do not turn */
+    int32_t interleaved;        /* pair i: nonzero channels 2i and 2i + 1,              */
+                                /* 0 channels i and i + pairs                           */
+    int32_t axes;               /* 1 .. 4                                               */
+    int32_t positions;          /* rows of pos: token t has row t % positions           */
+    int32_t pos_f32;            /* nonzero: pos is float, 0: int32                      */
+    int32_t x_f32;              /* nonzero: x and y are float, 0: bf16                  */
+    const void *pos;            /* [positions][axes]                                    */
+    const float *inv_freq;      /* [pairs]                                              */
+    const int32_t *axis;        /* [pairs]; a pair of another axis than 0 .. axes - 1   */
+                                /* does not turn                                        */
+} qwam_rope_plan;
+
+/*
+ * y[a] = x[a] cos - x[b] sin,  y[b] = x[a] sin + x[b] cos  for the channels a, b of pair i,
+ * the angle pos[t % positions][axis[i]] * inv_freq[i] (inverse: its negative, which
+ * is also the gradient).  The angle is reduced in float64 (its error below 2^-50 of
+ * itself), cos and sin are within 2^-22, products and sums in float32, y is rounded
+ * once; channels that do not turn are copied.
+ *   tokens   in  >= 1, tokens % positions == 0, tokens * heads * dim <= 2^32
+ *   x        in  bf16 or float, token t's heads x dim values at t * x_stride (aligned to its
+ *                elements; 16-byte aligned rows and widths of 8 are faster)
+ *   y        out as x; may be x itself with the same stride, and must not overlap it otherwise;
+ *                with more than one token |y_stride| >= heads * dim
+ */
+qwam_status qwam_rope(const qwam_rope_plan *p, int32_t tokens, int32_t inverse, const void *x, int64_t x_stride, void *y,
+                      int64_t y_stride, void *stream);
 
 /* Message describing the calling thread's last non-OK status ("" if none). */
 const char *qwam_last_error(void);

@@ -22,7 +22,8 @@ import torch
 from . import qwam as _q
 
 NORM_KINDS = {"rms": 0, "layer": 1}
-CACHE_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1}
+CACHE_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float4_e2m1fn_x2: 4}
+FP4_GROUP = 32                   # channels of a scale of 4-bit pages
 
 
 # ---------------------------------------------------------------------------
@@ -208,9 +209,11 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
 class PagedCache:
     """Keys and values in pages (include/qwam.h): position p of sequence s in row p % page of page table[s, p // page].
 
-    k, v: bf16 or float8_e4m3fn [pages][heads][page][dim], equal strides, dim contiguous (any order of the others: pages
-    that hold their rows first, or both of k and v, are views of this form).  table: int32 [sequences][width], entries
-    outside the pages mean no page.  k_scale, v_scale: float32 [heads], with float8 pages (value = code * scale)."""
+    k, v: bf16 or float8_e4m3fn [pages][heads][page][dim], or float4_e2m1fn_x2 [pages][heads][page][dim / 2], equal strides,
+    dim contiguous (any order of the others: pages that hold their rows first, or both of k and v, are views of this
+    form).  table: int32 [sequences][width], entries outside the pages mean no page.  k_scale, v_scale: with float8
+    pages float32 [heads] (value = code * scale); with float4 pages float8_e8m0fnu [pages][heads][dim / 32][page], a power
+    of two for each position and group of 32 channels, which kv_append writes beside the codes."""
     k: torch.Tensor
     v: torch.Tensor
     table: torch.Tensor
@@ -227,7 +230,8 @@ class PagedCache:
             if t.device.type != "cuda":
                 raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
             if t.dtype not in CACHE_TYPES or t.dtype != self.k.dtype:
-                raise TypeError(f"{name} must be {torch.bfloat16} or {torch.float8_e4m3fn}, k and v alike (got {t.dtype})")
+                raise TypeError(f"{name} must be {torch.bfloat16}, {torch.float8_e4m3fn} or {torch.float4_e2m1fn_x2}, k and v alike "
+                                f"(got {t.dtype})")
             if t.dim() != 4 or t.shape != self.k.shape:
                 raise ValueError(f"{name} must have shape [pages][heads][page][dim], k and v alike (got {tuple(t.shape)})")
             if t.stride(3) != 1 or t.stride() != self.k.stride():
@@ -237,18 +241,31 @@ class PagedCache:
         c = _q.QwamCacheC()
         c.pages, c.heads, c.page_size, c.dim = self.k.shape
         c.type, (c.seqs, c.table_width) = CACHE_TYPES[self.k.dtype], self.table.shape
+        four = self.k.dtype == torch.float4_e2m1fn_x2
+        if four:
+            c.dim *= 2
         c.page_stride, c.head_stride, c.row_stride = self.k.stride()[:3]
         c.k, c.v = self.k.data_ptr(), self.v.data_ptr()
         c.table = _q._req(self.table, "table", torch.int32, tuple(self.table.shape))
         if c.type:
-            c.k_scale = _q._req(self.k_scale, "k_scale", torch.float32, (c.heads,))
-            c.v_scale = _q._req(self.v_scale, "v_scale", torch.float32, (c.heads,))
+            shape = (c.pages, c.heads, c.dim // FP4_GROUP, c.page_size) if four else (c.heads,)
+            kind = torch.float8_e8m0fnu if four else torch.float32
+            c.k_scale = _q._req(self.k_scale, "k_scale", kind, shape)
+            c.v_scale = _q._req(self.v_scale, "v_scale", kind, shape)
         return c
 
 
 def new_cache(pages: int, heads: int, dim: int, seqs: int, table_width: int, page: int = 64, dtype=torch.bfloat16,
               k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda") -> PagedCache:
-    """An empty cache: zeroed pages, tables without pages."""
+    """An empty cache: zeroed pages, tables without pages.  dtype: bfloat16, float8_e4m3fn (with k_scale and v_scale) or
+    float4_e2m1fn_x2 (whose scales are allocated here, all 1, unless given)."""
+    if dtype == torch.float4_e2m1fn_x2:
+        if dim % FP4_GROUP:
+            raise ValueError(f"dim must be a multiple of {FP4_GROUP} with {dtype} (got {dim})")
+        one = lambda: torch.full((pages, heads, dim // FP4_GROUP, page), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)  # noqa: E731
+        z = lambda: torch.zeros((pages, heads, page, dim // 2), dtype=torch.uint8, device=device).view(dtype)  # noqa: E731
+        return PagedCache(z(), z(), torch.full((seqs, table_width), -1, dtype=torch.int32, device=device),
+                          one() if k_scale is None else k_scale, one() if v_scale is None else v_scale)
     z = lambda: torch.zeros((pages, heads, page, dim), dtype=torch.bfloat16, device=device).to(dtype)  # noqa: E731
     return PagedCache(z(), z(), torch.full((seqs, table_width), -1, dtype=torch.int32, device=device), k_scale, v_scale)
 
@@ -270,7 +287,7 @@ def _rows(t: torch.Tensor, name: str, shape) -> int:
 
 def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None) -> None:
     """qwam_kv_append: k, v bf16 [tokens][heads][dim] to position pos[t] of sequence seq[t] (int32 [tokens]), rounded to
-    float8 where the pages are.  Tokens without a place (pos < 0, no page) are not stored.  There is no gradient: tensors
+    float8 where the pages are, and quantized to 4 bits with a power of two for 32 channels where they are float4.  Tokens without a place (pos < 0, no page) are not stored.  There is no gradient: tensors
     that require one are refused where autograd records."""
     if stream is None:
         st = (_q._call or _q._native()).append(cache, k, v, seq, pos)
@@ -282,11 +299,38 @@ def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Te
         raise ValueError("k must be a tensor of three dimensions (tokens, heads, dim)")
     n = k.shape[0]
     _q._no_gradient("kv_append", k=k, v=v, **cache._values())
+    _q._on_current_device("kv_append", stream, k=k, v=v, seq=seq, pos=pos, table=cache.table, **cache._values())
     st = _q.lib().qwam_kv_append(ctypes.byref(c), n, _rows(k, "k", (n, c.heads, c.dim)), k.stride(0) if n > 1 else 0,
                                  _rows(v, "v", (n, c.heads, c.dim)), v.stride(0) if n > 1 else 0,
                                  _q._req(seq, "seq", torch.int32, (n,)), _q._req(pos, "pos", torch.int32, (n,)),
                                  _q._stream_ptr(stream))
     _q._check("qwam_kv_append", st)
+
+
+def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, stream=None):
+    """qwam_kv_read: the stored keys and values of positions pos[t] of sequences seq[t] (int32 [tokens]) as bf16
+    [tokens][heads][dim] each; zeros where kv_append would not store (pos < 0, no page).  `out` = (k, v) gives the outputs,
+    whose rows may be apart.  There is no gradient, as for kv_append."""
+    if stream is None:
+        done = (_q._call or _q._native()).read(cache, seq, pos, out)
+        if done is not None:
+            if type(done) is int:
+                _q._check("qwam_kv_read", done)
+            return done
+    c = cache.c_struct()
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 1:
+        raise ValueError("pos must be a tensor of one dimension (tokens)")
+    n = pos.shape[0]
+    ps, pp = _q._req(seq, "seq", torch.int32, (n,)), _q._req(pos, "pos", torch.int32, (n,))
+    _q._no_gradient("kv_read", **cache._values())
+    shape = (n, c.heads, c.dim)
+    k, v = (_q._empty(shape, torch.bfloat16, cache.k.device, stream) for _ in range(2)) if out is None else out
+    _q._no_gradient("kv_read", **{"out[0]": k, "out[1]": v})
+    _q._on_current_device("kv_read", stream, seq=seq, pos=pos, table=cache.table, **{"out[0]": k, "out[1]": v}, **cache._values())
+    st = _q.lib().qwam_kv_read(ctypes.byref(c), n, ps, pp, _rows(k, "out[0]", shape), k.stride(0) if n > 1 else 0,
+                               _rows(v, "out[1]", shape), v.stride(0) if n > 1 else 0, _q._stream_ptr(stream))
+    _q._check("qwam_kv_read", st)
+    return k, v
 
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *, starts: Optional[torch.Tensor] = None,
@@ -309,6 +353,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
     shape = (c.seqs, Hq, c.dim)
     pq = _rows(q, "q", shape)
     _q._no_gradient("paged_attention", q=q, **cache._values())
+    _q._on_current_device("paged_attention", stream, q=q, lengths=lengths, starts=starts, out=out, table=cache.table, **cache._values())
     if max_len is None:
         max_len = c.table_width * c.page_size
     need = _q._need("qwam_paged_attention", _q.lib().qwam_paged_attention_workspace(ctypes.byref(c), Hq, max_len))

@@ -409,15 +409,15 @@ qwam_status check_norm(const char* fn, const qwam_norm* p, qwam::NormParams* out
 // the cache's integers
 qwam_status check_cache_shape(const char* fn, const qwam_cache* c, qwam::CacheParams* out) {
   if (c == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: cache is NULL", fn);
-  if (c->type != QWAM_CACHE_BF16 && c->type != QWAM_CACHE_FP8)
-    return fail(QWAM_ERR_INVALID_ARG, "%s: type must be QWAM_CACHE_BF16 or QWAM_CACHE_FP8 (got %d)", fn, c->type);
-  const int32_t step = c->type == QWAM_CACHE_FP8 ? 16 : 8;
+  if (c->type != QWAM_CACHE_BF16 && c->type != QWAM_CACHE_FP8 && c->type != QWAM_CACHE_FP4)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: type must be QWAM_CACHE_BF16, QWAM_CACHE_FP8 or QWAM_CACHE_FP4 (got %d)", fn, c->type);
+  const int32_t step = c->type == QWAM_CACHE_BF16 ? 8 : 16, width = c->type == QWAM_CACHE_FP4 ? qwam::kFp4Group : step;
   if (c->pages <= 0 || c->heads <= 0 || c->seqs <= 0 || c->table_width <= 0)
     return fail(QWAM_ERR_INVALID_ARG, "%s: pages, heads, seqs and table_width must be >= 1", fn);
   if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0)
     return fail(QWAM_ERR_INVALID_ARG, "%s: page_size must be a power of two in [16, 4096] (got %d)", fn, c->page_size);
-  if (c->dim <= 0 || c->dim % step != 0)
-    return fail(QWAM_ERR_INVALID_ARG, "%s: dim must be a positive multiple of %d (got %d)", fn, step, c->dim);
+  if (c->dim <= 0 || c->dim % width != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: dim must be a positive multiple of %d (got %d)", fn, width, c->dim);
   if (c->dim > 256) return fail(QWAM_ERR_UNSUPPORTED, "%s: dim = %d exceeds 256", fn, c->dim);
   if (c->heads > 4096 || c->seqs > 65535)
     return fail(QWAM_ERR_UNSUPPORTED, "%s: at most 4096 heads and 65535 sequences", fn);
@@ -430,9 +430,18 @@ qwam_status check_cache_shape(const char* fn, const qwam_cache* c, qwam::CachePa
   if (c->row_stride <= -(1 << 26) || c->row_stride >= (1 << 26))
     return fail(QWAM_ERR_UNSUPPORTED, "%s: row_stride must be within 2^26", fn);
   *out = {c->pages, __builtin_ctz(static_cast<unsigned>(c->page_size)), c->heads, c->dim, c->seqs, c->table_width,
-          c->page_stride, c->head_stride, c->row_stride, c->k, c->v, c->k_scale, c->v_scale, c->table};
+          c->page_stride, c->head_stride, c->row_stride, c->k, c->v, nullptr, nullptr, c->table, nullptr, nullptr};
+  if (c->type == QWAM_CACHE_FP8) {
+    out->k_scale = static_cast<const float*>(c->k_scale);
+    out->v_scale = static_cast<const float*>(c->v_scale);
+  } else if (c->type == QWAM_CACHE_FP4) {
+    out->k_exp = static_cast<uint8_t*>(const_cast<void*>(c->k_scale));
+    out->v_exp = static_cast<uint8_t*>(const_cast<void*>(c->v_scale));
+  }
   return QWAM_OK;
 }
+
+qwam::CacheType type_of(const qwam_cache* c) { return static_cast<qwam::CacheType>(c->type); }
 
 qwam_status check_cache(const char* fn, const qwam_cache* c, qwam::CacheParams* out) {
   qwam_status s = check_cache_shape(fn, c, out);
@@ -443,8 +452,31 @@ qwam_status check_cache(const char* fn, const qwam_cache* c, qwam::CacheParams* 
   if (c->type == QWAM_CACHE_FP8) {
     QWAM_REQUIRE_ELEM(c->k_scale, 4);
     QWAM_REQUIRE_ELEM(c->v_scale, 4);
+  } else if (c->type == QWAM_CACHE_FP4) {
+    QWAM_REQUIRE_PTR(c->k_scale);
+    QWAM_REQUIRE_PTR(c->v_scale);
   }
   return QWAM_OK;
+}
+
+// the arguments that the calls on a list of tokens share
+qwam_status check_tokens(const char* fn, const qwam_cache* c, int32_t tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                         int64_t v_stride, const int32_t* seq, const int32_t* pos) {
+  if (tokens <= 0) return fail(QWAM_ERR_INVALID_ARG, "%s: tokens must be >= 1 (got %d)", fn, tokens);
+  if (static_cast<int64_t>(tokens) * c->heads * c->dim > (int64_t(1) << 32))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: tokens * heads * dim must be at most 2^32", fn);
+  QWAM_REQUIRE_PTR(k);
+  QWAM_REQUIRE_PTR(v);
+  if (k_stride % 8 != 0 || v_stride % 8 != 0)
+    return fail(QWAM_ERR_MISALIGNED, "%s: k_stride and v_stride must be multiples of 8", fn);
+  QWAM_REQUIRE_ELEM(seq, 4);
+  QWAM_REQUIRE_ELEM(pos, 4);
+  return QWAM_OK;
+}
+
+// whether the rows of an output lie apart from each other
+bool rows_apart(int32_t rows, int64_t stride, int64_t width) {
+  return rows <= 1 || stride >= width || stride <= -width;
 }
 
 qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::CacheParams& cp, int32_t q_heads, int32_t max_len) {
@@ -459,7 +491,7 @@ qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::Cac
   // the kernels count positions in 32 bits, up to a range past the last
   if (static_cast<int64_t>(max_len) + qwam::kMaxChunk > (int64_t(1) << 31))
     return fail(QWAM_ERR_UNSUPPORTED, "%s: max_len = %d exceeds 2^31 - %d", fn, max_len, qwam::kMaxChunk);
-  if (!qwam::paged_attention_fits(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len))
+  if (!qwam::paged_attention_fits(cp, type_of(c), q_heads, max_len))
     return fail(QWAM_ERR_UNSUPPORTED, "%s: too many sequences and heads of too long a max_len for one launch", fn);
   return QWAM_OK;
 }
@@ -561,18 +593,25 @@ qwam_status qwam_kv_append(const qwam_cache* c, int32_t tokens, const uint16_t* 
   qwam::CacheParams cp;
   qwam_status s = check_cache(fn, c, &cp);
   if (s != QWAM_OK) return s;
-  if (tokens <= 0) return fail(QWAM_ERR_INVALID_ARG, "%s: tokens must be >= 1 (got %d)", fn, tokens);
-  if (static_cast<int64_t>(tokens) * c->heads * c->dim > (int64_t(1) << 32))
-    return fail(QWAM_ERR_UNSUPPORTED, "%s: tokens * heads * dim must be at most 2^32", fn);
-  QWAM_REQUIRE_PTR(k);
-  QWAM_REQUIRE_PTR(v);
-  if (k_stride % 8 != 0 || v_stride % 8 != 0)
-    return fail(QWAM_ERR_MISALIGNED, "%s: k_stride and v_stride must be multiples of 8", fn);
-  QWAM_REQUIRE_ELEM(seq, 4);
-  QWAM_REQUIRE_ELEM(pos, 4);
+  if ((s = check_tokens(fn, c, tokens, k, k_stride, v, v_stride, seq, pos)) != QWAM_OK) return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;
-  return launched(fn, qwam::launch_kv_append(cp, c->type == QWAM_CACHE_FP8, tokens, k, k_stride, v, v_stride, seq, pos,
+  return launched(fn, qwam::launch_kv_append(cp, type_of(c), tokens, k, k_stride, v, v_stride, seq, pos,
                                              static_cast<hipStream_t>(stream)));
+}
+
+qwam_status qwam_kv_read(const qwam_cache* c, int32_t tokens, const int32_t* seq, const int32_t* pos, uint16_t* k, int64_t k_stride,
+                         uint16_t* v, int64_t v_stride, void* stream) {
+  const char* fn = "qwam_kv_read";
+  qwam::CacheParams cp;
+  qwam_status s = check_cache(fn, c, &cp);
+  if (s != QWAM_OK) return s;
+  if ((s = check_tokens(fn, c, tokens, k, k_stride, v, v_stride, seq, pos)) != QWAM_OK) return s;
+  const int64_t width = static_cast<int64_t>(c->heads) * c->dim;
+  if (!rows_apart(tokens, k_stride, width) || !rows_apart(tokens, v_stride, width))
+    return fail(QWAM_ERR_INVALID_ARG, "%s: k_stride and v_stride must be at least heads * dim apart", fn);
+  if ((s = check_device(fn)) != QWAM_OK) return s;
+  return launched(fn, qwam::launch_kv_read(cp, type_of(c), tokens, seq, pos, k, k_stride, v, v_stride,
+                                           static_cast<hipStream_t>(stream)));
 }
 
 int64_t qwam_paged_attention_workspace(const qwam_cache* c, int32_t q_heads, int32_t max_len) {
@@ -580,7 +619,7 @@ int64_t qwam_paged_attention_workspace(const qwam_cache* c, int32_t q_heads, int
   qwam::CacheParams cp;
   if (check_cache_shape(fn, c, &cp) != QWAM_OK || check_attention(fn, c, cp, q_heads, max_len) != QWAM_OK) return -1;
   ok();
-  return qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len);
+  return qwam::paged_attention_workspace_bytes(cp, type_of(c), q_heads, max_len);
 }
 
 qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uint16_t* q, int64_t q_stride,
@@ -597,13 +636,47 @@ qwam_status qwam_paged_attention(const qwam_cache* c, int32_t q_heads, const uin
   QWAM_REQUIRE_ELEM(lengths, 4);
   QWAM_OPTIONAL_ELEM(starts, 4);
   QWAM_REQUIRE_PTR(out);
-  const bool fp8 = c->type == QWAM_CACHE_FP8;
-  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, c->type == QWAM_CACHE_FP8, q_heads, max_len))) !=
+  if ((s = check_workspace(fn, workspace, workspace_bytes, qwam::paged_attention_workspace_bytes(cp, type_of(c), q_heads, max_len))) !=
       QWAM_OK)
     return s;
   if ((s = check_device(fn)) != QWAM_OK) return s;
-  return launched(fn, qwam::launch_paged_attention(cp, fp8, q_heads, q, q_stride, lengths, starts, max_len, scale, out, workspace,
+  return launched(fn, qwam::launch_paged_attention(cp, type_of(c), q_heads, q, q_stride, lengths, starts, max_len, scale, out, workspace,
                                                    static_cast<hipStream_t>(stream)));
+}
+
+qwam_status qwam_rope(const qwam_rope_plan* p, int32_t tokens, int32_t inverse, const void* x, int64_t x_stride, void* y,
+                      int64_t y_stride, void* stream) {
+  const char* fn = "qwam_rope";
+  if (p == nullptr) return fail(QWAM_ERR_INVALID_ARG, "%s: p is NULL", fn);
+  if (p->heads <= 0 || p->dim <= 0 || p->positions <= 0 || tokens <= 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: heads, dim, positions and tokens must be >= 1 (got %d, %d, %d, %d)", fn, p->heads, p->dim,
+                p->positions, tokens);
+  if (p->pairs <= 0 || p->pairs > p->dim / 2)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: pairs must be in [1, dim / 2] (got %d for dim = %d)", fn, p->pairs, p->dim);
+  if (p->axes <= 0 || p->axes > qwam::kRopeMaxAxes)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: axes must be in [1, %d] (got %d)", fn, qwam::kRopeMaxAxes, p->axes);
+  if (tokens % p->positions != 0)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: tokens must be a multiple of positions (got %d, %d)", fn, tokens, p->positions);
+  if (p->dim > qwam::kRopeMaxDim) return fail(QWAM_ERR_UNSUPPORTED, "%s: dim = %d exceeds %d", fn, p->dim, qwam::kRopeMaxDim);
+  // (in two steps: the product of the three passes 64 bits)
+  const int64_t width = static_cast<int64_t>(p->heads) * p->dim;
+  if (width > (int64_t(1) << 32) || width * tokens > (int64_t(1) << 32))
+    return fail(QWAM_ERR_UNSUPPORTED, "%s: tokens * heads * dim must be at most 2^32", fn);
+  const uintptr_t xe = p->x_f32 ? 4 : 2;
+  QWAM_REQUIRE_ELEM(p->pos, 4);
+  QWAM_REQUIRE_ELEM(p->inv_freq, 4);
+  QWAM_REQUIRE_ELEM(p->axis, 4);
+  QWAM_REQUIRE_ELEM(x, xe);
+  QWAM_REQUIRE_ELEM(y, xe);
+  if (!rows_apart(tokens, y_stride, width))
+    return fail(QWAM_ERR_INVALID_ARG, "%s: y_stride must be at least heads * dim apart", fn);
+  if (x == y && tokens > 1 && x_stride != y_stride)
+    return fail(QWAM_ERR_INVALID_ARG, "%s: y is x with another stride", fn);
+  qwam_status s = check_device(fn);
+  if (s != QWAM_OK) return s;
+  const qwam::RopeParams rp = {p->heads, p->dim, p->pairs, p->axes, p->positions, p->interleaved != 0, p->pos_f32 != 0, p->x_f32 != 0,
+                               p->pos, p->inv_freq, p->axis};
+  return launched(fn, qwam::launch_rope(rp, tokens, inverse != 0, x, x_stride, y, y_stride, static_cast<hipStream_t>(stream)));
 }
 
 const char* qwam_last_error(void) { return g_err; }

@@ -33,9 +33,9 @@
 // one of 4096 10.0 us, in a table that reaches 131072 17.0 (ranges go by the reach).  8 x 8 x G heads over 4096:
 // G = 16 31.6 us, 32 (two tiles of heads, each reading the pages) 49.5.  One of 77, 16 heads of 64, 3.9 us in a graph.
 #include <initializer_list>
+#include <type_traits>
 
-#include "qwam_device.h"
-#include "qwam_internal.h"
+#include "qwam_fp4.h"
 #include "qwam_mfma.h"
 
 namespace qwam {
@@ -136,12 +136,14 @@ __device__ __forceinline__ v8bf bf8(uint32_t a, uint32_t b, uint32_t c, uint32_t
 }  // namespace
 
 // DP: dim rounded up to 64, 128 or 256; FULL: dim == DP
-template <int DP, bool FP8, bool FULL>
-__global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void paged_attention_kernel(AttnArgs a) {
-  constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value
+template <int DP, CacheType TYPE, bool FULL>
+__global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 128 ? 4 : 1) void paged_attention_kernel(AttnArgs a) {
+  constexpr bool FP8 = TYPE == CacheType::kFp8, FP4 = TYPE == CacheType::kFp4;
+  constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value (fp4: rows and strides are in bytes)
+  constexpr int SB = FP4 ? 1 : EB;                // bytes that the cache's strides count
   constexpr int DC = DP / 16;                     // channels of V in a lane
-  constexpr int NK = DP * EB / 64;                // 16-byte pieces of K in a lane, per 16 keys
-  constexpr int NV = DC * EB / 4;                 // words of V in a lane, per key
+  constexpr int NK = FP4 ? (DP + 127) / 128 : DP * EB / 64;       // 16-byte pieces of K in a lane, per 16 keys
+  constexpr int NV = FP4 ? (DC + 7) / 8 : DC * EB / 4;            // words of V in a lane, per key
   constexpr int NF = DP / 32;                     // MFMA steps over the channels
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
@@ -176,7 +178,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
   }
 
   // q as the second operand of S^T: head r, channels of this quarter
-  auto channel = [&](int f) { return FP8 ? 64 * (f >> 1) + 16 * c + 8 * (f & 1) : 32 * f + 8 * c; };
+  auto channel = [&](int f) {
+    if constexpr (FP4) return DP == 64 ? 16 * c + 8 * f : 128 * (f >> 2) + 32 * c + 8 * (f & 3);
+    else return FP8 ? 64 * (f >> 1) + 16 * c + 8 * (f & 1) : 32 * f + 8 * c;
+  };
   v8bf qf[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f) {
@@ -188,21 +193,48 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
   const float ks = FP8 ? a.c.k_scale[h] : 1.0f;
   const float sscale = a.scale * ks * kLog2e;
 
-  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride * EB;
-  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride * EB;
-  const int row = static_cast<int>(a.c.row_stride) * EB;          // bytes; 16 rows stay below 2^31
+  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride * SB;
+  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride * SB;
+  const int row = static_cast<int>(a.c.row_stride) * SB;          // bytes; 16 rows stay below 2^31
   const int row_mask = (1 << a.c.page_bits) - 1;
   // bytes from the head's first row of page 0 to row 0 of 16 positions; a missing page reads page 0, unseen
   auto place = [&](int tile, int t, int& id) -> int64_t {
     id = __builtin_amdgcn_readlane(pid, 2 * tile + t);
     const int64_t page = id < 0 ? 0 : id;
-    return (page * a.c.page_stride + static_cast<int64_t>((start(tile) + 16 * t) & row_mask) * a.c.row_stride) * EB;
+    return (page * a.c.page_stride + static_cast<int64_t>((start(tile) + 16 * t) & row_mask) * a.c.row_stride) * SB;
+  };
+  // fp4: the exponents of a key's groups that its lane holds, and of the lane's channels of V for four keys each
+  uint32_t ke[2][NK], va_exp[2], vb_exp[2];
+  auto exponents_at = [&](int tile, int t) __attribute__((always_inline)) {
+    const int page = __builtin_amdgcn_readlane(pid, 2 * tile + t);
+    return (page < 0 ? 0 : page) * fp4_exp_page(a.c) + fp4_exp_group(a.c, h, 0) + ((start(tile) + 16 * t) & row_mask);
+  };
+  auto load_ke = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t* const e = a.c.k_exp + exponents_at(tile, t) + r;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const int g = DP == 64 ? c >> 1 : 4 * i + c;
+        ke[t][i] = 0;
+        if (FULL || g * kFp4Group < D) ke[t][i] = e[static_cast<int64_t>(g) << a.c.page_bits];
+      }
+    }
+  };
+  auto load_ve = [&](int tile, uint32_t (&ve)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int g = DC * r / kFp4Group;
+      ve[t] = 0;
+      if (FULL || DC * r < D)
+        ve[t] = *reinterpret_cast<const uint32_t*>(a.c.v_exp + exponents_at(tile, t) + 4 * c + (static_cast<int64_t>(g) << a.c.page_bits));
+    }
   };
 
   uint4 kr[2][NK];
   // heads of 64: V comes a tile ahead too (in wider ones its registers cost more waves than that gains: 4 ragged
   // contexts up to 16384, 16 heads of 64, 32.4 -> 27.6 us, one alone 17.0 -> 17.7; 16 up to 4096, 8 x 3 of 128, 18.0 -> 19.2)
-  constexpr bool V_AHEAD = DP == 64;
+  constexpr bool V_AHEAD = FP4 || DP == 64;
   uint32_t va[8][NV], vb[8][NV];
   int id[2], idn[2];
   int64_t at[2], atn[2];
@@ -211,18 +243,30 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const int ch = 64 / EB * i + 16 / EB * c;
         kr[t][i] = make_uint4(0, 0, 0, 0);
-        if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
+        if constexpr (FP4 && DP == 64) {
+          if (FULL || 16 * c < D) {
+            const uint2 w = *reinterpret_cast<const uint2*>(kbase + o[t] + (r * row + 8 * c));
+            kr[t][i].x = w.x;
+            kr[t][i].y = w.y;
+          }
+        } else if constexpr (FP4) {
+          if (FULL || 128 * i + 32 * c < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + 64 * i + 16 * c));
+        } else {
+          const int ch = 64 / EB * i + 16 / EB * c;
+          if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
+        }
       }
   };
   auto load_v = [&](const int64_t (&o)[2], uint32_t (&vr)[8][NV]) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + DC * r * EB);
+      const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + (FP4 ? DC * r / 2 : DC * r * EB));
 #pragma unroll
       for (int w = 0; w < NV; ++w) vr[j][w] = 0;
-      if constexpr (NV == 8) {
+      if constexpr (FP4 && DC == 4) {
+        if (FULL || DC * r < D) vr[j][0] = *reinterpret_cast<const uint16_t*>(src);
+      } else if constexpr (NV == 8) {
         if (FULL || DC * r < D) *reinterpret_cast<uint4*>(&vr[j][0]) = *reinterpret_cast<const uint4*>(src);
         if (FULL || DC * r + 8 < D) *reinterpret_cast<uint4*>(&vr[j][4]) = *reinterpret_cast<const uint4*>(src + 16);
       } else if (FULL || DC * r < D) {
@@ -242,9 +286,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 #pragma unroll
     for (int t = 0; t < 2; ++t) at[t] = place(0, t, id[t]);
     load_k(at);
+    if constexpr (FP4) load_ke(0);
     if constexpr (V_AHEAD) load_v(at, va);
+    if constexpr (FP4) load_ve(0, va_exp);
   }
-  auto turn = [&](int tile, uint32_t (&vr)[8][NV], uint32_t (&vn)[8][NV]) __attribute__((always_inline)) {
+  auto turn = [&](int tile, uint32_t (&vr)[8][NV], uint32_t (&vn)[8][NV], uint32_t (&ve)[2], uint32_t (&ven)[2]) __attribute__((always_inline)) {
     if constexpr (!V_AHEAD) load_v(at, vr);
     // scores of keys 16 t + 4 c + i, head r
     v4f s[2];
@@ -254,7 +300,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         v8bf k;
-        if constexpr (FP8) {
+        if constexpr (FP4) {
+          const uint4 p = kr[t][f >> 2];
+          const uint32_t w = (f & 3) == 0 ? p.x : (f & 3) == 1 ? p.y : (f & 3) == 2 ? p.z : p.w, e = ke[t][f >> 2] << 23;
+          k = bf8(fp4_pair(w, e, 0), fp4_pair(w, e, 1), fp4_pair(w, e, 2), fp4_pair(w, e, 3));
+        } else if constexpr (FP8) {
           const uint4 w = kr[t][f >> 1];
           const uint32_t x = f & 1 ? w.z : w.x, y = f & 1 ? w.w : w.y;
           k = bf8(fp8_pair<false>(x), fp8_pair<true>(x), fp8_pair<false>(y), fp8_pair<true>(y));
@@ -268,7 +318,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 #pragma unroll
       for (int t = 0; t < 2; ++t) atn[t] = place(tile + 1, t, idn[t]);
       load_k(atn);
+      if constexpr (FP4) load_ke(tile + 1);
       if constexpr (V_AHEAD) load_v(atn, vn);
+      if constexpr (FP4) load_ve(tile + 1, ven);
     }
     const int p0 = start(tile);
     const bool whole = p0 >= sp.first && p0 + 32 <= sp.len && id[0] >= 0 && id[1] >= 0;
@@ -311,6 +363,17 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 #pragma unroll
         for (int w = 0; w < NV; ++w)
           if (!(seen >> j & 1u)) vr[j][w] = 0;
+      if constexpr (FP4) {                        // (an exponent of 255 makes NaN of a code 0 too)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (!(seen >> j & 1u)) ve[j >> 2] &= ~(0xFFu << (8 * (j & 3)));
+      }
+    }
+    // the exponents at a float's place; the conversion does not look at its other bits
+    uint32_t vs8[8];
+    if constexpr (FP4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vs8[j] = (j & 3) == 3 ? ve[j >> 2] >> 1 : ve[j >> 2] << (23 - 8 * (j & 3));
     }
     // o^T += V^T S^T: channel DC r + e of the lane's eight keys
 #pragma unroll
@@ -318,7 +381,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
       uint32_t y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if constexpr (FP8) y[j] = w & 1 ? fp8_pair<true>(vr[j][w >> 1]) : fp8_pair<false>(vr[j][w >> 1]);
+        if constexpr (FP4) y[j] = fp4_pair(vr[j][w >> 2], vs8[j], w & 3);
+        else if constexpr (FP8) y[j] = w & 1 ? fp8_pair<true>(vr[j][w >> 1]) : fp8_pair<false>(vr[j][w >> 1]);
         else y[j] = vr[j][w];
       }
       const v8bf even = bf8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7]));
@@ -336,11 +400,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
   };
   if constexpr (V_AHEAD) {
     for (int tile = 0; tile < tiles; tile += 2) {
-      turn(tile, va, vb);
-      if (tile + 1 < tiles) turn(tile + 1, vb, va);
+      turn(tile, va, vb, va_exp, vb_exp);
+      if (tile + 1 < tiles) turn(tile + 1, vb, va, vb_exp, va_exp);
     }
   } else {
-    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vb);
+    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vb, va_exp, vb_exp);
   }
 
   // join the waves: one maximum, then sums of l and o through LDS
@@ -471,7 +535,8 @@ struct Plan {
 
 constexpr int kOneRange = 512;
 
-Plan plan_of(const CacheParams& c, bool fp8, int q_heads, int max_len) {
+Plan plan_of(const CacheParams& c, CacheType type, int q_heads, int max_len) {
+  const bool fp8 = type != CacheType::kBf16;
   auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
   const int64_t rows = rows_of(c, q_heads);
   // one range where a second launch would cost as much as the waves' turns (1.1 us for
@@ -490,18 +555,19 @@ Plan plan_of(const CacheParams& c, bool fp8, int q_heads, int max_len) {
   return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n)};
 }
 
-template <int DP, bool FP8>
+template <int DP, CacheType TYPE>
 hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
   const int nq = a.group < 16 ? a.group : 16;
   const dim3 grid(static_cast<unsigned>(rows_of(a.c, a.q_heads) * a.splits)), block(64 * kAttnWaves);
   const int bytes = (2 * kAttnWaves * 16 + kAttnWaves * nq * (DP + 4)) * 4;
-  auto kernel = a.c.dim == DP ? paged_attention_kernel<DP, FP8, true> : paged_attention_kernel<DP, FP8, false>;
+  auto kernel = a.c.dim == DP ? paged_attention_kernel<DP, TYPE, true> : paged_attention_kernel<DP, TYPE, false>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a);
   const unsigned heads = static_cast<unsigned>(a.c.seqs) * a.q_heads;
+  constexpr bool FP8 = TYPE == CacheType::kFp8;
   if (a.splits > 16)
     hipLaunchKernelGGL((attention_join_kernel<8, FP8>), dim3(heads, (a.c.dim + 31) / 32), dim3(256), 0, stream, a);
   else if (a.splits > 1)
@@ -511,37 +577,41 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+hipError_t launch_kv_append(const CacheParams& c, CacheType type, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream) {
+  if (type == CacheType::kFp4) return launch_kv_append_fp4(c, tokens, k, k_stride, v, v_stride, seq, pos, stream);
   const uint32_t n = static_cast<uint32_t>(static_cast<int64_t>(tokens) * c.heads * (c.dim / 8));
   const dim3 grid((n + 255) / 256), block(256);
-  if (fp8) hipLaunchKernelGGL((kv_append_kernel<true>), grid, block, 0, stream, c, n, k, k_stride, v, v_stride, seq, pos);
+  if (type == CacheType::kFp8) hipLaunchKernelGGL((kv_append_kernel<true>), grid, block, 0, stream, c, n, k, k_stride, v, v_stride, seq, pos);
   else hipLaunchKernelGGL((kv_append_kernel<false>), grid, block, 0, stream, c, n, k, k_stride, v, v_stride, seq, pos);
   return hipGetLastError();
 }
 
-bool paged_attention_fits(const CacheParams& c, bool fp8, int q_heads, int max_len) {
-  return rows_of(c, q_heads) * plan_of(c, fp8, q_heads, max_len).splits < (int64_t(1) << 23);
+bool paged_attention_fits(const CacheParams& c, CacheType type, int q_heads, int max_len) {
+  return rows_of(c, q_heads) * plan_of(c, type, q_heads, max_len).splits < (int64_t(1) << 23);
 }
 
-int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len) {
-  const int64_t splits = plan_of(c, fp8, q_heads, max_len).splits;
+int64_t paged_attention_workspace_bytes(const CacheParams& c, CacheType type, int q_heads, int max_len) {
+  const int64_t splits = plan_of(c, type, q_heads, max_len).splits;
   return splits <= 1 ? 0 : static_cast<int64_t>(c.seqs) * q_heads * splits * (c.dim + 2) * 4;
 }
 
-hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
+hipError_t launch_paged_attention(const CacheParams& c, CacheType type, int q_heads, const uint16_t* q, int64_t q_stride,
                                   const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
                                   void* workspace, hipStream_t stream) {
-  const Plan p = plan_of(c, fp8, q_heads, max_len);
+  const Plan p = plan_of(c, type, q_heads, max_len);
   float* const part = static_cast<float*>(workspace);
   const AttnArgs a = {c, q, q_stride, lengths, starts, out, part,
                       p.splits > 1 ? part + static_cast<int64_t>(c.seqs) * q_heads * p.splits * c.dim : nullptr,
                       q_heads, q_heads / c.heads, max_len, p.chunk, p.splits, scale};
-  if (fp8)
-    return c.dim <= 64 ? launch_attention<64, true>(a, stream) : c.dim <= 128 ? launch_attention<128, true>(a, stream)
-                                                                              : launch_attention<256, true>(a, stream);
-  return c.dim <= 64 ? launch_attention<64, false>(a, stream) : c.dim <= 128 ? launch_attention<128, false>(a, stream)
-                                                                             : launch_attention<256, false>(a, stream);
+  auto run = [&](auto tag) {
+    constexpr CacheType TYPE = decltype(tag)::value;
+    return c.dim <= 64 ? launch_attention<64, TYPE>(a, stream) : c.dim <= 128 ? launch_attention<128, TYPE>(a, stream)
+                                                                              : launch_attention<256, TYPE>(a, stream);
+  };
+  return type == CacheType::kFp4   ? run(std::integral_constant<CacheType, CacheType::kFp4>())
+         : type == CacheType::kFp8 ? run(std::integral_constant<CacheType, CacheType::kFp8>())
+                                   : run(std::integral_constant<CacheType, CacheType::kBf16>());
 }
 
 }  // namespace qwam

@@ -1,6 +1,7 @@
 // CPython module `_qwam_call`: the per-token calls of qwam.py (quantize_act,
 // quantize_act_deflated, asp_linear, asp_layer, asp_matvec) and block.py
-// (block_norm, block_norm_backward, kv_append, paged_attention) without ctypes.
+// (block_norm, block_norm_backward, kv_append, kv_read, paged_attention) and
+// rotary.py (rope) without ctypes.
 //
 // A few-token call runs for 5-10 us on the GPU; marshalling one through ctypes
 // took 14 us of Python (nine tensor checks of the layer, four or five of the
@@ -49,6 +50,8 @@ decltype(&qwam_block_norm_backward_workspace) g_norm_workspace;
 decltype(&qwam_kv_append) g_append;
 decltype(&qwam_paged_attention) g_attention;
 decltype(&qwam_paged_attention_workspace) g_attention_workspace;
+decltype(&qwam_kv_read) g_read;
+decltype(&qwam_rope) g_rope;
 
 enum Attr { kK, kN, kR, kGroup, kHadamard, kWq, kWs, kInv, kL1t, kL2t, kBias, kL1, kWsp, kL1f, kAttrs };
 const char* const kAttrNames[kAttrs] = {"K",   "N",   "r",    "group", "hadamard", "wq",  "ws",
@@ -58,6 +61,7 @@ PyObject *g_cuda_stream, *g_device_index;
 enum CacheAttr { kCacheK, kCacheV, kCacheTable, kCacheKScale, kCacheVScale, kCacheAttrs };
 const char* const kCacheAttrNames[kCacheAttrs] = {"k", "v", "table", "k_scale", "v_scale"};
 PyObject* g_cache_names[kCacheAttrs];
+PyObject *g_inv_freq, *g_axis, *g_interleaved;
 enum Grad { kDx, kDbranch, kDgate, kDpostWeight, kDweight, kDscale, kDshift, kGrads };
 const char* const kGradNames[kGrads] = {"dx", "dbranch", "dgate", "dpost_weight", "dweight", "dscale", "dshift"};
 PyObject* g_grad_names[kGrads];
@@ -315,6 +319,14 @@ const at::Tensor* tensor_of(PyObject* o) {
   return t.is_cuda() ? &t : nullptr;
 }
 
+// whether the kernels, which run on the current device, may take these (GPU tensors)
+bool on_current_device(std::initializer_list<const at::Tensor*> tensors) {
+  const auto now = c10::hip::current_device();
+  for (const at::Tensor* t : tensors)
+    if (t->get_device() != now) return false;
+  return true;
+}
+
 // the arguments that the norm's calls share, from `a`: norm ("rms" or "layer"), eps, residual_scale, gate, post_norm, post_weight,
 // weight, scale, shift
 constexpr int kNormArgs = 9;
@@ -452,16 +464,17 @@ struct Cache {
     if (k == nullptr || v == nullptr || t == nullptr || k->dim() != 4 || k->sizes() != v->sizes() || k->strides() != v->strides() ||
         k->scalar_type() != v->scalar_type() || k->stride(3) != 1 || t->dim() != 2)
       return false;
-    const bool fp8 = k->scalar_type() == at::kFloat8_e4m3fn;
-    if (!fp8 && k->scalar_type() != at::kBFloat16) return false;
+    const bool fp8 = k->scalar_type() == at::kFloat8_e4m3fn, fp4 = k->scalar_type() == at::ScalarType::Float4_e2m1fn_x2;
+    if ((!fp8 && !fp4 && k->scalar_type() != at::kBFloat16) || !on_current_device({k, v, t})) return false;
     for (int i = 0; i < 4; ++i)
       if (k->size(i) > INT32_MAX) return false;
     if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) return false;
     c.pages = static_cast<int32_t>(k->size(0));
     c.heads = static_cast<int32_t>(k->size(1));
     c.page_size = static_cast<int32_t>(k->size(2));
-    c.dim = static_cast<int32_t>(k->size(3));
-    c.type = fp8 ? QWAM_CACHE_FP8 : QWAM_CACHE_BF16;
+    if (fp4 && k->size(3) > INT32_MAX / 2) return false;
+    c.dim = static_cast<int32_t>(fp4 ? 2 * k->size(3) : k->size(3));
+    c.type = fp4 ? QWAM_CACHE_FP4 : fp8 ? QWAM_CACHE_FP8 : QWAM_CACHE_BF16;
     c.seqs = static_cast<int32_t>(t->size(0));
     c.table_width = static_cast<int32_t>(t->size(1));
     c.page_stride = k->stride(0);
@@ -472,11 +485,17 @@ struct Cache {
     void *table, *ks, *vs;
     if (!data_of(held[kCacheTable], at::kInt, {c.seqs, c.table_width}, &table)) return false;
     c.table = static_cast<const int32_t*>(table);
-    if (!fp8) return true;
-    if (!data_of(held[kCacheKScale], at::kFloat, {c.heads}, &ks) || !data_of(held[kCacheVScale], at::kFloat, {c.heads}, &vs))
+    if (!fp8 && !fp4) return true;
+    if (fp4) {
+      const std::initializer_list<int64_t> shape = {c.pages, c.heads, c.dim / 32, c.page_size};
+      constexpr auto type = at::ScalarType::Float8_e8m0fnu;
+      if (!data_of(held[kCacheKScale], type, shape, &ks) || !data_of(held[kCacheVScale], type, shape, &vs)) return false;
+    } else if (!data_of(held[kCacheKScale], at::kFloat, {c.heads}, &ks) || !data_of(held[kCacheVScale], at::kFloat, {c.heads}, &vs)) {
       return false;
-    c.k_scale = static_cast<const float*>(ks);
-    c.v_scale = static_cast<const float*>(vs);
+    }
+    if (!on_current_device({&THPVariable_Unpack(held[kCacheKScale]), &THPVariable_Unpack(held[kCacheVScale])})) return false;
+    c.k_scale = ks;
+    c.v_scale = vs;
     return true;
   }
   bool followed() const { return tracked({held[kCacheK], held[kCacheV], held[kCacheKScale], held[kCacheVScale]}); }
@@ -505,6 +524,7 @@ PyObject* py_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       !data_of(args[4], at::kInt, {n}, &pos))
     return none_or_error();
   if (C.followed() || tracked({args[1], args[2]})) Py_RETURN_NONE;
+  if (!on_current_device({k, v, &THPVariable_Unpack(args[3]), &THPVariable_Unpack(args[4])})) Py_RETURN_NONE;
   return PyLong_FromLong(g_append(&C.c, static_cast<int32_t>(n), static_cast<const uint16_t*>(k->data_ptr()), n > 1 ? k->stride(0) : 0,
                                   static_cast<const uint16_t*>(v->data_ptr()), n > 1 ? v->stride(0) : 0,
                                   static_cast<const int32_t*>(seq), static_cast<const int32_t*>(pos), current_stream()));
@@ -535,13 +555,16 @@ PyObject* py_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     max_len = PyLong_AsLongLong(args[5]);
   }
   if (PyErr_Occurred() || max_len < 1 || max_len > INT32_MAX) return none_or_error();
+  if (!on_current_device({q, &THPVariable_Unpack(args[2])}) || (starts != nullptr && !on_current_device({&THPVariable_Unpack(args[3])})))
+    Py_RETURN_NONE;
   Held o;
   if (args[6] == Py_None) {
     const at::Tensor t = at::empty({C.c.seqs, heads, C.c.dim}, q->options());
     po = t.data_ptr();
     o.o = THPVariable_Wrap(t);
   } else {
-    if (!data_of(args[6], at::kBFloat16, {C.c.seqs, heads, C.c.dim}, &po)) return none_or_error();
+    if (!data_of(args[6], at::kBFloat16, {C.c.seqs, heads, C.c.dim}, &po) || !on_current_device({&THPVariable_Unpack(args[6])}))
+      return none_or_error();
     o.o = Py_NewRef(args[6]);
   }
   const int64_t need = g_attention_workspace(&C.c, heads, static_cast<int32_t>(max_len));
@@ -556,6 +579,95 @@ PyObject* py_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// read(cache, seq, pos, out) -> (k, v); out may be None
+PyObject* py_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 4) Py_RETURN_NONE;
+  Cache C;
+  const at::Tensor* at_pos = tensor_of(args[2]);
+  if (at_pos == nullptr || at_pos->dim() != 1 || at_pos->size(0) > INT32_MAX || !C.load(args[0])) return none_or_error();
+  const int64_t n = at_pos->size(0);
+  void *seq, *pos;
+  if (!data_of(args[1], at::kInt, {n}, &seq) || !data_of(args[2], at::kInt, {n}, &pos) || C.followed() ||
+      !on_current_device({&THPVariable_Unpack(args[1]), at_pos}))
+    return none_or_error();
+  Held o[2];
+  const at::Tensor* t[2];
+  for (int i = 0; i < 2; ++i) {
+    if (args[3] == Py_None) {
+      o[i].o = THPVariable_Wrap(at::empty({n, C.c.heads, C.c.dim}, C.k->options().dtype(at::kBFloat16)));
+      if (o[i].o == nullptr) return nullptr;
+    } else {
+      if (!PyTuple_Check(args[3]) || PyTuple_GET_SIZE(args[3]) != 2) Py_RETURN_NONE;
+      o[i].o = Py_NewRef(PyTuple_GET_ITEM(args[3], i));
+    }
+    t[i] = rows3_of(o[i].o, n, C.c.heads, C.c.dim);
+    if (t[i] == nullptr || tracked(o[i].o) || !on_current_device({t[i]})) return none_or_error();
+  }
+  const qwam_status st = g_read(&C.c, static_cast<int32_t>(n), static_cast<const int32_t*>(seq), static_cast<const int32_t*>(pos),
+                                static_cast<uint16_t*>(t[0]->data_ptr()), n > 1 ? t[0]->stride(0) : 0,
+                                static_cast<uint16_t*>(t[1]->data_ptr()), n > 1 ? t[1]->stride(0) : 0, current_stream());
+  if (st != QWAM_OK) return PyLong_FromLong(st);
+  return PyTuple_Pack(2, o[0].o, o[1].o);
+  END_HANDLE_TH_ERRORS
+}
+
+// rope(x, positions, plan, inverse, out) -> y; None with an out that is not x (its overlap is looked at there) and where
+// autograd follows x
+PyObject* py_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 5 || !PyBool_Check(args[3]) || (args[4] != Py_None && args[4] != args[0])) Py_RETURN_NONE;
+  Held freq, axis, interleaved;
+  freq.o = PyObject_GetAttr(args[2], g_inv_freq);
+  axis.o = freq.o == nullptr ? nullptr : PyObject_GetAttr(args[2], g_axis);
+  interleaved.o = axis.o == nullptr ? nullptr : PyObject_GetAttr(args[2], g_interleaved);
+  if (interleaved.o == nullptr) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  const at::Tensor *x = tensor_of(args[0]), *pos = tensor_of(args[1]), *f = tensor_of(freq.o);
+  if (!PyBool_Check(interleaved.o) || x == nullptr || pos == nullptr || f == nullptr || x->dim() != 3 || pos->dim() != 2 || f->dim() != 1)
+    Py_RETURN_NONE;
+  for (int i = 0; i < 3; ++i)
+    if (x->size(i) > INT32_MAX) Py_RETURN_NONE;
+  if (pos->size(0) > INT32_MAX || pos->size(1) > INT32_MAX || f->size(0) > INT32_MAX) Py_RETURN_NONE;
+  qwam_rope_plan p = {};
+  p.heads = static_cast<int32_t>(x->size(1));
+  p.dim = static_cast<int32_t>(x->size(2));
+  p.pairs = static_cast<int32_t>(f->size(0));
+  p.interleaved = interleaved.o == Py_True;
+  p.positions = static_cast<int32_t>(pos->size(0));
+  p.axes = static_cast<int32_t>(pos->size(1));
+  p.pos_f32 = pos->scalar_type() == at::kFloat;
+  p.x_f32 = x->scalar_type() == at::kFloat;
+  if ((!p.x_f32 && x->scalar_type() != at::kBFloat16) || (!p.pos_f32 && pos->scalar_type() != at::kInt) || !pos->is_contiguous() ||
+      (x->size(2) > 1 && x->stride(2) != 1) || (x->size(1) > 1 && x->stride(1) != x->size(2)))
+    Py_RETURN_NONE;
+  void *fp, *ap;
+  if (!data_of(freq.o, at::kFloat, {p.pairs}, &fp) || !data_of(axis.o, at::kInt, {p.pairs}, &ap)) return none_or_error();
+  if (!on_current_device({x, pos, f, &THPVariable_Unpack(axis.o)}) || tracked({args[0], args[1], freq.o})) Py_RETURN_NONE;
+  p.pos = pos->data_ptr();
+  p.inv_freq = static_cast<const float*>(fp);
+  p.axis = static_cast<const int32_t*>(ap);
+  const int64_t T = x->size(0), stride = T > 1 ? x->stride(0) : 0;
+  Held y;
+  void* py = x->data_ptr();
+  int64_t y_stride = stride;
+  if (args[4] == Py_None) {
+    const at::Tensor t = at::empty(x->sizes(), x->options());
+    py = t.data_ptr();
+    y_stride = T > 1 ? t.stride(0) : 0;
+    y.o = THPVariable_Wrap(t);
+    if (y.o == nullptr) return nullptr;
+  } else {
+    y.o = Py_NewRef(args[4]);
+  }
+  const qwam_status st = g_rope(&p, static_cast<int32_t>(T), args[3] == Py_True, x->data_ptr(), stride, py, y_stride, current_stream());
+  if (st != QWAM_OK) return PyLong_FromLong(st);
+  return y.release();
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(the addresses of the library's entry points, in the order below)
 PyObject* py_bind(PyObject*, PyObject* args) {
   void** const to[] = {reinterpret_cast<void**>(&g_quantize), reinterpret_cast<void**>(&g_workspace),
@@ -563,7 +675,8 @@ PyObject* py_bind(PyObject*, PyObject* args) {
                        reinterpret_cast<void**>(&g_matvec),   reinterpret_cast<void**>(&g_matvec_workspace),
                        reinterpret_cast<void**>(&g_norm),     reinterpret_cast<void**>(&g_norm_bwd),
                        reinterpret_cast<void**>(&g_norm_workspace), reinterpret_cast<void**>(&g_append),
-                       reinterpret_cast<void**>(&g_attention), reinterpret_cast<void**>(&g_attention_workspace)};
+                       reinterpret_cast<void**>(&g_attention), reinterpret_cast<void**>(&g_attention_workspace),
+                       reinterpret_cast<void**>(&g_read), reinterpret_cast<void**>(&g_rope)};
   constexpr Py_ssize_t n = sizeof(to) / sizeof(to[0]);
   if (PyTuple_GET_SIZE(args) != n) {
     PyErr_Format(PyExc_TypeError, "bind takes %zd addresses", n);
@@ -588,6 +701,8 @@ PyMethodDef methods[] = {
     {"norm_backward", reinterpret_cast<PyCFunction>(py_norm_bwd), METH_FASTCALL, nullptr},
     {"append", reinterpret_cast<PyCFunction>(py_append), METH_FASTCALL, nullptr},
     {"attention", reinterpret_cast<PyCFunction>(py_attention), METH_FASTCALL, nullptr},
+    {"read", reinterpret_cast<PyCFunction>(py_read), METH_FASTCALL, nullptr},
+    {"rope", reinterpret_cast<PyCFunction>(py_rope), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qwam_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -601,6 +716,9 @@ PyMODINIT_FUNC PyInit__qwam_call() {
     if ((g_cache_names[a] = PyUnicode_InternFromString(kCacheAttrNames[a])) == nullptr) return nullptr;
   for (int a = 0; a < kGrads; ++a)
     if ((g_grad_names[a] = PyUnicode_InternFromString(kGradNames[a])) == nullptr) return nullptr;
+  if ((g_inv_freq = PyUnicode_InternFromString("inv_freq")) == nullptr || (g_axis = PyUnicode_InternFromString("axis")) == nullptr ||
+      (g_interleaved = PyUnicode_InternFromString("interleaved")) == nullptr)
+    return nullptr;
   if ((g_cuda_stream = PyUnicode_InternFromString("cuda_stream")) == nullptr ||
       (g_device_index = PyUnicode_InternFromString("device_index")) == nullptr)
     return nullptr;

@@ -132,22 +132,42 @@ hipError_t launch_block_norm_bwd(const NormParams& p, int T, const void* dxo, co
                                  const uint16_t* branch, void* dx, uint16_t* dbranch, float* dgate, float* dscale, float* dshift,
                                  float* dpost_weight, float* dweight, void* workspace, hipStream_t stream);
 
-// qwam_cache as the kernels take it: pages of 1 << page_bits rows
+// qwam_cache as the kernels take it: pages of 1 << page_bits rows; k_scale and v_scale of fp8, k_exp and v_exp of fp4
+enum class CacheType { kBf16 = 0, kFp8 = 1, kFp4 = 4 };
+constexpr int kFp4Group = 32;          // channels of a scale
 struct CacheParams {
   int pages, page_bits, heads, dim, seqs, table_width;
   int64_t page_stride, head_stride, row_stride;
   void *k, *v;
   const float *k_scale, *v_scale;
   const int32_t* table;
+  uint8_t *k_exp, *v_exp;
 };
 constexpr int kMaxHeadGroup = 64;      // query heads per key head
 constexpr int kMaxChunk = 4096;        // positions of a workgroup of the attention, the pages of 16 in each lane
-hipError_t launch_kv_append(const CacheParams& c, bool fp8, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+hipError_t launch_kv_append(const CacheParams& c, CacheType type, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                             int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream);
-bool paged_attention_fits(const CacheParams& c, bool fp8, int q_heads, int max_len);      // one launch's workgroups
-int64_t paged_attention_workspace_bytes(const CacheParams& c, bool fp8, int q_heads, int max_len);
-hipError_t launch_paged_attention(const CacheParams& c, bool fp8, int q_heads, const uint16_t* q, int64_t q_stride,
+hipError_t launch_kv_append_fp4(const CacheParams& c, int tokens, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                                int64_t v_stride, const int32_t* seq, const int32_t* pos, hipStream_t stream);
+hipError_t launch_kv_read(const CacheParams& c, CacheType type, int tokens, const int32_t* seq, const int32_t* pos, uint16_t* k,
+                          int64_t k_stride, uint16_t* v, int64_t v_stride, hipStream_t stream);
+bool paged_attention_fits(const CacheParams& c, CacheType type, int q_heads, int max_len);      // one launch's workgroups
+int64_t paged_attention_workspace_bytes(const CacheParams& c, CacheType type, int q_heads, int max_len);
+hipError_t launch_paged_attention(const CacheParams& c, CacheType type, int q_heads, const uint16_t* q, int64_t q_stride,
                                   const int32_t* lengths, const int32_t* starts, int max_len, float scale, uint16_t* out,
                                   void* workspace, hipStream_t stream);
+
+constexpr int kRopeMaxAxes = 4, kRopeMaxDim = 4096;
+
+// qwam_rope_plan as the kernels take it
+struct RopeParams {
+  int heads, dim, pairs, axes, positions;
+  bool interleaved, pos_f32, x_f32;
+  const void* pos;
+  const float* inv_freq;
+  const int32_t* axis;
+};
+hipError_t launch_rope(const RopeParams& p, int tokens, bool inverse, const void* x, int64_t x_stride, void* y, int64_t y_stride,
+                       hipStream_t stream);
 
 }  // namespace qwam

@@ -6,7 +6,7 @@ raw device pointers plus the current HIP stream across the C ABI.  If the
 library is not built, every call raises: there is no fallback.
 
 The per-token calls (quantize_act, quantize_act_deflated, asp_linear,
-asp_layer, asp_matvec and those of block.py) marshal natively
+asp_layer, asp_matvec and those of block.py and rotary.py) marshal natively
 (csrc/qwam_binding.cpp); what that path does not take (for all but the
 activation calls an explicit stream, for all of them an argument that fails a check) goes through ctypes here, which raises for the
 argument that is wrong.
@@ -14,7 +14,7 @@ argument that is wrong.
 Names follow the C ABI (include/qwam.h): pack_weights, quantize_act,
 quantize_act_deflated (both over qwam_quantize_act_ws), asp_linear, asp_layer, debug_group_partials,
 asp_matvec, aog_accumulate, aog_protected_basis; block.py holds the norms around a block and
-the paged key-value cache; and the measurement probes of include/qwam_probe.h:
+the paged key-value cache, rotary.py the rotary positions; and the measurement probes of include/qwam_probe.h:
 probe_mfma, probe_valu_fma, probe_copy, probe_empty, probe_gemm_form.
 """
 
@@ -60,9 +60,15 @@ class QwamCacheC(ctypes.Structure):
                 ("v_scale", _c_void_p), ("table", _c_void_p)]
 
 
+class QwamRopePlanC(ctypes.Structure):
+    _fields_ = [("heads", _i32), ("dim", _i32), ("pairs", _i32), ("interleaved", _i32), ("axes", _i32), ("positions", _i32),
+                ("pos_f32", _i32), ("x_f32", _i32), ("pos", _c_void_p), ("inv_freq", _c_void_p), ("axis", _c_void_p)]
+
+
 _LP = ctypes.POINTER(QwamLayerC)
 _NP = ctypes.POINTER(QwamNormC)
 _CP = ctypes.POINTER(QwamCacheC)
+_RP = ctypes.POINTER(QwamRopePlanC)
 SIGNATURES = {
     "qwam_pack_weights": (ctypes.c_int, [_i32, _i32, _i32, _c_void_p, _c_void_p, _c_void_p,
                                          _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
@@ -85,6 +91,8 @@ SIGNATURES = {
     "qwam_block_norm_backward_workspace": (ctypes.c_int64, [_NP]),
     "qwam_kv_append": (ctypes.c_int, [_CP, _i32, _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64, _c_void_p, _c_void_p,
                                       _c_void_p]),
+    "qwam_kv_read": (ctypes.c_int, [_CP, _i32, _c_void_p, _c_void_p, _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64, _c_void_p]),
+    "qwam_rope": (ctypes.c_int, [_RP, _i32, _i32, _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64, _c_void_p]),
     "qwam_paged_attention": (ctypes.c_int, [_CP, _i32, _c_void_p, ctypes.c_int64, _c_void_p, _c_void_p, _i32, ctypes.c_float,
                                             _c_void_p, _c_void_p, ctypes.c_int64, _c_void_p]),
     "qwam_paged_attention_workspace": (ctypes.c_int64, [_CP, _i32, _i32]),
@@ -144,7 +152,7 @@ def _native():
                    for f in ("qwam_quantize_act_ws", "qwam_quantize_act_workspace", "qwam_asp_linear", "qwam_asp_layer", "qwam_asp_matvec",
                              "qwam_asp_matvec_workspace", "qwam_block_norm", "qwam_block_norm_backward",
                              "qwam_block_norm_backward_workspace", "qwam_kv_append", "qwam_paged_attention",
-                             "qwam_paged_attention_workspace")))
+                             "qwam_paged_attention_workspace", "qwam_kv_read", "qwam_rope")))
         _call = mod
     return _call
 
@@ -381,6 +389,16 @@ def _need(fn: str, nbytes: int) -> int:
     if nbytes < 0:
         raise QwamError(fn, 2, lib().qwam_last_error().decode())
     return int(nbytes)
+
+
+def _on_current_device(fn: str, stream, **tensors) -> None:
+    """For a call whose kernels run on the current device: refuses tensors and streams of another."""
+    now = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.device.type == "cuda" and t.device.index != now:
+            raise ValueError(f"{name} is on {t.device}, {fn} runs on the current device cuda:{now}")
+    if isinstance(stream, torch.cuda.Stream) and stream.device.index != now:
+        raise ValueError(f"stream is of {stream.device}, {fn} runs on the current device cuda:{now}")
 
 
 def _tangent(t: Optional[torch.Tensor]) -> bool:

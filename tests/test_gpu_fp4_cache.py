@@ -1,0 +1,518 @@
+"""The 4-bit key-value cache on the GPU: kv_append's codes and scales against the definition bit for bit, kv_read's values
+exactly, paged_attention against float64 with the bound of the bf16 cache (every stored value is a bf16 value, so a bf16
+cache that holds them is the reference's)."""
+
+import types
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_33269_amd as P
+from paper_2609_33269_amd import qwam as Q
+from test_gpu_paged_attention import EDGES, FP8, _check, _q
+from test_gpu_paged_attention import _cache as _wide
+
+pytestmark = pytest.mark.gpu
+
+FP4, E8M0 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    Q.lib()
+
+
+# ---- the format, from its definition ----
+
+def _quantize(x):
+    """float64 [..][dim] -> codes uint8 [..][dim] and exponent bytes uint8 [..][dim / 32]."""
+    v = x.numpy().reshape(*x.shape[:-1], -1, 32)
+    top = np.abs(v).max(-1)
+    e = np.full(top.shape, -123)
+    for i in range(-122, 126):
+        e = np.where(top > 7 * 2.0 ** (i - 1), i, e)
+    with np.errstate(invalid="ignore"):
+        a = np.abs(v) * 2.0 ** -e[..., None].astype(np.float64)
+        near = np.abs(a[..., None] - GRID)
+        near[..., 1::2] += 2.0 ** -40                       # of two as near, the even code
+    near = np.where(np.isnan(near), 0.0, near)
+    code = near.argmin(-1) + 8 * np.signbit(v)
+    byte = np.where(np.isfinite(top), e + 127, 255)
+    return torch.from_numpy(code.reshape(x.shape).astype(np.uint8)), torch.from_numpy(byte.astype(np.uint8))
+
+
+def _pack(code):
+    return code[..., ::2] | code[..., 1::2] << 4
+
+
+def _values(codes, scales):
+    """Stored codes [pages][heads][page][dim / 2] and scales [pages][heads][dim / 32][page] -> float64 [pages][heads][page][dim]."""
+    c, e = codes.contiguous().view(torch.uint8).cpu().numpy(), scales.view(torch.uint8).cpu().numpy()
+    full = np.stack((c & 15, c >> 4), -1).reshape(*c.shape[:-1], -1)
+    v = np.where(full & 8, -1.0, 1.0) * GRID[full & 7]
+    s = np.where(e == 255, NAN, 2.0 ** (e.astype(np.float64) - 127)).swapaxes(2, 3).repeat(32, -1)
+    return torch.from_numpy(v * s)
+
+
+def _cache(lengths, H, D, page=16, seed=0, layout="heads", width=None, junk=255, device="cuda"):
+    """Random codes and scales up to `lengths`; everywhere else any codes and the scale `junk`."""
+    g = torch.Generator().manual_seed(seed)
+    used = [-(-max(n, 0) // page) for n in lengths]
+    width = max([1] + used) if width is None else width
+    total = sum(used) + 2
+    order = torch.randperm(total, generator=g)
+    table = torch.full((len(lengths), width), -1, dtype=torch.int32)
+    written = torch.zeros(total, page, dtype=torch.bool)
+    at = 0
+    for b, n in enumerate(lengths):
+        table[b, :used[b]] = order[at:at + used[b]].to(torch.int32)
+        for i in range(used[b]):
+            written[order[at + i], :min(page, n - i * page)] = True
+        at += used[b]
+    kv = torch.randint(0, 256, (2, total, H, page, D // 2), generator=g, dtype=torch.uint8).to(device)
+    if layout == "rows":                    # pages that hold their rows first
+        kv = kv.transpose(2, 3).contiguous().transpose(2, 3)
+    k, v = kv[0], kv[1]
+    if layout == "both":                    # pages that hold their keys, then their values
+        kv = kv.transpose(0, 1).contiguous()
+        k, v = kv[:, 0], kv[:, 1]
+    s = torch.randint(122, 127, (2, total, H, D // 32, page), generator=g, dtype=torch.uint8)
+    s = torch.where(written[None, :, None, None], s, torch.tensor(junk, dtype=torch.uint8)).to(device)
+    return P.PagedCache(k.view(FP4), v.view(FP4), table.to(device), s[0].view(E8M0), s[1].view(E8M0))
+
+
+def _as_bf16(cache):
+    """The same keys and values in bf16 pages."""
+    def wide(c, s):
+        v = _values(c, s)
+        b = v.bfloat16()
+        assert torch.equal(b.double().nan_to_num(7.0), v.nan_to_num(7.0))
+        return b.cuda()
+    return P.PagedCache(wide(cache.k, cache.k_scale), wide(cache.v, cache.v_scale), cache.table)
+
+
+def _int(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _run(lengths, H, G, D, page=16, seed=0, starts=None, max_len=None, scale=None, least=0.0, **kw):
+    cache = _cache(lengths, H, D, page, seed=seed, **kw)
+    q = _q(len(lengths), H * G, D, seed + 1)
+    out = P.paged_attention(cache, q, _int(lengths), starts=None if starts is None else _int(starts), max_len=max_len, scale=scale)
+    return _check(_as_bf16(cache), q, lengths, out, starts, scale=scale, max_len=max_len, least=least)
+
+
+# ---- attention ----
+
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_lengths(D, page):
+    _run(EDGES, 2, 3, D, page)
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_head_widths(D):
+    _run([1, 5, 16, 40, 100, 300, 0, 700], 3, 2, D, 32, seed=D)
+    _run([3000], 1, 5, D, 16, seed=D)
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 8, 15, 16, 17, 31, 32, 33, 64])
+@pytest.mark.parametrize("H", [1, 3])
+def test_head_groups(H, G):
+    _run([3, 77, 260, 0, 530], H, G, 64, 16, seed=G)
+    _run([3, 77, 260, 0, 530], H, G, 128, 16, seed=G)
+
+
+@pytest.mark.parametrize("layout", ["heads", "rows", "both"])
+def test_layouts(layout):
+    for H, G, D, page in ((4, 4, 128, 64), (4, 1, 96, 16), (2, 2, 256, 32), (3, 1, 32, 16)):
+        _run([1, 17, 64, 200, 999], H, G, D, page, layout=layout)
+
+
+@pytest.mark.parametrize("B,H,L", [(1, 1, 5000), (1, 8, 20000), (2, 1, 70001), (40, 2, 2000), (1, 16, 77), (1, 1, 131072)])
+def test_long_and_ragged(B, H, L):
+    g = torch.Generator().manual_seed(L)
+    _run([L] + [int(torch.randint(0, L, (1,), generator=g)) for _ in range(B - 1)], H, 3, 128, 64)
+
+
+@pytest.mark.parametrize("junk", [0, 1, 200, 252, 255])
+def test_unwritten_slots(junk):
+    for D in (64, 128, 256):
+        _run([1, 16, 31, 100, 0, 517], 2, 2, D, 64, junk=junk)
+
+
+def test_starts():
+    lengths = [100, 100, 100, 100, 100, 1000, 1000, 1000, 0, 5]
+    starts = [0, 1, 99, 100, 250, 17, 512, 999, 3, -7]
+    for D in (64, 128, 256):
+        _run(lengths, 2, 4, D, 16, starts=starts)
+    # what lies before a start has no effect, whatever it holds
+    cache = _cache(lengths, 2, 128, 16)
+    q, L, S = _q(len(lengths), 8, 128), _int(lengths), _int(starts)
+    a = P.paged_attention(cache, q, L, starts=S)
+    for b, s in enumerate(starts):
+        for p in range(0, min(s, lengths[b])):
+            for c in (cache.k_scale, cache.v_scale):
+                c.view(torch.uint8)[int(cache.table[b, p // 16]), :, :, p % 16] = 255
+    assert torch.equal(a, P.paged_attention(cache, q, L, starts=S))
+
+
+def test_missing_pages_and_limits():
+    lengths = [200, 200, 64, 200, 5000, -3]
+    cache = _cache([200, 200, 64, 200, 200, 16], 2, 64, 16, width=13, junk=120)
+    cache.table[0, 3] = -1
+    cache.table[1, 0] = cache.k.shape[0]
+    cache.table[1, 12] = 2 ** 31 - 1
+    cache.table[2, :] = -2 ** 31
+    cache.table[3, 4:9] = 10 ** 6
+    q, L, ref = _q(6, 6, 64), _int(lengths), _as_bf16(cache)
+    _check(ref, q, lengths, P.paged_attention(cache, q, L))
+    for n in (1, 16, 50, 129, 208):
+        _check(ref, q, lengths, P.paged_attention(cache, q, L, max_len=n), max_len=n)
+
+
+def test_scales_of_every_size():
+    """Exponents over a wide range, one large, and the smallest that is written, where a result may fall below the normal
+    numbers (2^-126) and is taken as 0 or in their steps."""
+    lengths = [600]
+    cache = _cache(lengths, 2, 128, 16)
+    e = torch.randint(60, 150, cache.k_scale.shape, generator=torch.Generator().manual_seed(1), dtype=torch.uint8).cuda()
+    cache.k_scale = torch.full_like(e, 100).view(E8M0)
+    cache.v_scale = e.view(E8M0)
+    q = _q(1, 4, 128)
+    _check(_as_bf16(cache), q, lengths, P.paged_attention(cache, q, _int(lengths)))
+    for byte in (4, 240):
+        cache.v_scale = torch.full_like(e, byte).view(E8M0)
+        _check(_as_bf16(cache), q, lengths, P.paged_attention(cache, q, _int(lengths)), least=2.0 ** -126)
+
+
+def test_extreme_scores():
+    """A value of the leading key may be exactly 0, and what the others add to its channel be of any size: a weight below
+    2^-126 of the largest, which is 1 before the sums' division, is below float32's normal numbers and may count as 0.  There
+    are at most 700, of values of at most 6 / 2: 700 * 3 * 2^-126 < 2^-114 of a result is not held to the bound."""
+    lengths = [700, 700, 300, 40]
+    for D in (64, 128, 256):
+        _run(lengths, 2, 2, D, 16, scale=4.0, least=2.0 ** -114)
+        _run(lengths, 2, 2, D, 16, scale=-4.0, least=2.0 ** -114)
+        _run(lengths, 2, 2, D, 16, scale=0.0)
+
+
+@pytest.mark.parametrize("length", [40, 5000])
+def test_nan_groups(length):
+    """A group without a value (scale byte 255): in a key it makes its head's results NaN, in a value its channels'."""
+    cache = _cache([length] * 2, 2, 128, 64)
+    q, L = _q(2, 6, 128), _int([length] * 2)
+    want = P.paged_attention(cache, q, L)
+    page = int(cache.table[1, 0])
+    cache.v_scale.view(torch.uint8)[page, 1, 2, 5] = 255
+    got = P.paged_attention(cache, q, L)
+    assert got[1, 3:, 64:96].isnan().all()
+    got[1, 3:, 64:96] = want[1, 3:, 64:96]
+    assert torch.equal(got, want)
+    cache.v_scale.view(torch.uint8)[page, 1, 2, 5] = 125
+    want = P.paged_attention(cache, q, L)
+    cache.k_scale.view(torch.uint8)[page, 0, 3, 5] = 255
+    got = P.paged_attention(cache, q, L)
+    assert got[1, :3].isnan().all()
+    got[1, :3] = want[1, :3]
+    assert torch.equal(got, want)
+
+
+def test_query_slices_streams_and_out():
+    lengths = [300, 20, 77]
+    cache = _cache(lengths, 2, 64, 32)
+    wide = torch.randn(3, 10 * 64, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    q = wide[:, 64:64 + 8 * 64].view(3, 8, 64)
+    a = P.paged_attention(cache, q, _int(lengths))
+    _check(_as_bf16(cache), q, lengths, a)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b = P.paged_attention(cache, q, _int(lengths), stream=s)
+    s.synchronize()
+    out = torch.full_like(a, NAN)
+    assert P.paged_attention(cache, q, _int(lengths), out=out) is out
+    assert torch.equal(a, b) and torch.equal(a, out)
+    assert all(torch.equal(a, P.paged_attention(cache, q, _int(lengths))) for _ in range(3))
+
+
+def test_offsets_past_32_bits():
+    """Codes' pages more than 2^32 bytes apart, and scales of pages past 2^32 bytes (their codes share one place)."""
+    H, D, page, lengths = 2, 128, 16, [40, 100]
+    small = _cache(lengths, H, D, page)
+    n = small.k.shape[0]
+    stride = 2 ** 32 // (n - 1) // 16 * 16 + 16 * H * page * D
+    k, v = (torch.empty((n - 1) * stride + H * page * D // 2, dtype=torch.uint8, device="cuda")
+            .as_strided((n, H, page, D // 2), (stride, page * D // 2, D // 2, 1)) for _ in range(2))
+    k.copy_(small.k.view(torch.uint8))
+    v.copy_(small.v.view(torch.uint8))
+    far = P.PagedCache(k.view(FP4), v.view(FP4), small.table, small.k_scale.clone(), small.v_scale.clone())
+    q, L = _q(2, 6, D), _int(lengths)
+    x = torch.randn(2, 2, H, D, generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    for c in (far, small):
+        P.kv_append(c, x[0], x[1], _int([0, 1]), _int([39, 99]))
+    assert torch.equal(P.paged_attention(far, q, L), P.paged_attention(small, q, L))
+    at = _int([0, 0, 1, 1]), _int([39, 3, 99, 50])
+    assert all(torch.equal(a, b) for a, b in zip(P.kv_read(far, *at), P.kv_read(small, *at)))
+    del k, v, far
+    torch.cuda.empty_cache()
+    pages, page, D = 2 ** 20 + 3, 4096, 32
+    codes = torch.randint(0, 256, (2, page, D // 2), generator=torch.Generator().manual_seed(5), dtype=torch.uint8).cuda()
+    k, v = (c.as_strided((pages, 1, page, D // 2), (0, 0, D // 2, 1)) for c in codes)
+    scales = torch.zeros(pages, 1, 1, page, dtype=torch.uint8, device="cuda")
+    scales[pages - 1] = torch.randint(120, 126, (page,), generator=torch.Generator().manual_seed(6), dtype=torch.uint8).cuda()
+    far = P.PagedCache(k.view(FP4), v.view(FP4), _int([[pages - 1]]), scales.view(E8M0), scales.view(E8M0))
+    near = P.PagedCache(k[:1].view(FP4), v[:1].view(FP4), _int([[0]]), scales[-1:].clone().view(E8M0), scales[-1:].clone().view(E8M0))
+    q, L = _q(1, 2, D), _int([4000])
+    assert torch.equal(P.paged_attention(far, q, L), P.paged_attention(near, q, L))
+    at = _int([0] * 3), _int([0, 1, 4095])
+    assert all(torch.equal(a, b) for a, b in zip(P.kv_read(far, *at), P.kv_read(near, *at)))
+    x = torch.randn(1, 1, D, generator=torch.Generator().manual_seed(7)).bfloat16().cuda()
+    near.k, near.v = k[:1].clone().contiguous(), v[:1].clone().contiguous()
+    near.k, near.v = near.k.view(FP4), near.v.view(FP4)
+    near.v_scale = near.k_scale
+    for c in (far, near):
+        P.kv_append(c, x, x, _int([0]), _int([17]))
+    assert all(torch.equal(a, b) for a, b in zip(P.kv_read(far, _int([0]), _int([17])), P.kv_read(near, _int([0]), _int([17]))))
+    del far, scales
+    torch.cuda.empty_cache()
+
+
+# ---- append ----
+
+@pytest.mark.parametrize("layout", ["heads", "rows", "both"])
+@pytest.mark.parametrize("H,D,page", [(1, 32, 16), (3, 96, 32), (8, 128, 64), (2, 256, 256)])
+def test_append(H, D, page, layout):
+    lengths = [0, 5, 77, 300]
+    cache = _cache([n + 40 for n in lengths], H, D, page, layout=layout)
+    g = torch.Generator().manual_seed(D)
+    seq = torch.tensor([b for b in range(4) for _ in range(37)], dtype=torch.int32)
+    pos = torch.tensor([n + i for n in lengths for i in range(37)], dtype=torch.int32)
+    perm = torch.randperm(len(seq), generator=g)
+    seq, pos = seq[perm], pos[perm]
+    seq[3], pos[7], pos[11], seq[13], pos[17] = -1, -1, 10 ** 6, 4, -2 ** 31             # tokens without a place
+    cache.table[1, (5 + 3) // page] = -1
+    wide = (torch.randn(len(seq), 3 * H * D, generator=g) * torch.exp(3 * torch.randn(len(seq), 1, generator=g))).bfloat16().cuda()
+    k, v = (wide[:, i * H * D:(i + 1) * H * D].view(-1, H, D) for i in (1, 2))
+    want = [(c.view(torch.uint8).clone(), s.view(torch.uint8).clone()) for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale))]
+    table = cache.table.cpu()
+    for (c, s), x in zip(want, (k, v)):
+        code, byte = _quantize(x.cpu().double())
+        code, byte = _pack(code).cuda(), byte.cuda()
+        for t in range(len(seq)):
+            b, p = int(seq[t]), int(pos[t])
+            if 0 <= b < 4 and 0 <= p < table.shape[1] * page and 0 <= int(table[b, p // page]) < cache.k.shape[0]:
+                c[int(table[b, p // page]), :, p % page] = code[t]
+                s[int(table[b, p // page]), :, :, p % page] = byte[t]
+    P.kv_append(cache, k, v, seq.cuda(), pos.cuda())
+    for got, scale, (c, s) in zip((cache.k, cache.v), (cache.k_scale, cache.v_scale), want):
+        assert torch.equal(got.view(torch.uint8), c) and torch.equal(scale.view(torch.uint8), s)
+
+
+def _edge_groups():
+    """Groups of 32 where the scale or a code can go wrong, as bf16."""
+    rows = []
+    for top in (7.0, 7.03125, 6.0, 6.9375, 4.0, 3.5, 3.515625, 1.0, 1.75, 1.7578125):
+        for e in (-126, -125, -124, -123, -30, 0, 30, 120, 125):
+            r = [top, -top, top * 0.96, top / 2, top / 3, -top / 7, top * 2.0 ** -9, 0.0, -0.0]
+            rows.append([v * 2.0 ** e if abs(v) * 2.0 ** (e - 127) < 2 else 0.0 for v in r])
+    for s in (1.0, 2.0 ** -20, 2.0 ** 20):                       # every border between two codes, and its neighbours
+        for sign in (1, -1):
+            ties = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]
+            rows.append([6.0 * s] + [sign * s * t * f for t in ties for f in (1.0, 1.0 - 2.0 ** -8, 1.0 + 2.0 ** -7)])
+    rows += [[0.0], [-0.0] * 32, [2.0 ** -133], [3e38, 1e38], [-3.3895e38, 1.0], [NAN], [1.0, INF], [-INF, 0.0, 1.0], [INF, NAN], [2.0 ** -127] * 32,
+             [2.0 ** -120, 2.0 ** -126, 2.0 ** -127]]
+    x = torch.zeros(len(rows), 32, dtype=torch.float64)
+    for i, r in enumerate(rows):
+        x[i, :len(r)] = torch.tensor(r, dtype=torch.float64)
+    return x.bfloat16()
+
+
+def test_append_edges():
+    """Largest values at the borders of a power of two, ties, zeros, the range's ends, infinities and NaN."""
+    g = _edge_groups()
+    n = len(g)
+    x = torch.stack((g, g.flip(0), g.roll(7, 1), g.roll(3, 0)), 1).reshape(n, 2, 64)     # 2 heads of 2 groups
+    cache = P.new_cache(-(-n // 16), 2, 64, 1, -(-n // 16), 16, FP4)
+    cache.table[0] = torch.arange(cache.k.shape[0])
+    seq, pos = torch.zeros(n, dtype=torch.int32).cuda(), torch.arange(n, dtype=torch.int32).cuda()
+    P.kv_append(cache, x.cuda(), (-x).cuda(), seq, pos)
+    k, v = P.kv_read(cache, seq, pos)
+    for stored, scale, back, y in ((cache.k, cache.k_scale, k, x), (cache.v, cache.v_scale, v, -x)):
+        code, byte = _quantize(y.double())
+        there = lambda t: t.transpose(1, 2).reshape(-1, 2, 32)[:n]  # noqa: E731
+        got_e = scale.view(torch.uint8).cpu().permute(0, 3, 1, 2).reshape(-1, 2, 2)[:n]
+        assert torch.equal(got_e, byte)
+        whole = (byte != 255).repeat_interleave(16, -1)
+        assert torch.equal(there(stored.view(torch.uint8).cpu())[whole], _pack(code)[whole])
+        want = torch.from_numpy(np.where(code & 8, -1.0, 1.0) * GRID[code.numpy() & 7]).double() * torch.where(
+            byte == 255, NAN, 2.0 ** (byte.double() - 127)).repeat_interleave(32, -1)
+        assert torch.equal(back.cpu().double().nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+def test_append_then_attend():
+    """Token by token against one call for the whole prompt, and against the definition."""
+    H, D, page, n = 2, 64, 16, 50
+    x = torch.randn(2, n, H, D, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    a, b = (P.new_cache(6, H, D, 1, 5, page, FP4) for _ in range(2))
+    for c in (a, b):
+        c.table[0, :4] = torch.tensor([5, 0, 2, 3], dtype=torch.int32)
+    zero, pos = torch.zeros(n, dtype=torch.int32).cuda(), torch.arange(n, dtype=torch.int32).cuda()
+    P.kv_append(a, x[0], x[1], zero, pos)
+    for t in range(n):
+        P.kv_append(b, x[0, t:t + 1], x[1, t:t + 1], zero[:1], pos[t:t + 1])
+    for f in ("k", "v", "k_scale", "v_scale"):
+        assert torch.equal(getattr(a, f).view(torch.uint8), getattr(b, f).view(torch.uint8))
+    q = _q(1, 4, D)
+    _check(_as_bf16(a), q, [n], P.paged_attention(a, q, _int([n])))
+    # stored values are within half a step of the codes, which is at most a seventh of the group's largest
+    k, v = P.kv_read(a, zero, pos)
+    for got, want in ((k, x[0]), (v, x[1])):
+        top = want.float().unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True)
+        assert ((got - want).float().unflatten(-1, (-1, 32)).abs() <= top * (2 / 7)).all()
+
+
+# ---- read ----
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("layout", ["heads", "rows", "both"])
+@pytest.mark.parametrize("H,D,page", [(1, 32, 16), (3, 96, 32), (8, 128, 64), (2, 256, 256)])
+def test_read(H, D, page, layout, kind):
+    lengths = [0, 5, 77, 300]
+    if kind == "fp4":
+        cache = _cache(lengths, H, D, page, layout=layout)
+        K, V = _values(cache.k, cache.k_scale), _values(cache.v, cache.v_scale)
+    else:
+        cache = _wide(lengths, H, D, page, fp8=kind == "fp8", layout=layout)
+        K, V = cache.k.float().cpu(), cache.v.float().cpu()
+        if kind == "fp8":
+            K, V = K * cache.k_scale.cpu()[:, None, None], V * cache.v_scale.cpu()[:, None, None]
+    cache.table[2, 1:2] = cache.k.shape[0]
+    seq, pos = [3] * 300 + [2] * 77 + [1] * 5, list(range(300)) + list(range(77)) + list(range(5))
+    seq += [-1, 4, 3, 3, 0, 3, 2 ** 31 - 1]
+    pos += [0, 0, -1, 10 ** 6, 0, 2 ** 31 - 1, 2 ** 31 - 1]
+    perm = torch.randperm(len(seq), generator=torch.Generator().manual_seed(1)).tolist()
+    seq, pos = [seq[i] for i in perm], [pos[i] for i in perm]
+    table = cache.table.cpu()
+    want = torch.zeros(2, len(seq), H, D, dtype=torch.float64)
+    for t, (b, p) in enumerate(zip(seq, pos)):
+        if 0 <= b < 4 and 0 <= p < table.shape[1] * page and 0 <= int(table[b, p // page]) < cache.k.shape[0]:
+            want[0, t], want[1, t] = K[int(table[b, p // page]), :, p % page], V[int(table[b, p // page]), :, p % page]
+    want = want.bfloat16()                    # (fp8: from the float32 product, one rounding; exact for the others)
+    same = lambda a, b: torch.equal(a.nan_to_num(7.0).cpu(), b.nan_to_num(7.0))  # noqa: E731
+    k, v = P.kv_read(cache, _int(seq), _int(pos))
+    assert k.dtype == torch.bfloat16 and k.is_contiguous() and same(k, want[0]) and same(v, want[1])
+    # outputs whose rows are apart, and nothing between them touched
+    wide = torch.full((len(seq), 3 * H * D + 8), 5.0, dtype=torch.bfloat16, device="cuda")
+    out = tuple(wide[:, i * H * D:(i + 1) * H * D].view(-1, H, D) for i in (0, 2))
+    got = P.kv_read(cache, _int(seq), _int(pos), out=out)
+    assert got[0] is out[0] and got[1] is out[1] and same(out[0], want[0]) and same(out[1], want[1])
+    assert (wide[:, H * D:2 * H * D] == 5).all() and (wide[:, 3 * H * D:] == 5).all()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    a, b = P.kv_read(cache, _int(seq), _int(pos), stream=s)
+    s.synchronize()
+    assert same(a, want[0]) and same(b, want[1])
+
+
+# ---- together ----
+
+def test_graph():
+    """One graph turns, appends, attends and reads; every replay against eager calls."""
+    lengths, H, D = [100, 3, 0, 515], 2, 128
+    cache, ref = (_cache([n + 8 for n in lengths], H, D, 64, width=10) for _ in range(2))
+    L, seq = _int(lengths), torch.arange(4, dtype=torch.int32).cuda()
+    plan = P.rope_plan((44, 42, 42), interleaved=True)
+    qkv = torch.randn(4, (8 + 2 * H) * D, generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+
+    def step(c, x, n):
+        h = x.unflatten(1, (-1, D))
+        qk = P.rope(h[:, :8 + H], n[:, None].expand(4, 3).contiguous(), plan)
+        P.kv_append(c, qk[:, 8:], h[:, 8 + H:], seq, n)
+        return P.paged_attention(c, qk[:, :8], n + 1), *P.kv_read(c, seq, n)
+
+    step(ref, qkv, L)
+    graph, n = torch.cuda.CUDAGraph(), L.clone()
+    with torch.cuda.graph(graph):
+        outs = step(cache, qkv, n)
+    for i in range(4):
+        n.copy_(L + i)
+        qkv.copy_(torch.randn(qkv.shape, generator=torch.Generator().manual_seed(i)).bfloat16())
+        for o in outs:
+            o.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, step(ref, qkv, L + i)):
+            assert torch.equal(o, w), f"replay {i}"
+        # what attention saw is what kv_read gives back
+        bf, top = P.new_cache(64, H, D, 4, 10, 64), max(lengths) + i + 1
+        bf.table[:] = torch.arange(40, dtype=torch.int32).reshape(4, 10)
+        sq, ps = torch.arange(4).repeat_interleave(top).int().cuda(), torch.arange(top).repeat(4).int().cuda()
+        ps = torch.where(ps <= (L + i)[sq.long()], ps, -1)
+        P.kv_append(bf, *P.kv_read(cache, sq, ps), sq, ps)
+        qk = P.rope(qkv.unflatten(1, (-1, D))[:, :8 + H], n[:, None].expand(4, 3).contiguous(), plan)
+        _check(bf, qk[:, :8], [m + i + 1 for m in lengths], outs[0])
+
+
+def test_graph_over_a_wide_table():
+    """A program records its step with a table for the longest context it will allow, and replays it from the first token on."""
+    H, D, page, width = 2, 128, 64, 1024
+    lengths = [0, 1, 100, 700, 9000, 5]
+    cache = _cache([n + 1 for n in lengths], H, D, page, width=width)
+    q, L, ref = _q(len(lengths), 3 * H, D), torch.zeros(len(lengths), dtype=torch.int32, device="cuda"), _as_bf16(cache)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = P.paged_attention(cache, q, L)
+    for now in ([0] * 6, [min(n, 1) for n in lengths], lengths, [n // 2 for n in lengths], [0, 1, 100, 5, 700, 5]):
+        L.copy_(torch.tensor(now, dtype=torch.int32))
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, P.paged_attention(cache, q, L)), f"lengths {now}"
+        _check(ref, q, now, out)
+
+
+def test_refusals():
+    cache = _cache([30, 40], 2, 64, 16)
+    q, L, z = _q(2, 4, 64), _int([30, 40]), _int([0, 0])
+    k = _q(2, 2, 64)
+    with pytest.raises(TypeError, match="k_scale must be torch.float8_e8m0fnu"):
+        P.paged_attention(P.PagedCache(cache.k, cache.v, cache.table, torch.ones(2).cuda(), torch.ones(2).cuda()), q, L)
+    with pytest.raises(ValueError, match="k_scale must have shape"):
+        P.kv_append(P.PagedCache(cache.k, cache.v, cache.table, cache.k_scale[:, :, :1], cache.v_scale), k, k, z, L)
+    with pytest.raises(TypeError, match="k_scale must be a torch.Tensor"):
+        P.kv_read(P.PagedCache(cache.k, cache.v, cache.table), z, L)
+    with pytest.raises(ValueError, match="k_scale must be contiguous"):
+        s = cache.k_scale.view(torch.uint8).transpose(2, 3).contiguous().transpose(2, 3).view(E8M0)
+        P.kv_read(P.PagedCache(cache.k, cache.v, cache.table, s, cache.v_scale), z, L)
+    with pytest.raises(ValueError, match="k and v alike"):
+        P.kv_read(P.PagedCache(cache.k, cache.v[:1], cache.table, cache.k_scale, cache.v_scale), z, L)
+    with pytest.raises(ValueError, match="seq must have shape"):
+        P.kv_read(cache, z[:1], L)
+    with pytest.raises(TypeError, match="pos must be torch.int32"):
+        P.kv_read(cache, z, L.long())
+    with pytest.raises(ValueError, match="pos must be a tensor of one dimension"):
+        P.kv_read(cache, z, L[:, None])
+    with pytest.raises(ValueError, match=r"out\[1\] must have shape"):
+        P.kv_read(cache, z, L, out=(k, k[:1]))
+    with pytest.raises(TypeError, match=r"out\[0\] must be torch.bfloat16"):
+        P.kv_read(cache, z, L, out=(k.float(), k))
+    with pytest.raises(Q.QwamError, match="at least heads"):
+        P.kv_read(cache, z, L, out=(k[:1].expand(2, 2, 64), k))
+    with pytest.raises(Q.QwamError, match="tokens must be"):
+        P.kv_read(cache, z[:0], L[:0])
+    with pytest.raises(ValueError, match="requires a gradient, which kv_read does not have"):
+        P.kv_read(cache, z, L, out=(k, k.clone().requires_grad_()))
+    with pytest.raises(ValueError, match="requires a gradient, which kv_append does not have"):
+        P.kv_append(cache, k.clone().requires_grad_(), k, z, L)
+    with pytest.raises(TypeError, match="a bare handle has no pool"):
+        P.kv_read(cache, z, L, stream=types.SimpleNamespace(cuda_stream=0))
+    wide = _wide([30, 40], 2, 64, 16, fp8=True)
+    wide.k_scale.requires_grad_()
+    with pytest.raises(ValueError, match="requires a gradient, which kv_read does not have"):
+        P.kv_read(wide, z, L)
+    assert wide.k.dtype == FP8
