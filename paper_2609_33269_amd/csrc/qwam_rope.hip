@@ -4,10 +4,16 @@
 // One pass over x, bound by its reading and y's writing.
 //
 //   * The angle is the same for all heads of a token, so a thread computes the
-//     cosines and sines of its few pairs once and then walks over heads.
+//     cosine and sine of its pair (or two) once and then walks over heads.  One
+//     pair a thread gives short calls their lanes and long ones enough bytes in
+//     flight: pieces of 8 channels took rope of 8192 x 32 heads of 128 24.1 us and
+//     of 4 x 20 of 64 4.3 us, where pieces of 2 take 21.9 and 2.7.
 //   * Far positions: the product is taken in float64 and in turns, where removing
 //     whole turns is exact; what is left within a quarter turn is small enough for
 //     the first terms of the series of sine and cosine in float32.
+// Measured, heads of 128 in bf16 (graph replays): 8192 x 32, interleaved, 21.9 us (6.1 TB/s, x and y within the
+// last-level cache); 4096 x 24 in halves 10.5 us (4.8 TB/s); 512 x 8 3.1 us; 4 tokens x 20 heads of 64 2.7 us, of which
+// a launch is 2.3.
 #include "qwam_device.h"
 #include "qwam_internal.h"
 #include "qwam_mfma.h"
@@ -37,9 +43,9 @@ __device__ __forceinline__ float2 cos_sin_turns(double t) {
   return make_float2((turn + 1) & 2 ? -u : u, turn & 2 ? -v : v);
 }
 
-// W values that lie beside each other, aligned to 16 bytes at most (to a value where nothing wider fits: W up to 2)
-template <typename E, int W>
-struct alignas(W <= 2 ? sizeof(E) : W * sizeof(E) < 16 ? W * sizeof(E) : 16) Piece {
+// W values that lie beside each other, read and written at once where they are aligned
+template <typename E, int W, bool ALIGNED>
+struct alignas(ALIGNED ? W * sizeof(E) : sizeof(E)) Piece {
   E e[W];
 };
 
@@ -54,20 +60,20 @@ struct RopeArgs {
   const void* x;
   void* y;
   int64_t x_stride, y_stride;
-  uint32_t units, spread, threads;    // pieces of a head, heads of a token taken at once, threads
+  uint32_t units, spread, threads;    // pieces of a head, threads of a piece (each with every spread-th head), all
   float sign;
 };
 
 }  // namespace
 
 // A thread's piece is W channels beside each other: W / 2 pairs (interleaved), or the first halves of W pairs, whose second
-// halves are another piece.  Pieces that do not turn are copied (one by one where W <= 2).  Threads: (token, head among
+// halves are another piece.  Channels that do not turn are copied (one by one if not ALIGNED).  Threads: (token, head among
 // `spread`, piece).  HEADS heads are read before the first is written, since x may be y.
-template <typename E, int W, bool INTERLEAVED>
+template <typename E, int W, bool INTERLEAVED, bool ALIGNED>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  constexpr int N = INTERLEAVED ? W / 2 : W, TAIL = W <= 2 ? 1 : W, HEADS = 4;
-  typedef Piece<E, W> piece;
-  typedef Piece<E, TAIL> tail;
+  constexpr int N = INTERLEAVED ? W / 2 : W, TAIL = ALIGNED ? W : 1, HEADS = 4;
+  typedef Piece<E, W, ALIGNED> piece;
+  typedef Piece<E, TAIL, ALIGNED> tail;
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   if (i >= a.threads) return;
   const uint32_t row = i / a.units, u = i - row * a.units, t = row / a.spread, h0 = row - t * a.spread;
@@ -94,14 +100,19 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   load(h0);
   float cs[N], sn[N];
   const int64_t pr = static_cast<int64_t>(t % static_cast<uint32_t>(a.p.positions)) * a.p.axes;
+  double at[kRopeMaxAxes];              // (all axes' positions at once, not behind the pair's axis)
+#pragma unroll
+  for (int k = 0; k < kRopeMaxAxes; ++k) {
+    at[k] = 0.0;
+    if (k < a.p.axes && a.p.pos_f32) at[k] = static_cast<const float*>(a.p.pos)[pr + k];
+    else if (k < a.p.axes) at[k] = static_cast<const int32_t*>(a.p.pos)[pr + k];       // (not by way of float32)
+  }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     const uint32_t pair = u * N + j;
     const uint32_t axis = static_cast<uint32_t>(a.p.axis[pair]);
+    const double pos = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
     const bool turns = axis < static_cast<uint32_t>(a.p.axes);
-    double pos = 0.0;
-    if (turns && a.p.pos_f32) pos = static_cast<const float*>(a.p.pos)[pr + axis];
-    else if (turns) pos = static_cast<const int32_t*>(a.p.pos)[pr + axis];       // (int32 to float64, not by way of float32)
     const float2 v = cos_sin_turns(turns ? pos * (a.p.inv_freq[pair] * 0.15915494309189535) : 0.0);
     cs[j] = v.x;
     sn[j] = v.y * a.sign;
@@ -157,30 +168,30 @@ namespace {
 template <typename E>
 void launch(RopeArgs& a, int tokens, hipStream_t stream) {
   const RopeParams& p = a.p;
-  // the widest pieces that every row and half consists of and that are aligned in both arrays
-  auto fits = [&](int w) {
-    const int64_t bytes = w * static_cast<int64_t>(sizeof(E)) < 16 ? w * static_cast<int64_t>(sizeof(E)) : 16;
-    const bool apart = tokens > 1;
-    return p.dim % w == 0 && (p.interleaved ? 2 * p.pairs : p.pairs) % w == 0 && reinterpret_cast<uintptr_t>(a.x) % bytes == 0 &&
-           reinterpret_cast<uintptr_t>(a.y) % bytes == 0 && (!apart || (a.x_stride % w == 0 && a.y_stride % w == 0));
-  };
-  const int w = fits(8) ? 8 : fits(4) ? 4 : 0;
-  auto run = [&](auto kernel, int width) {
-    const int tail = width <= 2 ? 1 : width;
-    a.units = static_cast<uint32_t>(p.pairs / (p.interleaved ? width / 2 : width) + (p.dim - 2 * p.pairs) / tail);
-    a.spread = static_cast<uint32_t>(p.heads);
+  const int64_t work = static_cast<int64_t>(tokens) * p.heads * p.pairs;
+  // Heads of a thread: 4 from where the chip is full (2^17 pairs; 512 x 32 heads of 128 4.1 us, with one head 8.4, with 16
+  // 5.9), up to 16 in longer calls, which have threads enough to spend fewer cosines (8192 x 32: 21.9 us, with 4 heads 28.5)
+  const int64_t per = work < (1 << 17) ? 1 : work >> 19 < 4 ? 4 : work >> 19 > 16 ? 16 : work >> 19;
+  a.spread = static_cast<uint32_t>((p.heads + per - 1) / per);
+  const bool apart = tokens > 1;
+  const bool twos = p.dim % 2 == 0 && reinterpret_cast<uintptr_t>(a.x) % (2 * sizeof(E)) == 0 &&
+                    reinterpret_cast<uintptr_t>(a.y) % (2 * sizeof(E)) == 0 && (!apart || (a.x_stride % 2 == 0 && a.y_stride % 2 == 0));
+  auto run = [&](auto kernel, int pairs, int tail) {
+    a.units = static_cast<uint32_t>(p.pairs / pairs + (p.dim - 2 * p.pairs) / tail);
     a.threads = static_cast<uint32_t>(static_cast<int64_t>(tokens) * a.spread * a.units);
     const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(a.threads) + 255) / 256);
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, stream, a);
   };
   if (p.interleaved) {
-    if (w == 8) run(rope_kernel<E, 8, true>, 8);
-    else if (w == 4) run(rope_kernel<E, 4, true>, 4);
-    else run(rope_kernel<E, 2, true>, 2);
+    if (twos) run(rope_kernel<E, 2, true, true>, 1, 2);
+    else run(rope_kernel<E, 2, true, false>, 1, 1);
   } else {
-    if (w == 8) run(rope_kernel<E, 8, false>, 8);
-    else if (w == 4) run(rope_kernel<E, 4, false>, 4);
-    else run(rope_kernel<E, 1, false>, 1);
+    // halves of bf16: two pairs a thread make words of them (4096 x 24 heads of 128 10.5 us, one by one 10.6, and 16384 x 8
+    // 12.8, one by one 13.9), except in short calls (4 x 20 of 64 2.7 us, two pairs 2.9) and in float32 (21.8 us, two 21.8)
+    if constexpr (sizeof(E) == 2) {
+      if (twos && p.pairs % 2 == 0 && work >= (1 << 18)) return run(rope_kernel<E, 2, false, true>, 2, 2);
+    }
+    run(rope_kernel<E, 1, false, false>, 1, 1);
   }
 }
 
