@@ -133,17 +133,74 @@ __device__ __forceinline__ v8bf bf8(uint32_t a, uint32_t b, uint32_t c, uint32_t
   return __builtin_bit_cast(v8bf, make_uint4(a, b, c, d));
 }
 
+// join the waves of a workgroup into the result of its range, or of the sequence where that is the only one: one maximum,
+// then sums of l and o through LDS.  acc: o of head `g0`, channel DP / 16 * (4 c + i) + e of its quarter c, in the lanes that
+// `hold` one (m and l are those of g0 in all of them); vs: what o is in.
+template <int DP>
+__device__ __forceinline__ void finish_range(const AttnArgs& a, const Span& sp, float m, float l, const v4f (&acc)[DP / 16], float* smem,
+                                             int wave, int g0, bool hold, int nq, int D, int64_t head_row, int range,
+                                             float vs) {
+  constexpr int waves = kAttnWaves, DC = DP / 16;
+  const int c = (threadIdx.x & 63) >> 4;
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  constexpr int RS = DP + 4;                      // floats of an o row in LDS
+  float* const sm = smem;                         // [waves][16] maxima, then sums
+  float* const so = smem + 2 * waves * 16;        // [waves][nq][RS]
+  if (c == 0) {
+    sm[wave * 16 + g0] = m;
+    sm[(waves + wave) * 16 + g0] = l;
+  }
+  __syncthreads();
+  float mt = sm[g0];
+  for (int w = 1; w < waves; ++w) mt = fmaxf(mt, sm[w * 16 + g0]);
+  const float f = __builtin_amdgcn_exp2f(m - (mt == -INFINITY ? 0.0f : mt));
+  if (hold)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < DC; e += 4)
+        *reinterpret_cast<float4*>(so + (wave * nq + g0) * RS + DC * (4 * c + i) + e) =
+            make_float4(acc[e][i] * f, acc[e + 1][i] * f, acc[e + 2][i] * f, acc[e + 3][i] * f);
+  __syncthreads();
+  for (int i = threadIdx.x; i < nq * (D / 4); i += 64 * waves) {
+    const int g = i / (D / 4), d = (i % (D / 4)) * 4;
+    float top = sm[g], sum = 0.0f;
+    for (int w = 1; w < waves; ++w) top = fmaxf(top, sm[w * 16 + g]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int w = 0; w < waves; ++w) {
+      sum += sm[(waves + w) * 16 + g] * __builtin_amdgcn_exp2f(sm[w * 16 + g] - ref);
+      const float4 v = *reinterpret_cast<const float4*>(so + (w * nq + g) * RS + d);
+      o.x += v.x;
+      o.y += v.y;
+      o.z += v.z;
+      o.w += v.w;
+    }
+    const int64_t hr = head_row + g;
+    if (sp.count == 1) {
+      const float n = sum > 0.0f || sum != sum ? vs / sum : 0.0f;
+      *reinterpret_cast<uint2*>(a.out + hr * D + d) = make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
+    } else {
+      const int64_t pr = hr * a.splits + range;
+      *reinterpret_cast<float4*>(a.part + pr * D + d) = o;
+      if (d == 0) {
+        a.stat[2 * pr] = top;
+        a.stat[2 * pr + 1] = sum;
+      }
+    }
+  }
+}
+
 }  // namespace
 
 // DP: dim rounded up to 64, 128 or 256; FULL: dim == DP
-template <int DP, CacheType TYPE, bool FULL>
-__global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 128 ? 4 : 1) void paged_attention_kernel(AttnArgs a) {
-  constexpr bool FP8 = TYPE == CacheType::kFp8, FP4 = TYPE == CacheType::kFp4;
-  constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value (fp4: rows and strides are in bytes)
-  constexpr int SB = FP4 ? 1 : EB;                // bytes that the cache's strides count
+template <int DP, bool FP8, bool FULL>
+__global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void paged_attention_kernel(AttnArgs a) {
+  constexpr int EB = FP8 ? 1 : 2;                 // bytes of a cached value
   constexpr int DC = DP / 16;                     // channels of V in a lane
-  constexpr int NK = FP4 ? (DP + 127) / 128 : DP * EB / 64;       // 16-byte pieces of K in a lane, per 16 keys
-  constexpr int NV = FP4 ? (DC + 7) / 8 : DC * EB / 4;            // words of V in a lane, per key
+  constexpr int NK = DP * EB / 64;                // 16-byte pieces of K in a lane, per 16 keys
+  constexpr int NV = DC * EB / 4;                 // words of V in a lane, per key
   constexpr int NF = DP / 32;                     // MFMA steps over the channels
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
@@ -178,10 +235,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
   }
 
   // q as the second operand of S^T: head r, channels of this quarter
-  auto channel = [&](int f) {
-    if constexpr (FP4) return DP == 64 ? 16 * c + 8 * f : 128 * (f >> 2) + 32 * c + 8 * (f & 3);
-    else return FP8 ? 64 * (f >> 1) + 16 * c + 8 * (f & 1) : 32 * f + 8 * c;
-  };
+  auto channel = [&](int f) { return FP8 ? 64 * (f >> 1) + 16 * c + 8 * (f & 1) : 32 * f + 8 * c; };
   v8bf qf[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f) {
@@ -193,48 +247,21 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
   const float ks = FP8 ? a.c.k_scale[h] : 1.0f;
   const float sscale = a.scale * ks * kLog2e;
 
-  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride * SB;
-  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride * SB;
-  const int row = static_cast<int>(a.c.row_stride) * SB;          // bytes; 16 rows stay below 2^31
+  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride * EB;
+  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride * EB;
+  const int row = static_cast<int>(a.c.row_stride) * EB;          // bytes; 16 rows stay below 2^31
   const int row_mask = (1 << a.c.page_bits) - 1;
   // bytes from the head's first row of page 0 to row 0 of 16 positions; a missing page reads page 0, unseen
   auto place = [&](int tile, int t, int& id) -> int64_t {
     id = __builtin_amdgcn_readlane(pid, 2 * tile + t);
     const int64_t page = id < 0 ? 0 : id;
-    return (page * a.c.page_stride + static_cast<int64_t>((start(tile) + 16 * t) & row_mask) * a.c.row_stride) * SB;
-  };
-  // fp4: the exponents of a key's groups that its lane holds, and of the lane's channels of V for four keys each
-  uint32_t ke[2][NK], va_exp[2], vb_exp[2];
-  auto exponents_at = [&](int tile, int t) __attribute__((always_inline)) {
-    const int page = __builtin_amdgcn_readlane(pid, 2 * tile + t);
-    return (page < 0 ? 0 : page) * fp4_exp_page(a.c) + fp4_exp_group(a.c, h, 0) + ((start(tile) + 16 * t) & row_mask);
-  };
-  auto load_ke = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint8_t* const e = a.c.k_exp + exponents_at(tile, t) + r;
-#pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        const int g = DP == 64 ? c >> 1 : 4 * i + c;
-        ke[t][i] = 0;
-        if (FULL || g * kFp4Group < D) ke[t][i] = e[static_cast<int64_t>(g) << a.c.page_bits];
-      }
-    }
-  };
-  auto load_ve = [&](int tile, uint32_t (&ve)[2]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int g = DC * r / kFp4Group;
-      ve[t] = 0;
-      if (FULL || DC * r < D)
-        ve[t] = *reinterpret_cast<const uint32_t*>(a.c.v_exp + exponents_at(tile, t) + 4 * c + (static_cast<int64_t>(g) << a.c.page_bits));
-    }
+    return (page * a.c.page_stride + static_cast<int64_t>((start(tile) + 16 * t) & row_mask) * a.c.row_stride) * EB;
   };
 
   uint4 kr[2][NK];
   // heads of 64: V comes a tile ahead too (in wider ones its registers cost more waves than that gains: 4 ragged
   // contexts up to 16384, 16 heads of 64, 32.4 -> 27.6 us, one alone 17.0 -> 17.7; 16 up to 4096, 8 x 3 of 128, 18.0 -> 19.2)
-  constexpr bool V_AHEAD = FP4 || DP == 64;
+  constexpr bool V_AHEAD = DP == 64;
   uint32_t va[8][NV], vb[8][NV];
   int id[2], idn[2];
   int64_t at[2], atn[2];
@@ -243,30 +270,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
+        const int ch = 64 / EB * i + 16 / EB * c;
         kr[t][i] = make_uint4(0, 0, 0, 0);
-        if constexpr (FP4 && DP == 64) {
-          if (FULL || 16 * c < D) {
-            const uint2 w = *reinterpret_cast<const uint2*>(kbase + o[t] + (r * row + 8 * c));
-            kr[t][i].x = w.x;
-            kr[t][i].y = w.y;
-          }
-        } else if constexpr (FP4) {
-          if (FULL || 128 * i + 32 * c < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + 64 * i + 16 * c));
-        } else {
-          const int ch = 64 / EB * i + 16 / EB * c;
-          if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
-        }
+        if (FULL || ch < D) kr[t][i] = *reinterpret_cast<const uint4*>(kbase + o[t] + (r * row + ch * EB));
       }
   };
   auto load_v = [&](const int64_t (&o)[2], uint32_t (&vr)[8][NV]) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + (FP4 ? DC * r / 2 : DC * r * EB));
+      const uint8_t* src = vbase + o[j >> 2] + ((4 * c + (j & 3)) * row + DC * r * EB);
 #pragma unroll
       for (int w = 0; w < NV; ++w) vr[j][w] = 0;
-      if constexpr (FP4 && DC == 4) {
-        if (FULL || DC * r < D) vr[j][0] = *reinterpret_cast<const uint16_t*>(src);
-      } else if constexpr (NV == 8) {
+      if constexpr (NV == 8) {
         if (FULL || DC * r < D) *reinterpret_cast<uint4*>(&vr[j][0]) = *reinterpret_cast<const uint4*>(src);
         if (FULL || DC * r + 8 < D) *reinterpret_cast<uint4*>(&vr[j][4]) = *reinterpret_cast<const uint4*>(src + 16);
       } else if (FULL || DC * r < D) {
@@ -286,11 +301,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
 #pragma unroll
     for (int t = 0; t < 2; ++t) at[t] = place(0, t, id[t]);
     load_k(at);
-    if constexpr (FP4) load_ke(0);
     if constexpr (V_AHEAD) load_v(at, va);
-    if constexpr (FP4) load_ve(0, va_exp);
   }
-  auto turn = [&](int tile, uint32_t (&vr)[8][NV], uint32_t (&vn)[8][NV], uint32_t (&ve)[2], uint32_t (&ven)[2]) __attribute__((always_inline)) {
+  auto turn = [&](int tile, uint32_t (&vr)[8][NV], uint32_t (&vn)[8][NV]) __attribute__((always_inline)) {
     if constexpr (!V_AHEAD) load_v(at, vr);
     // scores of keys 16 t + 4 c + i, head r
     v4f s[2];
@@ -300,11 +313,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         v8bf k;
-        if constexpr (FP4) {
-          const uint4 p = kr[t][f >> 2];
-          const uint32_t w = (f & 3) == 0 ? p.x : (f & 3) == 1 ? p.y : (f & 3) == 2 ? p.z : p.w, e = ke[t][f >> 2] << 23;
-          k = bf8(fp4_pair(w, e, 0), fp4_pair(w, e, 1), fp4_pair(w, e, 2), fp4_pair(w, e, 3));
-        } else if constexpr (FP8) {
+        if constexpr (FP8) {
           const uint4 w = kr[t][f >> 1];
           const uint32_t x = f & 1 ? w.z : w.x, y = f & 1 ? w.w : w.y;
           k = bf8(fp8_pair<false>(x), fp8_pair<true>(x), fp8_pair<false>(y), fp8_pair<true>(y));
@@ -318,9 +327,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
 #pragma unroll
       for (int t = 0; t < 2; ++t) atn[t] = place(tile + 1, t, idn[t]);
       load_k(atn);
-      if constexpr (FP4) load_ke(tile + 1);
       if constexpr (V_AHEAD) load_v(atn, vn);
-      if constexpr (FP4) load_ve(tile + 1, ven);
     }
     const int p0 = start(tile);
     const bool whole = p0 >= sp.first && p0 + 32 <= sp.len && id[0] >= 0 && id[1] >= 0;
@@ -363,17 +370,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
 #pragma unroll
         for (int w = 0; w < NV; ++w)
           if (!(seen >> j & 1u)) vr[j][w] = 0;
-      if constexpr (FP4) {                        // (an exponent of 255 makes NaN of a code 0 too)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!(seen >> j & 1u)) ve[j >> 2] &= ~(0xFFu << (8 * (j & 3)));
-      }
-    }
-    // the exponents at a float's place; the conversion does not look at its other bits
-    uint32_t vs8[8];
-    if constexpr (FP4) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) vs8[j] = (j & 3) == 3 ? ve[j >> 2] >> 1 : ve[j >> 2] << (23 - 8 * (j & 3));
     }
     // o^T += V^T S^T: channel DC r + e of the lane's eight keys
 #pragma unroll
@@ -381,8 +377,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
       uint32_t y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if constexpr (FP4) y[j] = fp4_pair(vr[j][w >> 2], vs8[j], w & 3);
-        else if constexpr (FP8) y[j] = w & 1 ? fp8_pair<true>(vr[j][w >> 1]) : fp8_pair<false>(vr[j][w >> 1]);
+        if constexpr (FP8) y[j] = w & 1 ? fp8_pair<true>(vr[j][w >> 1]) : fp8_pair<false>(vr[j][w >> 1]);
         else y[j] = vr[j][w];
       }
       const v8bf even = bf8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7]));
@@ -400,69 +395,462 @@ __global__ __launch_bounds__(64 * kAttnWaves, TYPE == CacheType::kFp8 && DP == 1
   };
   if constexpr (V_AHEAD) {
     for (int tile = 0; tile < tiles; tile += 2) {
-      turn(tile, va, vb, va_exp, vb_exp);
-      if (tile + 1 < tiles) turn(tile + 1, vb, va, vb_exp, va_exp);
+      turn(tile, va, vb);
+      if (tile + 1 < tiles) turn(tile + 1, vb, va);
     }
   } else {
-    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vb, va_exp, vb_exp);
+    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vb);
   }
 
-  // join the waves: one maximum, then sums of l and o through LDS
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  constexpr int RS = DP + 4;                      // floats of an o row in LDS
-  float* const sm = smem;                         // [waves][16] maxima, then sums
-  float* const so = smem + 2 * waves * 16;        // [waves][nq][RS]
-  if (c == 0) {
-    sm[wave * 16 + r] = m;
-    sm[(waves + wave) * 16 + r] = l;
+  finish_range<DP>(a, sp, m, l, acc, smem, wave, r, r < nq, nq, D, head_row, range, FP8 ? a.c.v_scale[h] : 1.0f);
+}
+
+// The same over 4-bit pages, for which the loads are so narrow that the instructions of a turn are the bound, so that
+// they are counted here:
+//   * A wave takes 64 positions a turn, in blocks of 16 (32 for heads above 128 in groups above 4), so that the maximum,
+//     the test for a new one and the loop are paid once for them.
+//   * Keys are multiplied as they are stored (v_mfma_scale_f32_16x16x128_f8f6f4: e2m1 with a power of two for 32 channels
+//     is its operand).  q enters as two e4m3 pieces, each of 4 bits of its 8: q exactly, where it is within 2^-15 of the
+//     largest of its 32 channels, and to 2^-22 of that below.
+//   * Values are converted to bf16, which is exact and applies the power of two, and weighted by two bf16 pieces.  With up
+//     to 4 query heads the 16 columns of that product hold each head four times, for both pieces of its weights and for
+//     even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them, and a lane
+//     needs no transposing.  The same four lanes share a head's 64 weights, 16 each.  (8 x 3 heads of 128: turns of 264
+//     instead of 500 instructions.)
+//   * Where a block of 16 positions lies is computed once, a lane each, and handed out by readlane; addresses are a
+//     scalar base and a lane's 32-bit offset that stays.
+//   * A new maximum counts from 2^kSlack above the old one on: weights stay below 2^kSlack, and o and the sum are
+//     rescaled in a few turns rather than in most (with 16 heads, one of them has a new maximum in most turns).
+constexpr float kSlack = 8.0f;
+constexpr int kNarrow = 4;              // query heads of a key head that the narrow form takes
+constexpr int kGridRanges = 32768;      // ranges in the grid's last dimension; more of them stand behind the heads
+
+// 16 bf16 values as two e4m3 pieces each: `hi` at 2^(e - 127), `lo` at 2^(e - 132).  e is 7 below the exponent of the largest
+// of a group, so that a piece is at most 2^8; what `hi` leaves is at most 2^3 of its steps.
+struct Pieces {
+  uint32_t hi[4], lo[4];
+};
+__device__ __forceinline__ Pieces fp8_pieces(const uint4& x, const uint4& y, uint32_t e) {
+  const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  const float s = __uint_as_float(e << 23), sl = __uint_as_float((e - 5) << 23);
+  typedef short v2s __attribute__((ext_vector_type(2)));
+  Pieces p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v2s hi = {0, 0}, lo = {0, 0};
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(v2bf16, w[2 * i]), s, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(v2bf16, w[2 * i + 1]), s, true);
+    p.hi[i] = __builtin_bit_cast(uint32_t, hi);
+    auto low = [](uint32_t u) { return __uint_as_float(u << 16); };
+    auto high = [](uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); };
+    const uint32_t b0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.hi[i], s, false));
+    const uint32_t b1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.hi[i], s, true));
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, low(w[2 * i]) - low(b0), high(w[2 * i]) - high(b0), sl, false);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, low(w[2 * i + 1]) - low(b1), high(w[2 * i + 1]) - high(b1), sl, true);
+    p.lo[i] = __builtin_bit_cast(uint32_t, lo);
   }
-  __syncthreads();
-  float mt = sm[r];
-  for (int w = 1; w < waves; ++w) mt = fmaxf(mt, sm[w * 16 + r]);
-  const float f = __builtin_amdgcn_exp2f(m - (mt == -INFINITY ? 0.0f : mt));
-  if (r < nq)
+  return p;
+}
+
+__device__ __forceinline__ uint32_t largest_of(const uint4& x, const uint4& y) {
+  const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
+  v2u16 m = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(v2u16, w[i] & 0x7FFF7FFFu));
+  return m[0] > m[1] ? m[0] : m[1];
+}
+
+// lane l's and lane l ^ 16's larger
+__device__ __forceinline__ uint32_t larger_xor16(uint32_t v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max(r[0], r[1]);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float quad(float v) {
+  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(v)), CTRL, 0xF, 0xF, true)));
+}
+constexpr int kQuadXor1 = 0xB1, kQuadXor2 = 0x4E;
+
+// Z of lane B of the lane's quad
+template <int B>
+__device__ __forceinline__ uint32_t quad_lane(uint32_t z) {
+  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(z), B * 0x55, 0xF, 0xF, true));
+}
+
+template <int DP, bool FULL, bool NARROW>
+__global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_attention_fp4_kernel(AttnArgs a) {
+  constexpr int BL = DP == 256 && !NARROW ? 2 : 4;        // blocks of 16 positions a turn
+  constexpr int DC = DP / 16;                     // channels of V in a lane
+  constexpr int NK = (DP + 127) / 128;            // 32 channels of a key in a lane; products over 128 channels
+  constexpr int NV = (DC + 7) / 8;                // words of V in a lane, per key
+  constexpr int NA = NARROW ? DC / 2 : DC;        // accumulators
+  constexpr int waves = kAttnWaves;
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, c = lane >> 4;
+  // a grid of heads (fastest, so that the first ranges of all, which short contexts have too, are dealt out over the chip
+  // first), sequences and ranges; the divisions are rare
+  const int qtiles = (a.group + 15) / 16, b = blockIdx.y;
+  int range = blockIdx.z, h = blockIdx.x, qt = 0;
+  if (static_cast<int>(gridDim.x) != a.c.heads * qtiles) {
+    const int high = h / (a.c.heads * qtiles);
+    h -= high * a.c.heads * qtiles;
+    range += high * kGridRanges;
+  }
+  if (qtiles > 1) {
+    const int ht = h;
+    h = ht / qtiles;
+    qt = ht - h * qtiles;
+  }
+  const Span sp = span_of(a, b);
+  if (range >= max(sp.count, 1)) return;
+  const int q0 = qt * 16, nq = min(16, a.group - q0);
+  const int64_t head_row = static_cast<int64_t>(b) * a.q_heads + h * a.group + q0;
+  const int D = FULL ? DP : a.c.dim;
+  if (sp.count == 0) {
+    for (int i = threadIdx.x; i < nq * D; i += 64 * waves) a.out[head_row * D + i] = 0;
+    return;
+  }
+
+  // positions [r0, r1) in tiles of 16 BL, every `waves`-th of them this wave's
+  const int r0 = sp.base + range * a.chunk, r1 = min(r0 + a.chunk, sp.len);
+  const int tiles = max(0, (r1 - r0 + 16 * BL - 1) / (16 * BL) - wave + waves - 1) / waves;
+  auto start = [&](int tile) { return r0 + 16 * BL * (tile * waves + wave); };
+
+  // lane i: block i % BL of tile i / BL.  Whether it has a page, and its bytes in the codes and in the scales (a missing
+  // page reads page 0, unseen)
+  uint64_t there;
+  uint32_t code_lo, code_hi, exp_lo, exp_hi;
+  {
+    const int p = start(lane / BL) + 16 * (lane % BL);
+    int pid = -1;
+    if (p < r0 + a.chunk && (p >> a.c.page_bits) < a.c.table_width)       // (does not wait for the length)
+      pid = a.c.table[static_cast<int64_t>(b) * a.c.table_width + (p >> a.c.page_bits)];
+    if (pid >= a.c.pages || p >= r1) pid = -1;
+    there = __ballot(pid >= 0);
+    const int64_t page = max(pid, 0), row = p & ((1 << a.c.page_bits) - 1);
+    const int64_t code = page * a.c.page_stride + row * a.c.row_stride, e = page * fp4_exp_page(a.c) + row;
+    code_lo = static_cast<uint32_t>(code);
+    code_hi = static_cast<uint32_t>(code >> 32);
+    exp_lo = static_cast<uint32_t>(e);
+    exp_hi = static_cast<uint32_t>(e >> 32);
+  }
+  auto handed = [&](uint32_t lo, uint32_t hi, int from) __attribute__((always_inline)) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(hi, from))) << 32 |
+                                static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, from)));
+  };
+
+  // q as the second operand of S^T, column r: its head's (in the narrow form r / 4's) pieces, of the sign of the scale.
+  // Lane quarter c supplies channels 16 c and 64 + 16 c on of 128 and the scale of channels 32 c on.  Heads up to 64: `hi` in
+  // the first 64 places and `lo` in the others, where the keys come a second time.
+  const int head = NARROW ? r >> 2 : r;
+  constexpr int NQ = DP == 64 ? 1 : 2 * NK;       // pieces of 16 channels of q in a lane
+  uint4 qx[NQ], qy[NQ];
 #pragma unroll
-      for (int e = 0; e < DC; e += 4)
-        *reinterpret_cast<float4*>(so + (wave * nq + r) * RS + DC * (4 * c + i) + e) =
-            make_float4(acc[e][i] * f, acc[e + 1][i] * f, acc[e + 2][i] * f, acc[e + 3][i] * f);
-  __syncthreads();
-  const float vs = FP8 ? a.c.v_scale[h] : 1.0f;
-  for (int i = threadIdx.x; i < nq * (D / 4); i += 64 * waves) {
-    const int g = i / (D / 4), d = (i % (D / 4)) * 4;
-    float top = sm[g], sum = 0.0f;
-    for (int w = 1; w < waves; ++w) top = fmaxf(top, sm[w * 16 + g]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int w = 0; w < waves; ++w) {
-      sum += sm[(waves + w) * 16 + g] * __builtin_amdgcn_exp2f(sm[w * 16 + g] - ref);
-      const float4 v = *reinterpret_cast<const float4*>(so + (w * nq + g) * RS + d);
-      o.x += v.x;
-      o.y += v.y;
-      o.z += v.z;
-      o.w += v.w;
+  for (int i = 0; i < NQ; ++i) {
+    qx[i] = qy[i] = make_uint4(0, 0, 0, 0);
+    const int ch = 64 * i + 16 * c;
+    if (head < nq && (FULL || ch < D)) {          // (dim is a multiple of 32)
+      const uint4* const src =
+          reinterpret_cast<const uint4*>(a.q + b * a.q_stride + static_cast<int64_t>(h * a.group + q0 + head) * D + ch);
+      qx[i] = src[0];
+      qy[i] = src[1];
     }
-    const int64_t hr = head_row + g;
-    if (sp.count == 1) {
-      const float n = sum > 0.0f || sum != sum ? vs / sum : 0.0f;
-      *reinterpret_cast<uint2*>(a.out + hr * D + d) = make_uint2(bf16_pair(o.x * n, o.y * n), bf16_pair(o.z * n, o.w * n));
-    } else {
-      const int64_t pr = hr * a.splits + range;
-      *reinterpret_cast<float4*>(a.part + pr * D + d) = o;
-      if (d == 0) {
-        a.stat[2 * pr] = top;
-        a.stat[2 * pr + 1] = sum;
+  }
+  // (above 0, so that a masked score of -inf times it is no NaN: with a scale of 0 scores below 2^118 still count as 0)
+  const float sscale = fmaxf(__builtin_fabsf(a.scale) * kLog2e, 0x1p-126f);
+
+  // bytes of a lane's rows from the first of 16, which is the last in memory where rows run backwards
+  const int row = static_cast<int>(a.c.row_stride);
+  const uint32_t step = static_cast<uint32_t>(row < 0 ? -row : row);
+  const int64_t back = row < 0 ? static_cast<int64_t>(15) * row : 0;
+  auto place = [&](int k) { return (row < 0 ? 15 - k : k) * step; };
+  const uint8_t* const kbase = static_cast<const uint8_t*>(a.c.k) + static_cast<int64_t>(h) * a.c.head_stride + back;
+  const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride + back;
+  const uint8_t* const kebase = a.c.k_exp + fp4_exp_group(a.c, h, 0);
+  const uint8_t* const vebase = a.c.v_exp + fp4_exp_group(a.c, h, 0);
+  const int kc = DP == 64 ? c & 1 : c;            // the 32 channels of a key that the lane holds (of each 128)
+  const uint32_t koff = place(r) + 16 * kc;
+  uint32_t voff[4], keoff[NK];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) voff[i] = place(4 * c + i) + DC / 2 * r;
+#pragma unroll
+  for (int i = 0; i < NK; ++i) keoff[i] = (static_cast<uint32_t>(4 * i + kc) << a.c.page_bits) + r;
+  const uint32_t veoff = (static_cast<uint32_t>(DC * r / kFp4Group) << a.c.page_bits) + 4 * c;
+  // whether the lane's channels exist
+  auto has_k = [&](int i) { return FULL || 128 * i + 32 * kc < D; };
+  const bool has_v = FULL || DC * r < D;
+
+  v4i kr[BL][NK];
+  constexpr bool V_AHEAD = NARROW && DP <= 128;   // values come a turn ahead too
+  uint32_t ke[BL][NK], va[BL][4][NV], vea[BL], vb[BL][4][NV], veb[BL];
+  int64_t code_at[BL], exp_at[BL];                // of the tile whose keys were loaded last
+  // a scalar base and a lane's offset in one load; the asm keeps the offset's extension to 64 bits beside the load, where
+  // it becomes the instruction's own
+  auto near = [](const uint8_t* base, uint32_t offset) __attribute__((always_inline)) {
+    asm("" : "+v"(offset));
+    return base + offset;
+  };
+  auto load_k = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < BL; ++t) {
+      code_at[t] = handed(code_lo, code_hi, tile * BL + t);
+      exp_at[t] = handed(exp_lo, exp_hi, tile * BL + t);
+      const uint8_t* const p = kbase + code_at[t];
+      const uint8_t* const e = kebase + exp_at[t];
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        kr[t][i] = v4i{0, 0, 0, 0};
+        ke[t][i] = 0;
+        if (!has_k(i)) continue;
+        kr[t][i] = *reinterpret_cast<const v4i*>(near(p + 64 * i, koff));
+        ke[t][i] = *near(e, keoff[i]);
       }
     }
+  };
+  auto load_v = [&](uint32_t (&vr)[BL][4][NV], uint32_t (&ve)[BL]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < BL; ++t) {
+      const uint8_t* const p = vbase + code_at[t];
+      const uint8_t* const e = vebase + exp_at[t];
+      ve[t] = 0;
+      if (has_v) ve[t] = *reinterpret_cast<const uint32_t*>(near(e, veoff));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int w = 0; w < NV; ++w) vr[t][i][w] = 0;
+        if (!has_v) continue;
+        if constexpr (DC == 4) {
+          vr[t][i][0] = *reinterpret_cast<const uint16_t*>(near(p, voff[i]));
+        } else if constexpr (DC == 8) {
+          vr[t][i][0] = *reinterpret_cast<const uint32_t*>(near(p, voff[i]));
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(near(p, voff[i]));
+          vr[t][i][0] = w.x;
+          vr[t][i][1] = w.y;
+        }
+      }
+    }
+  };
+
+  const int k = r & 3;                            // narrow: the block of a turn whose weights the lane computes; the piece
+                                                  // (k & 1) and the parity (k / 2) that its column stands for
+  const uint32_t pick = (k & 1 ? 0x0302u : 0x0100u) << (k & 2 ? 16 : 0) | (k & 2 ? 0x0C0Cu : 0x0C0C0000u);
+  float m = -INFINITY, l = 0.0f;
+  v4f acc[NA];
+#pragma unroll
+  for (int e = 0; e < NA; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  if (tiles > 0) {
+    load_k(0);
+    load_v(va, vea);
+  }
+
+  // q's pieces (while the first keys are on their way)
+  v8i qhi[NK], qlo[NK];
+  uint32_t qe[NK];                                // exponent of `hi` in the first byte, of `lo` in the second
+  {
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+    uint32_t e[NQ], other[NQ];
+    Pieces u[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const uint4 x = make_uint4(qx[i].x ^ flip, qx[i].y ^ flip, qx[i].z ^ flip, qx[i].w ^ flip);
+      const uint4 y = make_uint4(qy[i].x ^ flip, qy[i].y ^ flip, qy[i].z ^ flip, qy[i].w ^ flip);
+      // of the largest |q| of 32 channels, the lane's and its neighbour quarter's; an infinity or NaN makes NaN of the scores
+      const uint32_t largest = larger_xor16(largest_of(x, y));
+      e[i] = largest >= 0x7F80u ? 255u : static_cast<uint32_t>(max(static_cast<int>(largest >> 7) - 7, 6));
+      other[i] = __shfl_xor(e[i], 48);
+      u[i] = fp8_pieces(x, y, e[i]);
+    }
+    auto join = [](const uint32_t (&x)[4], const uint32_t (&y)[4]) {
+      return v8i{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
+                 static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
+    };
+    auto lower = [](uint32_t e) { return e == 255u ? e : e - 5; };
+    if constexpr (DP == 64) {
+      qhi[0] = join(u[0].hi, u[0].lo);
+      qe[0] = c == 0 ? e[0] : c == 1 ? other[0] : c == 2 ? lower(other[0]) : lower(e[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        qhi[i] = join(u[2 * i].hi, u[2 * i + 1].hi);
+        qlo[i] = join(u[2 * i].lo, u[2 * i + 1].lo);
+        const uint32_t own = c == 0 ? e[2 * i] : c == 1 ? other[2 * i] : c == 2 ? other[2 * i + 1] : e[2 * i + 1];
+        qe[i] = own | lower(own) << 8;
+      }
+    }
+  }
+
+  auto turn = [&](int tile, uint32_t (&vr)[BL][4][NV], uint32_t (&ve)[BL], uint32_t (&vn)[BL][4][NV],
+                  uint32_t (&ven)[BL]) __attribute__((always_inline)) {
+    // scores of keys 16 t + 4 c + i
+    v4f s[BL];
+#pragma unroll
+    for (int t = 0; t < BL; ++t) s[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int piece = 0; piece < (DP == 64 ? 1 : 2); ++piece)
+#pragma unroll
+        for (int t = 0; t < BL; ++t) {
+          const v8i keys = __builtin_shufflevector(kr[t][i], kr[t][i], 0, 1, 2, 3, -1, -1, -1, -1);
+          const int e = static_cast<int>(ke[t][i]), f = static_cast<int>(qe[i]);
+          s[t] = piece == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(keys, qhi[i], s[t], 4, 0, 0, e, 0, f)
+                            : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(keys, qlo[i], s[t], 4, 0, 0, e, 1, f);
+        }
+    const bool more = tile + 1 < tiles;
+    if (more) {
+      load_k(tile + 1);
+      if constexpr (V_AHEAD) load_v(vn, ven);
+    }
+    const int p0 = start(tile);
+    constexpr uint64_t blocks = (uint64_t(1) << BL) - 1;
+    const uint32_t paged = static_cast<uint32_t>(there >> (tile * BL) & blocks);
+    const bool whole = p0 >= sp.first && p0 + 16 * BL <= sp.len && paged == blocks;
+    constexpr int NS = NARROW ? 1 : BL;
+    v4f x[NS];
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[0][i] = k == 0 ? s[0][i] : k == 1 ? s[1][i] : k == 2 ? s[2][i] : s[3][i];
+    } else {
+#pragma unroll
+      for (int t = 0; t < BL; ++t) x[t] = s[t];
+    }
+    if (!whole) {
+      // positions from the first visible one on, unsigned
+      const uint32_t near = static_cast<uint32_t>(p0 + 4 * c - sp.first), seen = static_cast<uint32_t>(sp.len - sp.first);
+#pragma unroll
+      for (int j = 0; j < 4 * NS; ++j) {
+        const int t = NARROW ? k : j >> 2;
+        if (near + 16 * t + (j & 3) >= seen || !(paged >> t & 1u)) x[j >> 2][j & 3] = -INFINITY;
+      }
+      // unseen values have weight 0; only an exponent of 255, or one near it, would make them infinite or NaN
+#pragma unroll
+      for (int t = 0; t < BL; ++t) {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep |= near + 16 * t + i < seen ? 0xFFu << (8 * i) : 0u;
+        ve[t] &= paged >> t & 1u ? keep : 0u;
+      }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int j = 1; j < 4 * NS; ++j) top = fmaxf(top, x[j >> 2][j & 3]);
+    top *= sscale;
+    if (__any(top > m + kSlack)) {
+      if constexpr (NARROW) {
+        top = fmaxf(top, quad<kQuadXor1>(top));
+        top = fmaxf(top, quad<kQuadXor2>(top));
+      }
+      const float mn = fmaxf(m, max_xor32(max_xor16(top))), f = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < NA; ++e) acc[e] *= f;
+      m = mn;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    // weights, and as two bf16 pieces each: pairs of keys
+    uint32_t hi[NS][2], lo[NS][2];
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][i], sscale, -base));
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][i + 1], sscale, -base));
+        l += u + v;
+        const uint32_t w = bf16_pair(u, v);
+        hi[t][i / 2] = w;
+        lo[t][i / 2] = bf16_pair(u - __uint_as_float(w << 16), v - __uint_as_float(w & 0xFFFF0000u));
+      }
+    // the exponent of key 4 c + i of block t at a float's place; the conversion reads no other bits
+    auto exponent_of = [&](int t, int i) { return i == 3 ? ve[t] >> 1 : ve[t] << (23 - 8 * i); };
+    if constexpr (NARROW) {
+      // o^T += V^T S^T: slot 2 i + parity is key 4 c + i; column 4 head + piece + 2 parity
+      uint32_t z[4];                              // both pieces of a weight: `hi` in the low half
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] = i & 1 ? high_halves(hi[0][i >> 1], lo[0][i >> 1]) : low_halves(hi[0][i >> 1], lo[0][i >> 1]);
+      auto block = [&](auto tag) __attribute__((always_inline)) {
+        constexpr int T = decltype(tag)::value;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t from = quad_lane<T>(z[i]);
+          w[i] = __builtin_amdgcn_perm(from, from, pick);
+        }
+        const v8bf weights = bf8(w[0], w[1], w[2], w[3]);
+#pragma unroll
+        for (int e = 0; e < NA; ++e) {
+          uint32_t y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = fp4_pair(vr[T][i][e >> 2], exponent_of(T, i), e & 3);
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf8(y[0], y[1], y[2], y[3]), weights, acc[e], 0, 0, 0);
+        }
+      };
+      block(std::integral_constant<int, 0>());
+      block(std::integral_constant<int, 1>());
+      block(std::integral_constant<int, 2>());
+      block(std::integral_constant<int, 3>());
+    } else {
+      // o^T += V^T S^T: channel DC r + e of the lane's keys
+#pragma unroll
+      for (int g = 0; g < BL / 2; ++g) {
+        const v8bf ph = bf8(hi[2 * g][0], hi[2 * g][1], hi[2 * g + 1][0], hi[2 * g + 1][1]);
+        const v8bf pl = bf8(lo[2 * g][0], lo[2 * g][1], lo[2 * g + 1][0], lo[2 * g + 1][1]);
+#pragma unroll
+        for (int w = 0; w < DC / 2; ++w) {
+          uint32_t y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = fp4_pair(vr[2 * g + (j >> 2)][j & 3][w >> 2], exponent_of(2 * g + (j >> 2), j & 3), w & 3);
+          const v8bf even = bf8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7]));
+          const v8bf odd = bf8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7]));
+          acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph, acc[2 * w], 0, 0, 0);
+          acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph, acc[2 * w + 1], 0, 0, 0);
+          acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl, acc[2 * w], 0, 0, 0);
+          acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl, acc[2 * w + 1], 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (!V_AHEAD) {
+      if (more) load_v(vr, ve);
+    }
+  };
+  if constexpr (V_AHEAD) {
+    for (int tile = 0; tile < tiles; tile += 2) {
+      turn(tile, va, vea, vb, veb);
+      if (tile + 1 < tiles) turn(tile + 1, vb, veb, va, vea);
+    }
+  } else {
+    for (int tile = 0; tile < tiles; ++tile) turn(tile, va, vea, va, vea);
+  }
+  if constexpr (NARROW) {
+    // the pieces of a channel, and odd channels beside even ones, in the first lane of a head's four
+    v4f o[DC];
+#pragma unroll
+    for (int e = 0; e < NA; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float sum = acc[e][i] + quad<kQuadXor1>(acc[e][i]);
+        o[2 * e][i] = sum;
+        o[2 * e + 1][i] = quad<kQuadXor2>(sum);
+      }
+    l += quad<kQuadXor1>(l);
+    l += quad<kQuadXor2>(l);
+    finish_range<DP>(a, sp, m, l, o, smem, wave, head, k == 0 && head < nq, nq, D, head_row, range, 1.0f);
+  } else {
+    finish_range<DP>(a, sp, m, l, acc, smem, wave, r, r < nq, nq, D, head_row, range, 1.0f);
   }
 }
 
 // the ranges of a sequence into one result: one workgroup per (sequence, query
-// head, 4 LR channels of o), the ranges dealt out over its groups of LR lanes
-template <int LR, bool FP8>
+// head, 4 LR channels of o), the ranges dealt out over its groups of LR lanes.
+// (4-bit pages: the first ranges are requested before the maximum is known, and
+// the groups of a wave are added in it.)
+template <int LR, CacheType TYPE>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
+  constexpr bool FP8 = TYPE == CacheType::kFp8, FP4 = TYPE == CacheType::kFp4;
   constexpr int SLOTS = 256 / LR;
   __shared__ float4 so[SLOTS][LR];
   __shared__ float ss[SLOTS], st[4];
@@ -471,21 +859,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   if (sp.count <= 1) return;                      // written by the first launch
   const int64_t row = static_cast<int64_t>(blockIdx.x) * a.splits;
   const int slot = threadIdx.x / LR, d = (blockIdx.y * LR + threadIdx.x % LR) * 4, D = a.c.dim;
-  float top = -INFINITY;
-  for (int s = threadIdx.x; s < sp.count; s += 256) top = fmaxf(top, a.stat[2 * (row + s)]);
-#pragma unroll
-  for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-  if ((threadIdx.x & 63) == 0) st[threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
-  const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f;
-  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   // so many rows requested before the first is added
   constexpr int AHEAD = LR == 8 ? 4 : 8;
-  for (int s0 = slot; s0 < sp.count; s0 += SLOTS * AHEAD) {
-    float2 q[AHEAD];
-    float4 v[AHEAD];
+  float2 q[AHEAD];
+  float4 v[AHEAD];
+  auto request = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int s = s0 + u * SLOTS;
@@ -496,6 +874,20 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
         if (d < D) v[u] = *reinterpret_cast<const float4*>(a.part + (row + s) * D + d);
       }
     }
+  };
+  if constexpr (FP4) request(slot);
+  float top = -INFINITY;
+  for (int s = threadIdx.x; s < sp.count; s += 256) top = fmaxf(top, a.stat[2 * (row + s)]);
+#pragma unroll
+  for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  if ((threadIdx.x & 63) == 0) st[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = slot; s0 < sp.count; s0 += SLOTS * AHEAD) {
+    if (!FP4 || s0 != slot) request(s0);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const float f = __builtin_amdgcn_exp2f(q[u].x - ref);
@@ -506,16 +898,31 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
       o.w = __builtin_fmaf(v[u].w, f, o.w);
     }
   }
-  so[slot][threadIdx.x % LR] = o;
-  if (threadIdx.x % LR == 0) ss[slot] = sum;
+  int parts = SLOTS, part = slot;                 // sums in LDS, and this lane's
+  if constexpr (FP4 && LR < 64) {
+#pragma unroll
+    for (int i = LR; i < 64; i <<= 1) {
+      sum += __shfl_xor(sum, i);
+      o.x += __shfl_xor(o.x, i);
+      o.y += __shfl_xor(o.y, i);
+      o.z += __shfl_xor(o.z, i);
+      o.w += __shfl_xor(o.w, i);
+    }
+    parts = 4;
+    part = threadIdx.x >> 6;
+  }
+  if (parts == SLOTS || (threadIdx.x & 63) < LR) {
+    so[part][threadIdx.x % LR] = o;
+    if (threadIdx.x % LR == 0) ss[part] = sum;
+  }
   __syncthreads();
   if (slot != 0 || d >= D) return;
-  for (int s = 1; s < SLOTS; ++s) {
-    const float4 v = so[s][threadIdx.x % LR];
-    o.x += v.x;
-    o.y += v.y;
-    o.z += v.z;
-    o.w += v.w;
+  for (int s = 1; s < parts; ++s) {
+    const float4 w = so[s][threadIdx.x % LR];
+    o.x += w.x;
+    o.y += w.y;
+    o.z += w.z;
+    o.w += w.w;
     sum += ss[s];
   }
   const float n = sum > 0.0f || sum != sum ? (FP8 ? a.c.v_scale[h] : 1.0f) / sum : 0.0f;
@@ -535,8 +942,21 @@ struct Plan {
 
 constexpr int kOneRange = 512;
 
+// 4-bit pages: a turn of a workgroup is 256 positions
+Plan plan_of_fp4(const CacheParams& c, int q_heads, int max_len) {
+  auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
+  if (max_len <= 1024) return {static_cast<int>(up(max_len, 32)), 1};
+  const int64_t rows = rows_of(c, q_heads), heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16;
+  const int64_t want = 256 * (c.seqs < 4 ? c.seqs : 4);
+  int64_t n = (rows * max_len + want - 1) / want;
+  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 16 * heads, int64_t(256)}) n = n < least ? least : n;
+  n = up(n, 256) > kMaxChunk ? kMaxChunk : up(n, 256);
+  return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n)};
+}
+
 Plan plan_of(const CacheParams& c, CacheType type, int q_heads, int max_len) {
-  const bool fp8 = type != CacheType::kBf16;
+  if (type == CacheType::kFp4) return plan_of_fp4(c, q_heads, max_len);
+  const bool fp8 = type == CacheType::kFp8;
   auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
   const int64_t rows = rows_of(c, q_heads);
   // one range where a second launch would cost as much as the waves' turns (1.1 us for
@@ -558,20 +978,29 @@ Plan plan_of(const CacheParams& c, CacheType type, int q_heads, int max_len) {
 template <int DP, CacheType TYPE>
 hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
   const int nq = a.group < 16 ? a.group : 16;
-  const dim3 grid(static_cast<unsigned>(rows_of(a.c, a.q_heads) * a.splits)), block(64 * kAttnWaves);
   const int bytes = (2 * kAttnWaves * 16 + kAttnWaves * nq * (DP + 4)) * 4;
-  auto kernel = a.c.dim == DP ? paged_attention_kernel<DP, TYPE, true> : paged_attention_kernel<DP, TYPE, false>;
+  void (*kernel)(AttnArgs);
+  dim3 grid(static_cast<unsigned>(rows_of(a.c, a.q_heads) * a.splits));
+  if constexpr (TYPE == CacheType::kFp4) {
+    const int high = (a.splits + kGridRanges - 1) / kGridRanges;
+    grid = dim3(static_cast<unsigned>(a.c.heads * ((a.group + 15) / 16) * high), static_cast<unsigned>(a.c.seqs),
+                static_cast<unsigned>(a.splits < kGridRanges ? a.splits : kGridRanges));
+    if (a.group <= kNarrow) kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, true> : paged_attention_fp4_kernel<DP, false, true>;
+    else kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, false> : paged_attention_fp4_kernel<DP, false, false>;
+  } else {
+    constexpr bool FP8 = TYPE == CacheType::kFp8;
+    kernel = a.c.dim == DP ? paged_attention_kernel<DP, FP8, true> : paged_attention_kernel<DP, FP8, false>;
+  }
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a);
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * kAttnWaves), bytes, stream, a);
   const unsigned heads = static_cast<unsigned>(a.c.seqs) * a.q_heads;
-  constexpr bool FP8 = TYPE == CacheType::kFp8;
   if (a.splits > 16)
-    hipLaunchKernelGGL((attention_join_kernel<8, FP8>), dim3(heads, (a.c.dim + 31) / 32), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attention_join_kernel<8, TYPE>), dim3(heads, (a.c.dim + 31) / 32), dim3(256), 0, stream, a);
   else if (a.splits > 1)
-    hipLaunchKernelGGL((attention_join_kernel<DP / 4, FP8>), dim3(heads), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attention_join_kernel<DP / 4, TYPE>), dim3(heads), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
