@@ -115,7 +115,7 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int b) {
   s.len = static_cast<int>(min(static_cast<int64_t>(min(a.lengths[b], a.max_len)), reach));
   s.first = a.starts != nullptr ? max(a.starts[b], 0) : 0;
   s.base = s.first & ~31;
-  s.count = s.len > s.first ? (s.len - s.base + a.chunk - 1) / a.chunk : 0;
+  s.count = s.len > s.first ? (a.splits == 1 ? 1 : (s.len - s.base + a.chunk - 1) / a.chunk) : 0;
   return s;
 }
 
@@ -467,6 +467,13 @@ __device__ __forceinline__ uint32_t larger_xor16(uint32_t v) {
   return max(r[0], r[1]);
 }
 
+// the i-th of four (by bits: compared one by one they became branches)
+template <typename T>
+__device__ __forceinline__ T of_four(int i, T a, T b, T c, T d) {
+  const T low = i & 1 ? b : a, high = i & 1 ? d : c;
+  return i & 2 ? high : low;
+}
+
 template <int CTRL>
 __device__ __forceinline__ float quad(float v) {
   return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(v)), CTRL, 0xF, 0xF, true)));
@@ -495,7 +502,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   // first), sequences and ranges; the divisions are rare
   const int qtiles = (a.group + 15) / 16, b = blockIdx.y;
   int range = blockIdx.z, h = blockIdx.x, qt = 0;
-  if (static_cast<int>(gridDim.x) != a.c.heads * qtiles) {
+  if (a.splits > kGridRanges) {
     const int high = h / (a.c.heads * qtiles);
     h -= high * a.c.heads * qtiles;
     range += high * kGridRanges;
@@ -672,13 +679,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
     auto lower = [](uint32_t e) { return e == 255u ? e : e - 5; };
     if constexpr (DP == 64) {
       qhi[0] = join(u[0].hi, u[0].lo);
-      qe[0] = c == 0 ? e[0] : c == 1 ? other[0] : c == 2 ? lower(other[0]) : lower(e[0]);
+      qe[0] = of_four(c, e[0], other[0], lower(other[0]), lower(e[0]));
     } else {
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         qhi[i] = join(u[2 * i].hi, u[2 * i + 1].hi);
         qlo[i] = join(u[2 * i].lo, u[2 * i + 1].lo);
-        const uint32_t own = c == 0 ? e[2 * i] : c == 1 ? other[2 * i] : c == 2 ? other[2 * i + 1] : e[2 * i + 1];
+        const uint32_t own = of_four(c, e[2 * i], other[2 * i], other[2 * i + 1], e[2 * i + 1]);
         qe[i] = own | lower(own) << 8;
       }
     }
@@ -714,7 +721,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
     v4f x[NS];
     if constexpr (NARROW) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[0][i] = k == 0 ? s[0][i] : k == 1 ? s[1][i] : k == 2 ? s[2][i] : s[3][i];
+      for (int i = 0; i < 4; ++i) x[0][i] = of_four(k, s[0][i], s[1][i], s[2][i], s[3][i]);
     } else {
 #pragma unroll
       for (int t = 0; t < BL; ++t) x[t] = s[t];
