@@ -3,6 +3,7 @@
 A block is, in the library's operators,
 
     qkv = asp_matvec(block.qkv, h)                         projections on unquantized tokens
+    rope(q and k, pos, model.rope)                         rotary positions, in place (a model with a plan for them)
     kv_append(cache, k, v, seq, pos)                       the new keys and values into the pages
     a   = paged_attention(cache, q, pos + 1)               attention over everything stored
     x, h = block_norm(x, asp_matvec(block.out, a), ...)    gate, residual, norm in front of the FFN
@@ -13,7 +14,7 @@ with a float32 residual stream x and everything else bf16.  Weights are random, 
 of the action expert (1024 channels, 4096 in the FFN, rank 16).  Run as a program, it fills the caches with a prompt,
 records a step in a HIP graph and replays it, and prints the time of a step.
 
-    python examples/token_step.py [--blocks 8] [--sequences 4] [--prompt 200] [--steps 64]
+    python examples/token_step.py [--blocks 8] [--sequences 4] [--prompt 200] [--steps 64] [--rope] [--cache bf16|fp8|fp4]
 """
 
 from __future__ import annotations
@@ -23,13 +24,16 @@ import os
 import sys
 import time
 from dataclasses import dataclass
-from typing import List
+from typing import List, Optional
 
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import paper_2609_33269_amd as qwam  # noqa: E402
+
+
+CACHES = {"bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn, "fp4": torch.float4_e2m1fn_x2}
 
 
 @dataclass
@@ -50,6 +54,7 @@ class Model:
     dim: int
     first_norm: torch.Tensor  # bf16 [width]: in front of the first block
     blocks: List[Block]
+    rope: Optional[qwam.RopePlan] = None
 
 
 def random_layer(K: int, N: int, rank: int, gen: torch.Generator, group: int = 64) -> qwam.PackedLayer:
@@ -64,14 +69,15 @@ def random_layer(K: int, N: int, rank: int, gen: torch.Generator, group: int = 6
 
 
 def random_model(blocks: int, width: int = 1024, ffn: int = 4096, heads: int = 16, key_heads: int = 4, rank: int = 16,
-                 seed: int = 0) -> Model:
+                 seed: int = 0, rope: bool = False) -> Model:
     g = torch.Generator().manual_seed(seed)
     dim = width // heads
     near_one = lambda *s: (1 + 0.1 * torch.randn(*s, generator=g)).bfloat16().cuda()  # noqa: E731
     layer = lambda K, N: random_layer(K, N, rank, g)  # noqa: E731
     return Model(width, heads, key_heads, dim, near_one(width),
                  [Block(layer(width, (heads + 2 * key_heads) * dim), layer(width, width), layer(width, ffn), layer(ffn, width),
-                        0.5 * near_one(2, width), near_one(2, width)) for _ in range(blocks)])
+                        0.5 * near_one(2, width), near_one(2, width)) for _ in range(blocks)],
+                 qwam.rope_plan((dim,)) if rope else None)
 
 
 def empty_caches(model: Model, sequences: int, positions: int, page: int = 64, dtype=torch.bfloat16) -> List[qwam.PagedCache]:
@@ -94,6 +100,9 @@ def step(model: Model, caches: List[qwam.PagedCache], x: torch.Tensor, seq: torc
     _, h = qwam.block_norm(x, weight=model.first_norm)
     for b, cache in zip(model.blocks, caches):
         qkv = qwam.asp_matvec(b.qkv, h)
+        if model.rope is not None:
+            qk = qkv[:, :(H + KH) * D].unflatten(1, (-1, D))
+            qwam.rope(qk, pos[:, None], model.rope, out=qk)
         q, k, v = (qkv[:, i:j].unflatten(1, (-1, D)) for i, j in ((0, H * D), (H * D, (H + KH) * D), ((H + KH) * D, (H + 2 * KH) * D)))
         qwam.kv_append(cache, k, v, seq, pos)
         a = qwam.paged_attention(cache, q, lengths)
@@ -109,9 +118,11 @@ def main() -> None:
     p.add_argument("--sequences", type=int, default=4)
     p.add_argument("--prompt", type=int, default=200)
     p.add_argument("--steps", type=int, default=64)
+    p.add_argument("--rope", action="store_true", help="rotary positions")
+    p.add_argument("--cache", choices=CACHES, default="bf16")
     a = p.parse_args()
-    model = random_model(a.blocks)
-    caches = empty_caches(model, a.sequences, a.prompt + a.steps + 4)
+    model = random_model(a.blocks, rope=a.rope)
+    caches = empty_caches(model, a.sequences, a.prompt + a.steps + 4, dtype=CACHES[a.cache])
     g = torch.Generator(device="cuda").manual_seed(1)
     seq = torch.arange(a.sequences, dtype=torch.int32, device="cuda")
     # a prompt's keys and values, as prefill would leave them

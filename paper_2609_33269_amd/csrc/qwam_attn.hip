@@ -407,16 +407,17 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 
 // The same over 4-bit pages, for which the loads are so narrow that the instructions of a turn are the bound, so that
 // they are counted here:
-//   * A wave takes 64 positions a turn, in blocks of 16 (32 for heads above 128 in groups above 4), so that the maximum,
-//     the test for a new one and the loop are paid once for them.
+//   * A wave takes 64 positions a turn, in blocks of 16 (32 for heads above 128), so that the maximum, the test for a new
+//     one and the loop are paid once for them.
 //   * Keys are multiplied as they are stored (v_mfma_scale_f32_16x16x128_f8f6f4: e2m1 with a power of two for 32 channels
 //     is its operand).  q enters as two e4m3 pieces, each of 4 bits of its 8: q exactly, where it is within 2^-15 of the
 //     largest of its 32 channels, and to 2^-22 of that below.
 //   * Values are converted to bf16, which is exact and applies the power of two, and weighted by two bf16 pieces.  With up
-//     to 4 query heads the 16 columns of that product hold each head four times, for both pieces of its weights and for
-//     even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them, and a lane
-//     needs no transposing.  The same four lanes share a head's 64 weights, 16 each.  (8 x 3 heads of 128: turns of 264
-//     instead of 500 instructions.)
+//     to 4 query heads (the narrow form) the 16 columns of that product hold each head four times, for both pieces of its
+//     weights and for even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them,
+//     and a lane needs no transposing.  The same four lanes share a head's 64 weights, 16 each.  (8 x 3 heads of 128, a
+//     turn of a wave 310 instead of 460 instructions; 16 ragged contexts up to 4096 12.1 us, in the wide form 13.5; 4 up
+//     to 16384, 16 heads of 64, 13.9, 16.2.)
 //   * Where a block of 16 positions lies is computed once, a lane each, and handed out by readlane; addresses are a
 //     scalar base and a lane's 32-bit offset that stays.
 //   * A new maximum counts from 2^kSlack above the old one on: weights stay below 2^kSlack, and o and the sum are
@@ -488,7 +489,8 @@ __device__ __forceinline__ uint32_t quad_lane(uint32_t z) {
 
 template <int DP, bool FULL, bool NARROW>
 __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_attention_fp4_kernel(AttnArgs a) {
-  constexpr int BL = DP == 256 && !NARROW ? 2 : 4;        // blocks of 16 positions a turn
+  static_assert(!NARROW || DP <= 128, "the narrow form takes heads up to 128");
+  constexpr int BL = DP == 256 ? 2 : 4;           // blocks of 16 positions a turn
   constexpr int DC = DP / 16;                     // channels of V in a lane
   constexpr int NK = (DP + 127) / 128;            // 32 channels of a key in a lane; products over 128 channels
   constexpr int NV = (DC + 7) / 8;                // words of V in a lane, per key
@@ -592,7 +594,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   const bool has_v = FULL || DC * r < D;
 
   v4i kr[BL][NK];
-  constexpr bool V_AHEAD = NARROW && DP <= 128;   // values come a turn ahead too
+  constexpr bool V_AHEAD = NARROW;                // values come a turn ahead too
   uint32_t ke[BL][NK], va[BL][4][NV], vea[BL], vb[BL][4][NV], veb[BL];
   int64_t code_at[BL], exp_at[BL];                // of the tile whose keys were loaded last
   // a scalar base and a lane's offset in one load; the asm keeps the offset's extension to 64 bits beside the load, where
@@ -992,8 +994,11 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
     const int high = (a.splits + kGridRanges - 1) / kGridRanges;
     grid = dim3(static_cast<unsigned>(a.c.heads * ((a.group + 15) / 16) * high), static_cast<unsigned>(a.c.seqs),
                 static_cast<unsigned>(a.splits < kGridRanges ? a.splits : kGridRanges));
-    if (a.group <= kNarrow) kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, true> : paged_attention_fp4_kernel<DP, false, true>;
-    else kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, false> : paged_attention_fp4_kernel<DP, false, false>;
+    kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, false> : paged_attention_fp4_kernel<DP, false, false>;
+    // (heads above 128: the narrow form is no faster, 32768 positions of 8 of 256 18.7 us to 18.8, and has too many registers)
+    if constexpr (DP <= 128) {
+      if (a.group <= kNarrow) kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, true> : paged_attention_fp4_kernel<DP, false, true>;
+    }
   } else {
     constexpr bool FP8 = TYPE == CacheType::kFp8;
     kernel = a.c.dim == DP ? paged_attention_kernel<DP, FP8, true> : paged_attention_kernel<DP, FP8, false>;

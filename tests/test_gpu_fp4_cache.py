@@ -516,3 +516,133 @@ def test_refusals():
     with pytest.raises(ValueError, match="requires a gradient, which kv_read does not have"):
         P.kv_read(wide, z, L)
     assert wide.k.dtype == FP8
+
+
+# ---- beyond the ordinary ----
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("G", [3, 8])
+def test_queries_of_unlike_size(D, G):
+    """Channels of q up to 2^24 apart within the 32 that share a scale: what lies 2^15 below the largest is held to 2^-22 of
+    it, which adds that times the sum of |k| of the 32 channels to a score's error."""
+    lengths = [300, 40, 700]
+    cache = _cache(lengths, 2, D, 16)
+    g = torch.Generator().manual_seed(D)
+    q = (torch.randn(3, 2 * G, D, generator=g) * 2.0 ** -torch.randint(0, 25, (3, 2 * G, D), generator=g)).bfloat16().cuda()
+    out = P.paged_attention(cache, q, _int(lengths))
+    ref = _as_bf16(cache)
+    K, V, table = ref.k.cpu().double(), ref.v.cpu().double(), cache.table.cpu()
+    for b, n in enumerate(lengths):
+        pos = torch.arange(n)
+        pg = table[b, pos // 16].long()
+        k, v = K[pg, :, pos % 16], V[pg, :, pos % 16]
+        qq = q[b].cpu().double().reshape(2, G, D)
+        s = torch.einsum("hgd,nhd->hgn", qq, k) * D ** -0.5
+        off = 2.0 ** -19 * torch.einsum("hgd,nhd->hgn", qq.abs(), k.abs()) * D ** -0.5
+        top = qq.abs().unflatten(-1, (-1, 32)).amax(-1)
+        off = (off + 2.0 ** -22 * torch.einsum("hgc,nhc->hgn", top, k.abs().unflatten(-1, (-1, 32)).sum(-1)) * D ** -0.5).amax(-1, keepdim=True)
+        w = torch.softmax(s, -1)
+        o, mag = torch.einsum("hgn,nhd->hgd", w, v), torch.einsum("hgn,nhd->hgd", w, v.abs())
+        e = (out[b].cpu().double().reshape(2, G, D) - o).abs()
+        assert (e <= 1.01 * 2.0 ** -8 * o.abs() + (2.0 ** -15 + 2 * off) * mag).all(), f"sequence {b}"
+
+
+@pytest.mark.parametrize("D,G", [(64, 2), (64, 6), (128, 3), (128, 16), (256, 2)])
+def test_queries_that_are_not_finite(D, G):
+    """An infinity or NaN makes that head's result NaN, and no other's."""
+    lengths = [300, 40]
+    cache = _cache(lengths, 2, D, 16)
+    q = _q(2, 2 * G, D)
+    want = P.paged_attention(cache, q, _int(lengths))
+    for bad in (INF, -INF, NAN):
+        p = q.clone()
+        p[0, 1, 17] = bad
+        got = P.paged_attention(cache, p, _int(lengths))
+        assert got[0, 1].isnan().all()
+        got[0, 1] = want[0, 1]
+        assert torch.equal(got, want)
+    zero = torch.zeros_like(q)
+    _check(_as_bf16(cache), zero, lengths, P.paged_attention(cache, zero, _int(lengths)))
+    tiny = (q.float() * 2.0 ** -120).bfloat16()
+    _check(_as_bf16(cache), tiny, lengths, P.paged_attention(cache, tiny, _int(lengths)))
+
+
+def test_rows_that_run_backwards():
+    """The C interface takes strides of either sign: pages, heads and rows in the opposite order in memory."""
+    import ctypes
+    lengths, H, D, page = [100, 3, 70], 3, 128, 16
+    cache = _cache(lengths, H, D, page)
+    n = cache.k.shape[0]
+    k, v = (c.view(torch.uint8).flip(0, 1, 2).contiguous() for c in (cache.k, cache.v))
+    q, L = _q(3, 2 * H, D), _int(lengths)
+    want = P.paged_attention(cache, q, L)
+    c = cache.c_struct()
+    last = k.numel() - D // 2
+    c.k, c.v = k.data_ptr() + last, v.data_ptr() + last
+    c.page_stride, c.head_stride, c.row_stride = -H * page * D // 2, -page * D // 2, -D // 2
+    out = torch.full_like(want, NAN)
+    lib = Q.lib()
+    s = torch.cuda.current_stream().cuda_stream
+    assert n > 3 and lib.qwam_paged_attention_workspace(ctypes.byref(c), 2 * H, 112) == 0
+    assert lib.qwam_paged_attention(ctypes.byref(c), 2 * H, q.data_ptr(), q.stride(0), L.data_ptr(), None, 112, D ** -0.5, out.data_ptr(), None, 0, s) == 0
+    assert torch.equal(out, want)
+    seq, pos = _int([0, 1, 2, 2]), _int([99, 2, 0, 69])
+    x = torch.randn(2, 4, H, D, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    P.kv_append(cache, x[0], x[1], seq, pos)
+    ke, ve = (e.view(torch.uint8).clone() for e in (cache.k_scale, cache.v_scale))
+    c.k_scale, c.v_scale = ke.data_ptr(), ve.data_ptr()
+    assert lib.qwam_kv_append(ctypes.byref(c), 4, x[0].data_ptr(), H * D, x[1].data_ptr(), H * D, seq.data_ptr(), pos.data_ptr(), s) == 0
+    assert torch.equal(k.flip(0, 1, 2), cache.k.view(torch.uint8)) and torch.equal(v.flip(0, 1, 2), cache.v.view(torch.uint8))
+    got = torch.empty_like(x)
+    assert lib.qwam_kv_read(ctypes.byref(c), 4, seq.data_ptr(), pos.data_ptr(), got[0].data_ptr(), H * D, got[1].data_ptr(), H * D, s) == 0
+    assert all(torch.equal(a, b) for a, b in zip(got, P.kv_read(cache, seq, pos)))
+
+
+def test_many_tokens():
+    """More than 2^31 keys in a call: appended and read back, the ends checked."""
+    H, D, page, n = 32, 128, 4096, 2 ** 19 + 5
+    pages = -(-n // page)
+    cache = P.new_cache(pages, H, D, 1, pages, page, FP4)
+    cache.table[0] = torch.arange(pages - 1, -1, -1)
+    x = torch.empty(n, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    seq, pos = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    P.kv_append(cache, x, x, seq, pos)
+    k, v = P.kv_read(cache, seq, pos)
+    small = P.new_cache(2, H, D, 1, 1, 64, FP4)
+    small.table[0] = 1
+    for at in (slice(0, 40), slice(n // 2, n // 2 + 40), slice(n - 40, n)):
+        P.kv_append(small, x[at], x[at], seq[:40], pos[:40])
+        want, _ = P.kv_read(small, seq[:40], pos[:40])
+        assert torch.equal(k[at], want) and torch.equal(v[at], want)
+    del x, k, v, cache
+    torch.cuda.empty_cache()
+
+
+def test_two_streams():
+    """Calls on two streams at once, each with a workspace of its own, and two graphs replayed at once."""
+    lengths = [9000, 100, 4000]
+    cache = _cache(lengths, 2, 128, 64)
+    qs = [_q(3, 8, 128, s) for s in (1, 2)]
+    L = _int(lengths)
+    want = [P.paged_attention(cache, q, L) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            got[i].append(P.paged_attention(cache, qs[i], L, stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(w, g) for w, gs in zip(want, got) for g in gs)
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in qs], []
+    for graph, q in zip(graphs, qs):
+        with torch.cuda.graph(graph):
+            outs.append(P.paged_attention(cache, q, L))
+    for _ in range(4):
+        for o in outs:
+            o.fill_(NAN)
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(w, o) for w, o in zip(want, outs))

@@ -174,6 +174,22 @@ def test_turns_undo_each_other():
         assert (back - x).abs().max() <= 8 * 2.0 ** -21       # (two turns, each within 2^-22 + 2^-23 + 2^-24 of |x_a| + |x_b| < 8)
 
 
+def test_many_values():
+    """2^32 values in one call, the ends and the middle checked."""
+    plan, T, H, D, P_ = P.rope_plan((44, 42, 42), interleaved=True), 2 ** 19, 64, 128, 2 ** 12
+    pos = _pos(P_, 3)
+    x = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    at = [slice(i, i + 16) for i in (0, T // 2 - 16, T // 2, T - 16)]
+    kept = [x[i].clone() for i in at]
+    assert P.rope(x, pos, plan, out=x) is x
+    for i, w in zip(at, kept):
+        _check(w, pos.roll(-i.start, 0)[:16].contiguous(), plan, x[i])
+    with pytest.raises(Q.QwamError, match="at most 2\\^32"):
+        P.rope(x[:1].expand(T + P_, H, D), pos, plan)
+    del x
+    torch.cuda.empty_cache()
+
+
 # ---- gradients ----
 
 @pytest.mark.parametrize("f32", [False, True])
