@@ -103,19 +103,40 @@ struct AttnArgs {
   float *part, *stat;             // [seqs][q_heads][splits][dim], and (maximum, sum) likewise
   int q_heads, group, max_len, chunk, splits;
   float scale;
+  int least;                      // positions of the shortest range over 4-bit pages
 };
+constexpr int kTurn = 256;        // positions of a workgroup's turn over 4-bit pages
 
 // visible positions of a sequence: [first, len), and where its ranges start (all 32 bits: len + kMaxChunk does not pass 2^31)
 struct Span {
-  int first, len, base, count;    // count: ranges
+  int first, len, base, count, chunk;     // count: ranges; chunk: positions of one
 };
+// Over bf16 and fp8 pages a range is as long as the call laid out for the longest contexts.  Over 4-bit pages a context below an
+// eighth of those, or the only one of a call, has shorter ones: as many as the call has for the longest (a quarter of that
+// in a batch, whose sequences share the chip), none shorter than the call's least.  One context of 4096 positions in a table
+// that reaches 131072 takes 8.1 us, with the call's ranges 20.4; four of 60 to 9000 there 12.1 and 21.8 (8 x 3 heads of 128).
+// As many for every sequence of a batch took 8 ragged ones up to 16000, 16 x 2 heads of 256, from 39.7 to 47.4.
+template <bool FP4>
 __device__ __forceinline__ Span span_of(const AttnArgs& a, int b) {
-  Span s;
   const int64_t reach = static_cast<int64_t>(a.c.table_width) << a.c.page_bits;
+  Span s;
   s.len = static_cast<int>(min(static_cast<int64_t>(min(a.lengths[b], a.max_len)), reach));
   s.first = a.starts != nullptr ? max(a.starts[b], 0) : 0;
   s.base = s.first & ~31;
-  s.count = s.len > s.first ? (a.splits == 1 ? 1 : (s.len - s.base + a.chunk - 1) / a.chunk) : 0;
+  s.chunk = a.chunk;
+  if constexpr (FP4) {
+    s.count = s.len > s.first ? 1 : 0;
+    if (a.splits > 1 && s.count) {
+      const uint32_t n = s.len - s.base;
+      if (a.c.seqs == 1 || n < static_cast<uint32_t>(a.max_len) / 8) {
+        const uint32_t ranges = a.c.seqs == 1 ? a.splits : (a.splits + 3) / 4, each = (n + ranges - 1) / ranges;
+        s.chunk = min(a.chunk, max(static_cast<int>((each + kTurn - 1) / kTurn * kTurn), a.least));
+      }
+      s.count = static_cast<int>((n + s.chunk - 1) / s.chunk);
+    }
+  } else {
+    s.count = s.len > s.first ? (s.len - s.base + a.chunk - 1) / a.chunk : 0;
+  }
   return s;
 }
 
@@ -210,7 +231,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
   const int qtiles = (a.group + 15) / 16, rows = a.c.seqs * a.c.heads * qtiles;
   const int range = blockIdx.x / rows, bh = blockIdx.x % rows / qtiles, qt = blockIdx.x % qtiles;
   const int h = bh % a.c.heads, b = bh / a.c.heads;
-  const Span sp = span_of(a, b);
+  const Span sp = span_of<false>(a, b);
   if (range >= max(sp.count, 1)) return;
   const int q0 = qt * 16, nq = min(16, a.group - q0);   // query heads of this tile
   const int64_t head_row = static_cast<int64_t>(b) * a.q_heads + h * a.group + q0;
@@ -514,7 +535,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
     h = ht / qtiles;
     qt = ht - h * qtiles;
   }
-  const Span sp = span_of(a, b);
+  const Span sp = span_of<true>(a, b);
   if (range >= max(sp.count, 1)) return;
   const int q0 = qt * 16, nq = min(16, a.group - q0);
   const int64_t head_row = static_cast<int64_t>(b) * a.q_heads + h * a.group + q0;
@@ -525,7 +546,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   }
 
   // positions [r0, r1) in tiles of 16 BL, every `waves`-th of them this wave's
-  const int r0 = sp.base + range * a.chunk, r1 = min(r0 + a.chunk, sp.len);
+  const int r0 = sp.base + range * sp.chunk, r1 = min(r0 + sp.chunk, sp.len);
   const int tiles = max(0, (r1 - r0 + 16 * BL - 1) / (16 * BL) - wave + waves - 1) / waves;
   auto start = [&](int tile) { return r0 + 16 * BL * (tile * waves + wave); };
 
@@ -536,7 +557,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   {
     const int p = start(lane / BL) + 16 * (lane % BL);
     int pid = -1;
-    if (p < r0 + a.chunk && (p >> a.c.page_bits) < a.c.table_width)       // (does not wait for the length)
+    if (p < r0 + sp.chunk && (p >> a.c.page_bits) < a.c.table_width)
       pid = a.c.table[static_cast<int64_t>(b) * a.c.table_width + (p >> a.c.page_bits)];
     if (pid >= a.c.pages || p >= r1) pid = -1;
     there = __ballot(pid >= 0);
@@ -866,7 +887,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   __shared__ float4 so[SLOTS][LR];
   __shared__ float ss[SLOTS], st[4];
   const int b = blockIdx.x / a.q_heads, hq = blockIdx.x % a.q_heads, h = hq / a.group;
-  const Span sp = span_of(a, b);
+  const Span sp = span_of<FP4>(a, b);
   if (sp.count <= 1) return;                      // written by the first launch
   const int64_t row = static_cast<int64_t>(blockIdx.x) * a.splits;
   const int slot = threadIdx.x / LR, d = (blockIdx.y * LR + threadIdx.x % LR) * 4, D = a.c.dim;
@@ -948,21 +969,26 @@ int64_t rows_of(const CacheParams& c, int q_heads) {
 
 // How a call is laid out: positions of a workgroup (a range), ranges of the longest sequence.
 struct Plan {
-  int chunk, splits;
+  int chunk, splits, least;
 };
 
 constexpr int kOneRange = 512;
 
-// 4-bit pages: a turn of a workgroup is 256 positions
+// 4-bit pages: a call's ranges of turns of a workgroup.  One range up to 1024 positions (64 x 8 heads of 1024 12.0 us, in
+// two ranges 15.5; one sequence of 16 heads of 64 7.6, in four 7.7).  Else workgroups for every CU once for one sequence
+// (one context of 32768 13.6 us; for twice as many 14.4, for half 17.6), and as often as there are sequences up to four times,
+// whose lengths differ (32 ragged ones up to 8192 20.4 us, with half as many 23.4); no more than 256 ranges to join, and
+// partial results at most half of what is read.
 Plan plan_of_fp4(const CacheParams& c, int q_heads, int max_len) {
   auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
   if (max_len <= 1024) return {static_cast<int>(up(max_len, 32)), 1};
   const int64_t rows = rows_of(c, q_heads), heads = q_heads / c.heads < 16 ? q_heads / c.heads : 16;
   const int64_t want = 256 * (c.seqs < 4 ? c.seqs : 4);
   int64_t n = (rows * max_len + want - 1) / want;
-  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 16 * heads, int64_t(256)}) n = n < least ? least : n;
-  n = up(n, 256) > kMaxChunk ? kMaxChunk : up(n, 256);
-  return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n)};
+  for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 16 * heads, int64_t(kTurn)}) n = n < least ? least : n;
+  n = up(n, kTurn) > kMaxChunk ? kMaxChunk : up(n, kTurn);
+  // (512 rows of 500 positions in a table for 32768: one range each 11.2 us, two 19.7)
+  return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n), rows < 256 ? kTurn : 4 * kTurn};
 }
 
 Plan plan_of(const CacheParams& c, CacheType type, int q_heads, int max_len) {
@@ -1046,7 +1072,7 @@ hipError_t launch_paged_attention(const CacheParams& c, CacheType type, int q_he
   float* const part = static_cast<float*>(workspace);
   const AttnArgs a = {c, q, q_stride, lengths, starts, out, part,
                       p.splits > 1 ? part + static_cast<int64_t>(c.seqs) * q_heads * p.splits * c.dim : nullptr,
-                      q_heads, q_heads / c.heads, max_len, p.chunk, p.splits, scale};
+                      q_heads, q_heads / c.heads, max_len, p.chunk, p.splits, scale, p.least};
   auto run = [&](auto tag) {
     constexpr CacheType TYPE = decltype(tag)::value;
     return c.dim <= 64 ? launch_attention<64, TYPE>(a, stream) : c.dim <= 128 ? launch_attention<128, TYPE>(a, stream)

@@ -476,6 +476,15 @@ def test_graph_over_a_wide_table():
         _check(ref, q, now, out)
 
 
+@pytest.mark.parametrize("lengths", [[1], [100], [1025], [4096], [9000], [20000], [60, 9000, 500, 3000], [4000] * 9, [16385, 16383, 2049, 2047]])
+def test_short_contexts_of_wide_tables(lengths):
+    """Ranges go by each context, not by the table's reach: whole contexts, windows of them, and a bound on all."""
+    for H, G, D in ((1, 3, 128), (2, 5, 64)):
+        _run(lengths, H, G, D, 64, width=2048)
+        _run(lengths, H, G, D, 64, width=2048, starts=[max(0, n - 1500) for n in lengths])
+        _run(lengths, H, G, D, 64, width=2048, max_len=5000)
+
+
 def test_refusals():
     cache = _cache([30, 40], 2, 64, 16)
     q, L, z = _q(2, 4, 64), _int([30, 40]), _int([0, 0])
