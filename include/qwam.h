@@ -476,7 +476,8 @@ qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *
  *   tokens   in  as for qwam_kv_append
  *   seq, pos in  int32 [tokens]
  *   k, v     out bf16, laid out as qwam_kv_append's; with more than one token
- *                |k_stride|, |v_stride| >= heads * dim
+ *                |k_stride|, |v_stride| >= heads * dim; apart from each other and
+ *                from the cache
  */
 qwam_status qwam_kv_read(const qwam_cache *c, int32_t tokens, const int32_t *seq, const int32_t *pos, uint16_t *k,
                          int64_t k_stride, uint16_t *v, int64_t v_stride, void *stream);
@@ -491,6 +492,12 @@ qwam_status qwam_kv_read(const qwam_cache *c, int32_t tokens, const int32_t *seq
  * Visible scores of -inf have weight 0, and where all are -inf o is zeros; one
  * of +inf or NaN makes o[b][h] NaN.  An infinite or NaN value makes its channel
  * of its heads' o infinite or NaN (which of the two is not specified).
+ * fp4: q enters the scores exactly where |q| is within 2^-14 of the largest of its
+ * 32 channels (q's groups are the cache's), and to 2^-22 of that below; an infinity
+ * or NaN in q makes o[b][h] NaN.  A group with E = 255 is NaN: in a key it makes the
+ * results of its heads NaN, in a value those of its 32 channels.  (E of 253 and 254,
+ * which qwam_kv_append does not write, count values past bf16's range as infinities
+ * of any channel of their group.)
  *   q        in  bf16, sequence b's q_heads x dim values at b * q_stride,
  *                16-byte aligned, q_stride % 8 == 0
  *   q_heads  in  a multiple of heads, at most 64 per key head, seqs * q_heads <= 2^22
@@ -539,7 +546,7 @@ typedef struct qwam_rope_plan {
  * once; channels that do not turn are copied.
  *   tokens   in  >= 1, tokens % positions == 0, tokens * heads * dim <= 2^32
  *   x        in  bf16 or float, token t's heads x dim values at t * x_stride (aligned to its
- *                elements; 16-byte aligned rows and widths of 8 are faster)
+ *                elements; even widths and rows aligned to two elements are faster)
  *   y        out as x; may be x itself with the same stride, and must not overlap it otherwise;
  *                with more than one token |y_stride| >= heads * dim
  */

@@ -287,8 +287,9 @@ def _rows(t: torch.Tensor, name: str, shape) -> int:
 
 def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None) -> None:
     """qwam_kv_append: k, v bf16 [tokens][heads][dim] to position pos[t] of sequence seq[t] (int32 [tokens]), rounded to
-    float8 where the pages are, and quantized to 4 bits with a power of two for 32 channels where they are float4.  Tokens without a place (pos < 0, no page) are not stored.  There is no gradient: tensors
-    that require one are refused where autograd records."""
+    float8 where the pages are, and quantized to 4 bits with a power of two for 32 channels where they are float4.  Tokens
+    without a place (pos < 0, no page) are not stored.  There is no gradient: tensors that require one are refused where
+    autograd records."""
     if stream is None:
         st = (_q._call or _q._native()).append(cache, k, v, seq, pos)
         if st is not None:
@@ -310,7 +311,7 @@ def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Te
 def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, stream=None):
     """qwam_kv_read: the stored keys and values of positions pos[t] of sequences seq[t] (int32 [tokens]) as bf16
     [tokens][heads][dim] each; zeros where kv_append would not store (pos < 0, no page).  `out` = (k, v) gives the outputs,
-    whose rows may be apart.  There is no gradient, as for kv_append."""
+    whose rows may be apart, and which must not overlap.  There is no gradient, as for kv_append."""
     if stream is None:
         done = (_q._call or _q._native()).read(cache, seq, pos, out)
         if done is not None:

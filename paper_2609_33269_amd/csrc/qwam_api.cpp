@@ -609,6 +609,7 @@ qwam_status qwam_kv_read(const qwam_cache* c, int32_t tokens, const int32_t* seq
   const int64_t width = static_cast<int64_t>(c->heads) * c->dim;
   if (!rows_apart(tokens, k_stride, width) || !rows_apart(tokens, v_stride, width))
     return fail(QWAM_ERR_INVALID_ARG, "%s: k_stride and v_stride must be at least heads * dim apart", fn);
+  if (k == v) return fail(QWAM_ERR_INVALID_ARG, "%s: k and v are one output", fn);
   if ((s = check_device(fn)) != QWAM_OK) return s;
   return launched(fn, qwam::launch_kv_read(cp, type_of(c), tokens, seq, pos, k, k_stride, v, v_stride,
                                            static_cast<hipStream_t>(stream)));

@@ -46,6 +46,12 @@ def test_read_refusals(lib, type_):  # noqa: F811
     assert lib.qwam_last_error().startswith(b"qwam_kv_read")
 
 
+def test_read_wants_two_outputs(lib):  # noqa: F811
+    for n in (1, 3):
+        assert _read(lib, _cache4(), n=n, k=FAKE, v=FAKE) == INVALID
+        assert lib.qwam_last_error() == b"qwam_kv_read: k and v are one output"
+
+
 def _plan(**kw):
     c = Q.QwamRopePlanC()
     base = dict(heads=4, dim=64, pairs=32, interleaved=0, axes=3, positions=6, pos_f32=0, x_f32=0, pos=FAKE, inv_freq=FAKE, axis=FAKE)
