@@ -1,6 +1,6 @@
 // The paged key-value cache: new keys and values into the pages
-// (qwam_kv_append), and the attention of one new token per sequence
-// (qwam_paged_attention):
+// (qwam_kv_append; into 4-bit ones in qwam_kv.hip), and the attention of one new
+// token per sequence (qwam_paged_attention):
 //   o[h] = sum_p softmax_p(scale q[h] . K[p]) V[p], the G = q_heads / heads query heads of a key head together.
 // Every key and value is read once for each 16 query heads of its key head (once
 // for G <= 16) and serves those; that is far below what the matrix cores need to be
@@ -431,8 +431,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 //   * A wave takes 64 positions a turn, in blocks of 16 (32 for heads above 128), so that the maximum, the test for a new
 //     one and the loop are paid once for them.
 //   * Keys are multiplied as they are stored (v_mfma_scale_f32_16x16x128_f8f6f4: e2m1 with a power of two for 32 channels
-//     is its operand).  q enters as two e4m3 pieces, each of 4 bits of its 8: q exactly, where it is within 2^-15 of the
-//     largest of its 32 channels, and to 2^-22 of that below.
+//     is its operand; 13% fewer instructions than by bf16).  q enters as two e4m3 pieces, each of 4 bits of its 8: q
+//     exactly, where it is within 2^-14 of the largest of its 32 channels, and to 2^-22 of that below.
 //   * Values are converted to bf16, which is exact and applies the power of two, and weighted by two bf16 pieces.  With up
 //     to 4 query heads (the narrow form) the 16 columns of that product hold each head four times, for both pieces of its
 //     weights and for even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them,
@@ -443,6 +443,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 //     scalar base and a lane's 32-bit offset that stays.
 //   * A new maximum counts from 2^kSlack above the old one on: weights stay below 2^kSlack, and o and the sum are
 //     rescaled in a few turns rather than in most (with 16 heads, one of them has a new maximum in most turns).
+// Measured, 8 x 3 heads of 128: two contexts up to 131072 41.4 us (38.3 of it this kernel, 4.6 TB/s), one of 32768 13.4 us, 16
+// ragged ones up to 4096 13.0 us (two turns of their workgroups of 1 us each behind launch, lengths, table and first keys,
+// and a join of 3.5); one of 77, 16 heads of 64, 4.5 us in a graph; windows of 6001 positions of 5 sequences, 2 x 16 heads
+// of 256, 13.2 us.
 constexpr float kSlack = 8.0f;
 constexpr int kNarrow = 4;              // query heads of a key head that the narrow form takes
 constexpr int kGridRanges = 32768;      // ranges in the grid's last dimension; more of them stand behind the heads
@@ -879,7 +883,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
 // the ranges of a sequence into one result: one workgroup per (sequence, query
 // head, 4 LR channels of o), the ranges dealt out over its groups of LR lanes.
 // (4-bit pages: the first ranges are requested before the maximum is known, and
-// the groups of a wave are added in it.)
+// the groups of a wave are added in it: 512 ranges of two contexts up to 131072
+// 53 us in all, 67 without.)
 template <int LR, CacheType TYPE>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   constexpr bool FP8 = TYPE == CacheType::kFp8, FP4 = TYPE == CacheType::kFp4;

@@ -485,6 +485,11 @@ def test_short_contexts_of_wide_tables(lengths):
         _run(lengths, H, G, D, 64, width=2048, max_len=5000)
 
 
+def test_short_contexts_of_many_rows():
+    """Where the sequences' heads fill the chip, a short context stays in one range."""
+    _run([500, 1500, 3000, 0, 1, 1024, 1025] * 10, 4, 3, 64, 64, width=512)
+
+
 def test_refusals():
     cache = _cache([30, 40], 2, 64, 16)
     q, L, z = _q(2, 4, 64), _int([30, 40]), _int([0, 0])
@@ -532,7 +537,7 @@ def test_refusals():
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
 @pytest.mark.parametrize("G", [3, 8])
 def test_queries_of_unlike_size(D, G):
-    """Channels of q up to 2^24 apart within the 32 that share a scale: what lies 2^15 below the largest is held to 2^-22 of
+    """Channels of q up to 2^24 apart within the 32 that share a scale: what lies 2^14 below the largest is held to 2^-22 of
     it, which adds that times the sum of |k| of the 32 channels to a score's error."""
     lengths = [300, 40, 700]
     cache = _cache(lengths, 2, D, 16)
