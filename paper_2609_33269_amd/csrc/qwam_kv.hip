@@ -75,9 +75,18 @@ __global__ __launch_bounds__(256) void kv_append_fp4_kernel(CacheParams c, uint3
   }
 }
 
-// Bound by the writing: 16384 tokens of 8 heads of 128 15.6 us from 4-bit pages (5.5 TB/s), 16.8 from fp8, 20.9 from bf16;
-// 65536 tokens, past the last-level cache, 90 us from either (268 MB at 3.0 TB/s).
-template <CacheType TYPE>
+// 8 values of an output, PAST the caches or into them
+template <bool PAST>
+__device__ __forceinline__ void put8(uint16_t* to, const uint4& x) {
+  typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+  const v4u v = {x.x, x.y, x.z, x.w};
+  if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<v4u*>(to));
+  else *reinterpret_cast<v4u*>(to) = v;
+}
+
+// Bound by the writing: 16384 tokens of 8 heads of 128 15.3 us from 4-bit pages (5.5 TB/s), 17.0 from fp8, 21.3 from bf16;
+// 65536 tokens of caches that are not in the last-level cache 72, 75 and 94 (4.7, 5.4 and 5.7 TB/s).
+template <CacheType TYPE, bool PAST>
 __global__ __launch_bounds__(256) void kv_read_kernel(CacheParams c, uint32_t threads, int run, const int32_t* seq, const int32_t* pos,
                                                       uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride) {
   const uint32_t i = place_of(blockIdx.x, run) * 256u + threadIdx.x;
@@ -111,8 +120,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheParams c, uint32_t th
       vo = make_uint4(fp4_pair(vw, vs, 0), fp4_pair(vw, vs, 1), fp4_pair(vw, vs, 2), fp4_pair(vw, vs, 3));
     }
   }
-  *reinterpret_cast<uint4*>(k + t * k_stride + head * c.dim + d) = ko;
-  *reinterpret_cast<uint4*>(v + t * v_stride + head * c.dim + d) = vo;
+  put8<PAST>(k + t * k_stride + head * c.dim + d, ko);
+  put8<PAST>(v + t * v_stride + head * c.dim + d, vo);
 }
 
 namespace {
@@ -147,12 +156,18 @@ hipError_t launch_kv_append_fp4(const CacheParams& c, int tokens, const uint16_t
 hipError_t launch_kv_read(const CacheParams& c, CacheType type, int tokens, const int32_t* seq, const int32_t* pos, uint16_t* k,
                           int64_t k_stride, uint16_t* v, int64_t v_stride, hipStream_t stream) {
   const Tokens t = tokens_of(c, tokens);
+  // Outputs that the last-level cache (256 MB) does not hold beside the pages go past it.  With an addition of k and v
+  // behind them, from caches that are not in it, 8 heads of 128: 65536 tokens 165 -> 143 us from 4-bit pages, 154 -> 144 from
+  // fp8; 40960 98 -> 92 from 4-bit pages.  Below, the reader pays (4-bit, 32768 tokens 55 -> 57 us; fp8, 49152 104 -> 112), and
+  // from bf16 pages, as large as the outputs, it gains nothing (65536 tokens 163 -> 161, 131072 318 -> 329).
+  const int64_t written = 32 * static_cast<int64_t>(t.threads);
+  const bool past = written >= (type == CacheType::kFp4 ? 144 << 20 : 256 << 20);
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, t.grid, dim3(256), 0, stream, c, t.threads, t.run, seq, pos, k, k_stride, v, v_stride);
   };
-  if (type == CacheType::kFp4) run(kv_read_kernel<CacheType::kFp4>);
-  else if (type == CacheType::kFp8) run(kv_read_kernel<CacheType::kFp8>);
-  else run(kv_read_kernel<CacheType::kBf16>);
+  if (type == CacheType::kFp4) past ? run(kv_read_kernel<CacheType::kFp4, true>) : run(kv_read_kernel<CacheType::kFp4, false>);
+  else if (type == CacheType::kFp8) past ? run(kv_read_kernel<CacheType::kFp8, true>) : run(kv_read_kernel<CacheType::kFp8, false>);
+  else run(kv_read_kernel<CacheType::kBf16, false>);
   return hipGetLastError();
 }
 

@@ -632,6 +632,32 @@ def test_many_tokens():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4"])
+def test_read_past_the_caches(kind):
+    """Outputs from 144 (4-bit pages) and 256 MiB (fp8) on are written past the caches; the values are those of short calls, on which the tests
+    above look, and a kernel behind the call sees them."""
+    H, D, page, n = 8, 128, 64, 65536 + 3
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pages = -(-n // page)
+    scale = torch.full((H,), 0.25, device="cuda") if kind == "fp8" else None
+    cache = P.new_cache(pages, H, D, 1, pages, page, {"bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn, "fp4": FP4}[kind], scale, scale)
+    cache.table[0] = torch.randperm(pages, device="cuda", generator=g)
+    x = torch.empty(n, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    seq, pos = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.randperm(n, device="cuda", generator=g).int()
+    P.kv_append(cache, x, -x, seq, pos)
+    for _ in range(3):
+        k, v = P.kv_read(cache, seq, pos)
+        total = k + v
+        assert not total.any() and k.any()
+        for at in range(0, n, 16384):
+            a, b = P.kv_read(cache, seq[at:at + 16384], pos[at:at + 16384])
+            assert torch.equal(k[at:at + 16384], a) and torch.equal(v[at:at + 16384], b)
+    if kind == "bf16":
+        assert torch.equal(k, x)
+    del x, k, v, total, cache
+    torch.cuda.empty_cache()
+
+
 def test_two_streams():
     """Calls on two streams at once, each with a workspace of its own, and two graphs replayed at once."""
     lengths = [9000, 100, 4000]
