@@ -492,12 +492,10 @@ qwam_status qwam_kv_read(const qwam_cache *c, int32_t tokens, const int32_t *seq
  * Visible scores of -inf have weight 0, and where all are -inf o is zeros; one
  * of +inf or NaN makes o[b][h] NaN.  An infinite or NaN value makes its channel
  * of its heads' o infinite or NaN (which of the two is not specified).
- * fp4: q enters the scores exactly where |q| is within 2^-14 of the largest of its
- * 32 channels (q's groups are the cache's), and to 2^-22 of that below; an infinity
- * or NaN in q makes o[b][h] NaN.  A group with E = 255 is NaN: in a key it makes the
- * results of its heads NaN, in a value those of its 32 channels.  (E of 253 and 254,
- * which qwam_kv_append does not write, count values past bf16's range as infinities
- * of any channel of their group.)
+ * fp4: an infinity or NaN in q makes o[b][h] NaN.  A group with E = 255 is NaN: in a
+ * key it makes the results of its heads NaN, in a value those of its 32 channels.
+ * (E of 253 and 254, which qwam_kv_append does not write, count what passes bf16's
+ * range as infinite, in a value for any channel of its group.)
  *   q        in  bf16, sequence b's q_heads x dim values at b * q_stride,
  *                16-byte aligned, q_stride % 8 == 0
  *   q_heads  in  a multiple of heads, at most 64 per key head, seqs * q_heads <= 2^22

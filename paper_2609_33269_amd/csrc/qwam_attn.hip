@@ -430,10 +430,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 // they are counted here:
 //   * A wave takes 64 positions a turn, in blocks of 16 (32 for heads above 128), so that the maximum, the test for a new
 //     one and the loop are paid once for them.
-//   * Keys are multiplied as they are stored (v_mfma_scale_f32_16x16x128_f8f6f4: e2m1 with a power of two for 32 channels
-//     is its operand; 13% fewer instructions than by bf16).  q enters as two e4m3 pieces, each of 4 bits of its 8: q
-//     exactly, where it is within 2^-14 of the largest of its 32 channels, and to 2^-22 of that below.
-//   * Values are converted to bf16, which is exact and applies the power of two, and weighted by two bf16 pieces.  With up
+//   * Keys are converted to bf16, which is exact and applies the power of two, and multiplied by q as it is, sums in float32.
+//     (The scaled products that take e2m1 keys as they are stored drop what lies below 2^-13 of the largest of eight
+//     neighbouring products: a score was off by up to 2^-16 of sum |q k|, and by 7 * 2^-14 of it beside one large channel.)
+//   * Values are converted likewise and weighted by two bf16 pieces.  With up
 //     to 4 query heads (the narrow form) the 16 columns of that product hold each head four times, for both pieces of its
 //     weights and for even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them,
 //     and a lane needs no transposing.  The same four lanes share a head's 64 weights, 16 each.  (8 x 3 heads of 128, a
@@ -451,47 +451,8 @@ constexpr float kSlack = 8.0f;
 constexpr int kNarrow = 4;              // query heads of a key head that the narrow form takes
 constexpr int kGridRanges = 32768;      // ranges in the grid's last dimension; more of them stand behind the heads
 
-// 16 bf16 values as two e4m3 pieces each: `hi` at 2^(e - 127), `lo` at 2^(e - 132).  e is 7 below the exponent of the largest
-// of a group, so that a piece is at most 2^8; what `hi` leaves is at most 2^3 of its steps.
-struct Pieces {
-  uint32_t hi[4], lo[4];
-};
-__device__ __forceinline__ Pieces fp8_pieces(const uint4& x, const uint4& y, uint32_t e) {
-  const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-  const float s = __uint_as_float(e << 23), sl = __uint_as_float((e - 5) << 23);
-  typedef short v2s __attribute__((ext_vector_type(2)));
-  Pieces p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v2s hi = {0, 0}, lo = {0, 0};
-    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(v2bf16, w[2 * i]), s, false);
-    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(v2bf16, w[2 * i + 1]), s, true);
-    p.hi[i] = __builtin_bit_cast(uint32_t, hi);
-    auto low = [](uint32_t u) { return __uint_as_float(u << 16); };
-    auto high = [](uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); };
-    const uint32_t b0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.hi[i], s, false));
-    const uint32_t b1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.hi[i], s, true));
-    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, low(w[2 * i]) - low(b0), high(w[2 * i]) - high(b0), sl, false);
-    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, low(w[2 * i + 1]) - low(b1), high(w[2 * i + 1]) - high(b1), sl, true);
-    p.lo[i] = __builtin_bit_cast(uint32_t, lo);
-  }
-  return p;
-}
-
-__device__ __forceinline__ uint32_t largest_of(const uint4& x, const uint4& y) {
-  const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-  typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
-  v2u16 m = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(v2u16, w[i] & 0x7FFF7FFFu));
-  return m[0] > m[1] ? m[0] : m[1];
-}
-
-// lane l's and lane l ^ 16's larger
-__device__ __forceinline__ uint32_t larger_xor16(uint32_t v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  return max(r[0], r[1]);
-}
+// two bf16 values, an infinity among them as NaN
+__device__ __forceinline__ uint32_t infinite_as_nan(uint32_t w) { return w | ((((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u) >> 9); }
 
 // the i-th of four (by bits: compared one by one they became branches)
 template <typename T>
@@ -517,7 +478,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   static_assert(!NARROW || DP <= 128, "the narrow form takes heads up to 128");
   constexpr int BL = DP == 256 ? 2 : 4;           // blocks of 16 positions a turn
   constexpr int DC = DP / 16;                     // channels of V in a lane
-  constexpr int NK = (DP + 127) / 128;            // 32 channels of a key in a lane; products over 128 channels
+  constexpr int NK = (DP + 127) / 128;            // pieces of up to 128 channels of a key
+  constexpr int KC = DP == 64 ? 16 : 32, KW = KC / 8;   // channels and words of a piece in a lane
   constexpr int NV = (DC + 7) / 8;                // words of V in a lane, per key
   constexpr int NA = NARROW ? DC / 2 : DC;        // accumulators
   constexpr int waves = kAttnWaves;
@@ -577,23 +539,21 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
                                 static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, from)));
   };
 
-  // q as the second operand of S^T, column r: its head's (in the narrow form r / 4's) pieces, of the sign of the scale.
-  // Lane quarter c supplies channels 16 c and 64 + 16 c on of 128 and the scale of channels 32 c on.  Heads up to 64: `hi` in
-  // the first 64 places and `lo` in the others, where the keys come a second time.
+  // q as the second operand of S^T, column r: its head's (in the narrow form r / 4's), of the sign of the scale.  Lane quarter c
+  // supplies the channels whose keys it holds, 8 a product.  An infinity counts as NaN, so that it makes NaN of every score.
   const int head = NARROW ? r >> 2 : r;
-  constexpr int NQ = DP == 64 ? 1 : 2 * NK;       // pieces of 16 channels of q in a lane
-  uint4 qx[NQ], qy[NQ];
+  v8bf qf[NK][KW];
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    qx[i] = qy[i] = make_uint4(0, 0, 0, 0);
-    const int ch = 64 * i + 16 * c;
-    if (head < nq && (FULL || ch < D)) {          // (dim is a multiple of 32)
-      const uint4* const src =
-          reinterpret_cast<const uint4*>(a.q + b * a.q_stride + static_cast<int64_t>(h * a.group + q0 + head) * D + ch);
-      qx[i] = src[0];
-      qy[i] = src[1];
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      const int ch = 128 * i + KC * c + 8 * w;
+      if (head < nq && (FULL || ch < D))            // (dim is a multiple of 32)
+        v = *reinterpret_cast<const uint4*>(a.q + b * a.q_stride + static_cast<int64_t>(h * a.group + q0 + head) * D + ch);
+      const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+      qf[i][w] = bf8(infinite_as_nan(v.x) ^ flip, infinite_as_nan(v.y) ^ flip, infinite_as_nan(v.z) ^ flip, infinite_as_nan(v.w) ^ flip);
     }
-  }
   // (above 0, so that a masked score of -inf times it is no NaN: with a scale of 0 scores below 2^118 still count as 0)
   const float sscale = fmaxf(__builtin_fabsf(a.scale) * kLog2e, 0x1p-126f);
 
@@ -606,19 +566,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   const uint8_t* const vbase = static_cast<const uint8_t*>(a.c.v) + static_cast<int64_t>(h) * a.c.head_stride + back;
   const uint8_t* const kebase = a.c.k_exp + fp4_exp_group(a.c, h, 0);
   const uint8_t* const vebase = a.c.v_exp + fp4_exp_group(a.c, h, 0);
-  const int kc = DP == 64 ? c & 1 : c;            // the 32 channels of a key that the lane holds (of each 128)
-  const uint32_t koff = place(r) + 16 * kc;
+  const uint32_t koff = place(r) + KC / 2 * c;
   uint32_t voff[4], keoff[NK];
 #pragma unroll
   for (int i = 0; i < 4; ++i) voff[i] = place(4 * c + i) + DC / 2 * r;
 #pragma unroll
-  for (int i = 0; i < NK; ++i) keoff[i] = (static_cast<uint32_t>(4 * i + kc) << a.c.page_bits) + r;
+  for (int i = 0; i < NK; ++i) keoff[i] = (static_cast<uint32_t>((128 * i + KC * c) / kFp4Group) << a.c.page_bits) + r;
   const uint32_t veoff = (static_cast<uint32_t>(DC * r / kFp4Group) << a.c.page_bits) + 4 * c;
   // whether the lane's channels exist
-  auto has_k = [&](int i) { return FULL || 128 * i + 32 * kc < D; };
+  auto has_k = [&](int i) { return FULL || 128 * i + KC * c < D; };
   const bool has_v = FULL || DC * r < D;
 
-  v4i kr[BL][NK];
+  uint32_t kr[BL][NK][KW];
   // values come a turn ahead too (in the wide form of 64 channels 64 ragged contexts up to 4096 24.7 us, without 25.6; of wider
   // heads it changes nothing or costs a wave)
   constexpr bool V_AHEAD = NARROW || DP == 64;
@@ -639,10 +598,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
       const uint8_t* const e = kebase + exp_at[t];
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        kr[t][i] = v4i{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < KW; ++w) kr[t][i][w] = 0;
         ke[t][i] = 0;
         if (!has_k(i)) continue;
-        kr[t][i] = *reinterpret_cast<const v4i*>(near(p + 64 * i, koff));
+        if constexpr (KW == 2) *reinterpret_cast<uint2*>(kr[t][i]) = *reinterpret_cast<const uint2*>(near(p + 64 * i, koff));
+        else *reinterpret_cast<uint4*>(kr[t][i]) = *reinterpret_cast<const uint4*>(near(p + 64 * i, koff));
         ke[t][i] = *near(e, keoff[i]);
       }
     }
@@ -684,42 +645,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
     load_v(va, vea);
   }
 
-  // q's pieces (while the first keys are on their way)
-  v8i qhi[NK], qlo[NK];
-  uint32_t qe[NK];                                // exponent of `hi` in the first byte, of `lo` in the second
-  {
-    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
-    uint32_t e[NQ], other[NQ];
-    Pieces u[NQ];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const uint4 x = make_uint4(qx[i].x ^ flip, qx[i].y ^ flip, qx[i].z ^ flip, qx[i].w ^ flip);
-      const uint4 y = make_uint4(qy[i].x ^ flip, qy[i].y ^ flip, qy[i].z ^ flip, qy[i].w ^ flip);
-      // of the largest |q| of 32 channels, the lane's and its neighbour quarter's; an infinity or NaN makes NaN of the scores
-      const uint32_t largest = larger_xor16(largest_of(x, y));
-      e[i] = largest >= 0x7F80u ? 255u : static_cast<uint32_t>(max(static_cast<int>(largest >> 7) - 7, 6));
-      other[i] = __shfl_xor(e[i], 48);
-      u[i] = fp8_pieces(x, y, e[i]);
-    }
-    auto join = [](const uint32_t (&x)[4], const uint32_t (&y)[4]) {
-      return v8i{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
-                 static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
-    };
-    auto lower = [](uint32_t e) { return e == 255u ? e : e - 5; };
-    if constexpr (DP == 64) {
-      qhi[0] = join(u[0].hi, u[0].lo);
-      qe[0] = of_four(c, e[0], other[0], lower(other[0]), lower(e[0]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        qhi[i] = join(u[2 * i].hi, u[2 * i + 1].hi);
-        qlo[i] = join(u[2 * i].lo, u[2 * i + 1].lo);
-        const uint32_t own = of_four(c, e[2 * i], other[2 * i], other[2 * i + 1], e[2 * i + 1]);
-        qe[i] = own | lower(own) << 8;
-      }
-    }
-  }
-
   auto turn = [&](int tile, uint32_t (&vr)[BL][4][NV], uint32_t (&ve)[BL], uint32_t (&vn)[BL][4][NV],
                   uint32_t (&ven)[BL]) __attribute__((always_inline)) {
     // scores of keys 16 t + 4 c + i
@@ -729,13 +654,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
-      for (int piece = 0; piece < (DP == 64 ? 1 : 2); ++piece)
+      for (int w = 0; w < KW; ++w)
 #pragma unroll
         for (int t = 0; t < BL; ++t) {
-          const v8i keys = __builtin_shufflevector(kr[t][i], kr[t][i], 0, 1, 2, 3, -1, -1, -1, -1);
-          const int e = static_cast<int>(ke[t][i]), f = static_cast<int>(qe[i]);
-          s[t] = piece == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(keys, qhi[i], s[t], 4, 0, 0, e, 0, f)
-                            : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(keys, qlo[i], s[t], 4, 0, 0, e, 1, f);
+          const uint32_t k = kr[t][i][w], e = ke[t][i] << 23;
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf8(fp4_pair(k, e, 0), fp4_pair(k, e, 1), fp4_pair(k, e, 2), fp4_pair(k, e, 3)),
+                                                         qf[i][w], s[t], 0, 0, 0);
         }
     const bool more = tile + 1 < tiles;
     if (more) {

@@ -282,6 +282,66 @@ def test_offsets_past_32_bits():
     torch.cuda.empty_cache()
 
 
+def _two_positions(q, codes):
+    """A cache of two positions a sequence, keys of the given codes [sequences][2][D] and values of 1 and -1 throughout: what
+    attention gives is tanh of half the difference of the two scores."""
+    B, _, D = codes.shape
+    k = torch.zeros(B, 1, 16, D // 2, dtype=torch.uint8)
+    v = torch.zeros_like(k)
+    k[:, 0, :2], v[:, 0, 0], v[:, 0, 1] = _pack(codes.to(torch.uint8)), 0x22, 0xAA
+    e = torch.full((B, 1, D // 32, 16), 127, dtype=torch.uint8).cuda().view(E8M0)
+    return P.PagedCache(k.cuda().view(FP4), v.cuda().view(FP4), torch.arange(B, dtype=torch.int32)[:, None].cuda(), e, e)
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 256])
+@pytest.mark.parametrize("G", [1, 5])
+def test_small_products_beside_a_large_one(D, G):
+    """A score keeps what lies 2^-14 below the largest product of its channels' neighbourhood: 256 (1 +- 7 * 2^-14), at every place
+    of the large channel."""
+    q = torch.zeros(D, G, D)
+    codes = torch.full((D, 2, D), 2)
+    codes[:, 1] = 10                                        # -1
+    for b in range(D):
+        q[b, :, b // 8 * 8:b // 8 * 8 + 8] = 2.0 ** -14
+        q[b, :, b] = 1
+        codes[b, 1, b] = 2
+    q = q.bfloat16().cuda()
+    cache, L = _two_positions(q, codes), _int([2] * D)
+    _check(_as_bf16(cache), q, [2] * D, P.paged_attention(cache, q, L, scale=256.0), scale=256.0)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128, 256])
+@pytest.mark.parametrize("G", [1, 5])
+def test_scores_that_nearly_meet(D, G):
+    """Two keys out of 96 random ones whose scores are closest: their difference shows the scores' own error."""
+    B, g = 512, torch.Generator().manual_seed(D)
+    q = torch.randn(B, 1, D, generator=g).bfloat16()
+    codes = torch.randint(0, 16, (B, 96, D), generator=g)
+    grid = torch.from_numpy(np.concatenate((GRID, -GRID)))
+    order = (grid[codes] * q.double()).sum(-1).sort(1)
+    i = order.values.diff(dim=1).argmin(1, keepdim=True)
+    at = torch.cat((order.indices.gather(1, i), order.indices.gather(1, i + 1)), 1)
+    cache, L = _two_positions(q, codes.gather(1, at[..., None].expand(B, 2, D))), _int([2] * B)
+    q = q.expand(B, G, D).contiguous().cuda()
+    _check(_as_bf16(cache), q, [2] * B, P.paged_attention(cache, q, L, scale=1.0), scale=1.0)
+
+
+@pytest.mark.parametrize("D,G", [(32, 1), (64, 6), (128, 2), (128, 16), (256, 3)])
+def test_an_infinite_query_before_one_key(D, G):
+    """It makes that head's result NaN whatever the key holds at its channel: one sign, the other, or 0."""
+    codes = torch.full((3, 2, D), 2)
+    codes[1, :, 17], codes[2, :, 17] = 10, 0
+    cache, L = _two_positions(torch.zeros(3, G, D), codes), _int([1] * 3)
+    for bad in (INF, -INF, NAN):
+        for scale in (1.0, -1.0):
+            q = _q(3, G, D)
+            q[:, G // 2, 17] = bad
+            got = P.paged_attention(cache, q, L, scale=scale)
+            assert got[:, G // 2].isnan().all()
+            got[:, G // 2] = 1
+            assert (got == 1).all()
+
+
 # ---- append ----
 
 @pytest.mark.parametrize("layout", ["heads", "rows", "both"])
