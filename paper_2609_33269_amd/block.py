@@ -96,6 +96,7 @@ def _forward(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight,
     st = _q.lib().qwam_block_norm(ctypes.byref(c), px, pb, None if xo is None else _q._req(xo, "out[0]", x.dtype, (T, D)),
                                   _q._req(h, "out[1]", torch.bfloat16, (T, D)), _q._stream_ptr(stream))
     _q._check("qwam_block_norm", st)
+    _q._written(*(out or ()))
     return xo, h
 
 
@@ -306,6 +307,7 @@ def kv_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Te
                                  _q._req(seq, "seq", torch.int32, (n,)), _q._req(pos, "pos", torch.int32, (n,)),
                                  _q._stream_ptr(stream))
     _q._check("qwam_kv_append", st)
+    _q._written(cache.k, cache.v, *((cache.k_scale, cache.v_scale) if c.type == CACHE_TYPES[torch.float4_e2m1fn_x2] else ()))
 
 
 def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, stream=None):
@@ -331,6 +333,7 @@ def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, s
     st = _q.lib().qwam_kv_read(ctypes.byref(c), n, ps, pp, _rows(k, "out[0]", shape), k.stride(0) if n > 1 else 0,
                                _rows(v, "out[1]", shape), v.stride(0) if n > 1 else 0, _q._stream_ptr(stream))
     _q._check("qwam_kv_read", st)
+    _q._written(*(out or ()))
     return k, v
 
 
@@ -366,4 +369,5 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
         float(c.dim ** -0.5 if scale is None else scale), _q._req(o, "out", torch.bfloat16, shape),
         None if ws is None else ws.data_ptr(), need, _q._stream_ptr(stream))
     _q._check("qwam_paged_attention", st)
+    _q._written(out)
     return o

@@ -158,6 +158,14 @@ struct Held {
   }
 };
 
+// What the call wrote into tensors that the caller gave, told to autograd, which may have saved them: as after torch's own
+// operations in place (a tensor of inference mode has no version).  None, and what is null, is no tensor.
+void written(std::initializer_list<PyObject*> objects) {
+  for (PyObject* o : objects)
+    if (o != nullptr && THPVariable_Check(o) && !THPVariable_Unpack(o).is_inference())
+      THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject* none_or_error() {
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
@@ -221,6 +229,7 @@ PyObject* py_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                   static_cast<float*>(ps), static_cast<uint16_t*>(pt), pw, need > 0 ? need : 0, stream);
   Py_END_ALLOW_THREADS
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({given[0], given[1], given[2]});
   return PyTuple_Pack(3, xq.o, xs.o, t.o);
   END_HANDLE_TH_ERRORS
 }
@@ -244,6 +253,7 @@ PyObject* py_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                 static_cast<const uint16_t*>(t), static_cast<uint16_t*>(py), stream);
   Py_END_ALLOW_THREADS
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({args[4]});
   return y.release();
   END_HANDLE_TH_ERRORS
 }
@@ -265,6 +275,7 @@ PyObject* py_layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                nullptr, nullptr, stream);
   Py_END_ALLOW_THREADS
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({args[2]});
   return y.release();
   END_HANDLE_TH_ERRORS
 }
@@ -308,6 +319,7 @@ PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                 need > 0 ? ws.data_ptr() : nullptr, need, stream);
   Py_END_ALLOW_THREADS
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({args[2]});
   return y.release();
   END_HANDLE_TH_ERRORS
 }
@@ -525,9 +537,14 @@ PyObject* py_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return none_or_error();
   if (C.followed() || tracked({args[1], args[2]})) Py_RETURN_NONE;
   if (!on_current_device({k, v, &THPVariable_Unpack(args[3]), &THPVariable_Unpack(args[4])})) Py_RETURN_NONE;
-  return PyLong_FromLong(g_append(&C.c, static_cast<int32_t>(n), static_cast<const uint16_t*>(k->data_ptr()), n > 1 ? k->stride(0) : 0,
+  const qwam_status st = g_append(&C.c, static_cast<int32_t>(n), static_cast<const uint16_t*>(k->data_ptr()), n > 1 ? k->stride(0) : 0,
                                   static_cast<const uint16_t*>(v->data_ptr()), n > 1 ? v->stride(0) : 0,
-                                  static_cast<const int32_t*>(seq), static_cast<const int32_t*>(pos), current_stream()));
+                                  static_cast<const int32_t*>(seq), static_cast<const int32_t*>(pos), current_stream());
+  if (st == QWAM_OK) {
+    written({C.held[kCacheK], C.held[kCacheV]});
+    if (C.c.type == QWAM_CACHE_FP4) written({C.held[kCacheKScale], C.held[kCacheVScale]});
+  }
+  return PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }
 
@@ -575,6 +592,7 @@ PyObject* py_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                                      static_cast<int32_t>(max_len), static_cast<float>(scale), static_cast<uint16_t*>(po),
                                      need > 0 ? ws.data_ptr() : nullptr, need, current_stream());
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({args[6]});
   return o.release();
   END_HANDLE_TH_ERRORS
 }
@@ -608,6 +626,7 @@ PyObject* py_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                                 static_cast<uint16_t*>(t[0]->data_ptr()), n > 1 ? t[0]->stride(0) : 0,
                                 static_cast<uint16_t*>(t[1]->data_ptr()), n > 1 ? t[1]->stride(0) : 0, current_stream());
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  if (args[3] != Py_None) written({o[0].o, o[1].o});
   return PyTuple_Pack(2, o[0].o, o[1].o);
   END_HANDLE_TH_ERRORS
 }
@@ -664,6 +683,7 @@ PyObject* py_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   }
   const qwam_status st = g_rope(&p, static_cast<int32_t>(T), args[3] == Py_True, x->data_ptr(), stride, py, y_stride, current_stream());
   if (st != QWAM_OK) return PyLong_FromLong(st);
+  written({args[4]});
   return y.release();
   END_HANDLE_TH_ERRORS
 }

@@ -162,6 +162,12 @@ def _check(fn: str, status: int) -> None:
         raise QwamError(fn, status, lib().qwam_last_error().decode())
 
 
+def _written(*tensors) -> None:
+    """Tells autograd, which may have saved them, that a call wrote these tensors of its caller's, as torch's own operations
+    in place do (None: not given)."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _stream_ptr(stream) -> int:
     s = torch.cuda.current_stream() if stream is None else stream
     return int(s.cuda_stream)
@@ -327,6 +333,8 @@ def _quantize(deflated: bool, name: str, layer: PackedLayer, x: torch.Tensor, st
     else:     # a bare stream handle has no pool to take a workspace from: the call runs unsplit
         st = getattr(lib(), name)(ctypes.byref(c), M, *ptrs, _stream_ptr(stream))
     _check(name, st)
+    if out is not None:
+        _written(xq, xs, t)
     return xq, xs, t
 
 
@@ -348,6 +356,7 @@ def asp_linear(layer: PackedLayer, xq: torch.Tensor, xs: torch.Tensor, t: torch.
                                _req(t, "t", torch.bfloat16, (M, layer.r)),
                                _req(y, "y", torch.bfloat16, (M, layer.N)), _stream_ptr(stream))
     _check("qwam_asp_linear", st)
+    _written(out)
     return y
 
 
@@ -381,6 +390,7 @@ def asp_layer(layer: PackedLayer, x: torch.Tensor, out=None, act_out=None, strea
     st = lib().qwam_asp_layer(ctypes.byref(c), M, _req(x, "x", torch.bfloat16, (M, layer.K)),
                               _req(y, "y", torch.bfloat16, (M, layer.N)), pq, ps, pt, _stream_ptr(stream))
     _check("qwam_asp_layer", st)
+    _written(out, *(act_out or ()))
     return y
 
 
@@ -441,6 +451,7 @@ def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] 
     st = lib().qwam_asp_matvec(ctypes.byref(c), M, px, _req(y, "y", torch.bfloat16, (M, layer.N)),
                                None if ws is None else ws.data_ptr(), need, _stream_ptr(stream))
     _check("qwam_asp_matvec", st)
+    _written(out)
     return y
 
 
@@ -464,6 +475,7 @@ def aog_accumulate(gT: torch.Tensor, A: torch.Tensor, stream=None) -> torch.Tens
     st = lib().qwam_aog_accumulate(d, n, _req(gT, "gT", torch.bfloat16, (d, n)),
                                    _req(A, "A", torch.float32, (d, d)), _stream_ptr(stream))
     _check("qwam_aog_accumulate", st)
+    _written(A)
     return A
 
 

@@ -93,6 +93,7 @@ def _rope(x, positions, plan, inverse, out, stream):
             raise ValueError("out overlaps x without being x")
     st = _q.lib().qwam_rope(ctypes.byref(c), T, bool(inverse), px, xs, py, ys, _q._stream_ptr(stream))
     _q._check("qwam_rope", st)
+    _q._written(out)
     return y
 
 
