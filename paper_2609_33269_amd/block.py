@@ -149,7 +149,7 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
             return done
     _q._no_tangent("block_norm", x=x, branch=branch, gate=gate, post_weight=post_weight, weight=weight, scale=scale, shift=shift)
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
-                                       for t in (x, branch, gate, post_weight, weight, scale, shift)):
+                                       for t in (x, branch, gate, post_weight, weight, scale, shift, *(out or ()))):
         if out is not None or stream is not None:
             raise ValueError("block_norm under autograd takes neither out nor stream")
         return _BlockNorm.apply(x, branch, gate, post_weight, weight, scale, shift, norm, eps, residual_scale, post_norm)
@@ -356,7 +356,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, lengths: torch.Tensor, *
     Hq = q.shape[1]
     shape = (c.seqs, Hq, c.dim)
     pq = _rows(q, "q", shape)
-    _q._no_gradient("paged_attention", q=q, **cache._values())
+    _q._no_gradient("paged_attention", q=q, out=out, **cache._values())
     _q._on_current_device("paged_attention", stream, q=q, lengths=lengths, starts=starts, out=out, table=cache.table, **cache._values())
     if max_len is None:
         max_len = c.table_width * c.page_size

@@ -305,7 +305,7 @@ PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t M = rows_of(args[1]);
   void *x, *py;
   if (M < 0 || !L.load(args[0], true) || !data_of(args[1], at::kBFloat16, {M, L.c.K}, &x)) return none_or_error();
-  if (tracked({args[1], L.held[kWs], L.held[kInv], L.held[kL1t], L.held[kL2t], L.held[kBias], L.held[kL1f]})) Py_RETURN_NONE;
+  if (tracked({args[1], args[2], L.held[kWs], L.held[kInv], L.held[kL1t], L.held[kL2t], L.held[kBias], L.held[kL1f]})) Py_RETURN_NONE;
   const at::Tensor& xt = THPVariable_Unpack(args[1]);
   Held y;
   if (!output(args[2], xt, at::kBFloat16, M, L.c.N, &y.o, &py)) return none_or_error();
@@ -557,7 +557,7 @@ PyObject* py_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (q == nullptr || q->dim() != 3 || q->size(1) > INT32_MAX || !C.load(args[0]) ||
       rows3_of(args[1], C.c.seqs, q->size(1), C.c.dim) == nullptr)
     return none_or_error();
-  if (C.followed() || tracked(args[1])) Py_RETURN_NONE;
+  if (C.followed() || tracked({args[1], args[6]})) Py_RETURN_NONE;
   const int32_t heads = static_cast<int32_t>(q->size(1));
   void *lengths, *starts = nullptr, *po;
   if (!data_of(args[2], at::kInt, {C.c.seqs}, &lengths) || (args[3] != Py_None && !data_of(args[3], at::kInt, {C.c.seqs}, &starts)))

@@ -443,7 +443,7 @@ def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] 
     M = x.shape[0]
     c = layer.c_struct(matvec=True)
     px = _req(x, "x", torch.bfloat16, (M, layer.K))
-    _no_gradient("asp_matvec", x=x, ws=layer.ws, inv_smooth=layer.inv_smooth, L1t=layer.L1t, L2t=layer.L2t, bias=layer.bias,
+    _no_gradient("asp_matvec", x=x, out=out, ws=layer.ws, inv_smooth=layer.inv_smooth, L1t=layer.L1t, L2t=layer.L2t, bias=layer.bias,
                  L1f=layer.L1f)
     need = _need("qwam_asp_matvec", lib().qwam_asp_matvec_workspace(ctypes.byref(c), M))
     y = _empty((M, layer.N), torch.bfloat16, x.device, stream) if out is None else out

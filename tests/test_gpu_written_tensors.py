@@ -135,3 +135,20 @@ def test_tensors_of_inference_mode(stream):
     assert P.rope(x, pos, plan, out=x, **kw) is x
     with torch.inference_mode():
         assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("stream", STREAM)
+def test_outputs_that_require_a_gradient(stream):
+    """They are refused where autograd records: what is written has no history."""
+    kw = {"stream": torch.cuda.current_stream()} if stream else {}
+    c, q = _cache([30, 40], 2, 64, 16), _q(2, 6, 64)
+    layer, x = _layer(256, 64, 16), _x(4, 256)
+    o, y, h = torch.empty_like(q), torch.empty(4, 64, dtype=torch.bfloat16, device="cuda"), torch.empty_like(x)
+    for t, name, call in ((o, "out requires a gradient, which paged_attention", lambda: P.paged_attention(c, q, _int([10, 12]), out=o, **kw)),
+                          (y, "out requires a gradient, which asp_matvec", lambda: P.asp_matvec(layer, x, out=y, **kw)),
+                          (h, "block_norm under autograd takes neither out", lambda: P.block_norm(x, x, out=(x.clone(), h), **kw))):
+        t.requires_grad_()
+        with pytest.raises(ValueError, match=name):
+            call()
+        with torch.no_grad():
+            call()
