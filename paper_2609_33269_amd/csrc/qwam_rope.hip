@@ -99,6 +99,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   };
   load(h0);
   float cs[N], sn[N];
+  bool still[N];                        // pairs that do not turn: copied, as an infinity times 0 is not 0
   const int64_t pr = static_cast<int64_t>(t % static_cast<uint32_t>(a.p.positions)) * a.p.axes;
   double at[kRopeMaxAxes];              // (all axes' positions at once, not behind the pair's axis)
 #pragma unroll
@@ -112,8 +113,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     const uint32_t pair = u * N + j;
     const uint32_t axis = static_cast<uint32_t>(a.p.axis[pair]);
     const double pos = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
-    const bool turns = axis < static_cast<uint32_t>(a.p.axes);
-    const float2 v = cos_sin_turns(turns ? pos * (a.p.inv_freq[pair] * 0.15915494309189535) : 0.0);
+    still[j] = axis >= static_cast<uint32_t>(a.p.axes);
+    const float2 v = cos_sin_turns(pos * (a.p.inv_freq[pair] * 0.15915494309189535));
     cs[j] = v.x;
     sn[j] = v.y * a.sign;
   }
@@ -149,6 +150,16 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         r.e[j + 1] = static_cast<E>(v >> 16);
         s.e[j] = static_cast<E>(w);
         s.e[j + 1] = static_cast<E>(w >> 16);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (INTERLEAVED) {
+        r.e[2 * j] = still[j] ? p.e[2 * j] : r.e[2 * j];
+        r.e[2 * j + 1] = still[j] ? p.e[2 * j + 1] : r.e[2 * j + 1];
+      } else {
+        r.e[j] = still[j] ? p.e[j] : r.e[j];
+        s.e[j] = still[j] ? q.e[j] : s.e[j];
       }
     }
     *reinterpret_cast<piece*>(y + h * dim + first) = r;

@@ -116,6 +116,30 @@ def test_axes_that_do_not_exist():
                 assert torch.equal(y[..., at], x[..., at])
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T", [5, 300])
+def test_pairs_without_an_axis_are_copied(interleaved, f32, T):
+    """Bit for bit: an infinity or a NaN of any kind stays in its channel, and a zero keeps its sign.  (300 x 55 heads of 32: two
+    pairs a thread in halves of bf16.)"""
+    plan = P.rope_plan((16, 16), interleaved=interleaved)
+    plan.axis[3], plan.axis[8], plan.axis[9] = 2, -1, 7
+    H = 3 if T == 5 else 55
+    x, pos = _x(T, H, 32, f32, T), _pos(T, 2)
+    bits = torch.int32 if f32 else torch.int16
+    odd = [0x7F800000, -0x800000, 0x7FC00001, 0x7F810000, -0x7E0000, -2 ** 31, 0, 1, -0x7FFF0000] if f32 else \
+        [0x7F80, -0x80, 0x7FC1, 0x7F81, -0x7E, -2 ** 15, 0, 1, -0x7FFF]
+    for i in (3, 8, 9):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + 16)
+        for n, v in enumerate(odd):
+            x.view(bits)[n % T, n % H, (a, b)[n % 2]] = v
+            x.view(bits)[(n + 1) % T, n // 2 % H, (b, a)[n % 2]] = v
+    for y in (P.rope(x, pos, plan), P.rope(x, pos, plan, inverse=True), P.rope(x.clone(), pos, plan, stream=torch.cuda.current_stream())):
+        for i in (3, 8, 9):
+            at = slice(2 * i, 2 * i + 2) if interleaved else slice(i, i + 17, 16)
+            assert torch.equal(y.view(bits)[..., at], x.view(bits)[..., at])
+
+
 def test_what_is_not_finite():
     """It stays in its pair; a NaN position, in its token's pairs of that axis."""
     plan = P.rope_plan((16, 16), interleaved=True)
