@@ -2,6 +2,8 @@
 // tokens of any page type back as bf16 (qwam_kv_read).  Both touch every value once
 // and compute almost nothing: a thread takes 8 channels of a token's head, keys and
 // values beside each other, so that the two streams' latencies overlap.
+#include <climits>
+
 #include "qwam_fp4.h"
 #include "qwam_mfma.h"
 
@@ -84,6 +86,43 @@ __device__ __forceinline__ void put8(uint16_t* to, const uint4& x) {
   else *reinterpret_cast<v4u*>(to) = v;
 }
 
+// f * scale for a rounding to bf16: the float32 product where that is exact, else of the two float32 values around it the odd one,
+// which is no middle of two bf16 values and lies to their same side.  (f is an e4m3 value, so the product has up to 28 bits; what
+// is left of it may lie below float32's numbers where the scale is small, and is taken times `up`.)
+__device__ __forceinline__ float product_to_odd(float f, float scale) {
+  const float up = __builtin_fabsf(scale) < 0x1p-60f ? 0x1p60f : 1.0f, p = f * scale, e = __builtin_fmaf(f, scale * up, -(p * up));
+  const uint32_t b = __float_as_uint(p), step = static_cast<uint32_t>(static_cast<int>(b ^ __float_as_uint(e)) >> 31) | 1u;
+  return __uint_as_float((b & 1u) == 0 && __builtin_fabsf(e) > 0.0f ? b + step : b);
+}
+
+// e4m3 codes of keys and values times their scales as bf16, rounded once.  The float32 products serve where none of them is the
+// middle of two bf16 values, which is where a second rounding can go wrong.  (16384 tokens of 8 heads of 128 17.3 us; without the test
+// for one 17.0, with every product to odd 20.9.)
+__device__ __forceinline__ void fp8_values(uint2 kw, uint2 vw, float ks, float vs, uint32_t (&y)[8]) {
+  typedef short v2i16 __attribute__((ext_vector_type(2)));
+  v2f f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t k = i < 2 ? kw.x : kw.y, v = i < 2 ? vw.x : vw.y;
+    f[i] = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(k, true) : __builtin_amdgcn_cvt_pk_f32_fp8(k, false);
+    f[4 + i] = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(v, true) : __builtin_amdgcn_cvt_pk_f32_fp8(v, false);
+  }
+  v2i16 least = {0, 0};                 // of the products' lower halves: -2^15 is a middle
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = i < 4 ? ks : vs, a = f[i][0] * s, b = f[i][1] * s;
+    y[i] = bf16_pair(a, b);
+    least = __builtin_elementwise_min(
+        least, __builtin_bit_cast(v2i16, __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x05040100u)));
+  }
+  if (min(least[0], least[1]) == SHRT_MIN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float s = i < 4 ? ks : vs;
+      y[i] = bf16_pair(product_to_odd(f[i][0], s), product_to_odd(f[i][1], s));
+    }
+}
+
 // Bound by the writing: 16384 tokens of 8 heads of 128 15.3 us from 4-bit pages (5.5 TB/s), 17.0 from fp8, 21.3 from bf16;
 // 65536 tokens of caches that are not in the last-level cache 72, 75 and 94 (4.7, 5.4 and 5.7 TB/s).
 template <CacheType TYPE, bool PAST>
@@ -102,15 +141,10 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheParams c, uint32_t th
     } else if constexpr (TYPE == CacheType::kFp8) {
       const uint2 kw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + at + d);
       const uint2 vw = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.v) + at + d);
-      auto values = [](uint2 w, float s) __attribute__((always_inline)) {
-        auto two = [s](uint32_t x, bool high) __attribute__((always_inline)) {
-          const v2f f = high ? __builtin_amdgcn_cvt_pk_f32_fp8(x, true) : __builtin_amdgcn_cvt_pk_f32_fp8(x, false);
-          return bf16_pair(f[0] * s, f[1] * s);
-        };
-        return make_uint4(two(w.x, false), two(w.x, true), two(w.y, false), two(w.y, true));
-      };
-      ko = values(kw, c.k_scale[head]);
-      vo = values(vw, c.v_scale[head]);
+      uint32_t y[8];
+      fp8_values(kw, vw, c.k_scale[head], c.v_scale[head], y);
+      ko = make_uint4(y[0], y[1], y[2], y[3]);
+      vo = make_uint4(y[4], y[5], y[6], y[7]);
     } else {
       const int64_t ea = slot.page * fp4_exp_page(c) + fp4_exp_group(c, head, d / kFp4Group) + slot.row;
       const uint32_t kw = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(c.k) + at + d / 2);

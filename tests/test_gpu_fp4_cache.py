@@ -479,6 +479,40 @@ def test_read(H, D, page, layout, kind):
     assert same(a, want[0]) and same(b, want[1])
 
 
+def _nearest_bf16(x):
+    """float64 -> the nearest bf16, ties to even, rounded once."""
+    f = x.float()
+    e, bits = x - f.double(), f.view(torch.int32)
+    away = torch.where(e != 0, torch.where((e > 0) == (x > 0), 1, -1), 0)      # whether |x| lies above or below |f|
+    odd = torch.where((bits & 1 == 0) & torch.isfinite(f), away, 0).int()
+    return (bits + odd).view(torch.float32).bfloat16()
+
+
+def test_read_fp8_is_rounded_once():
+    """code * scale has up to 28 bits.  Scales that bring one of a code's four odd mantissas next to the middle of two bf16
+    values, where its float32 value is the middle itself; the same among results below float32's normal numbers; and the range's
+    ends."""
+    H, D, page = 16, 256, 16
+    scales = [2.0 ** -120, 2.0 ** 118, 1e-38, 3.0, 0.0, 1.0]
+    for m in (9, 11, 13, 15):
+        for t in (1 + 2.0 ** -8, 1 + 3 * 2.0 ** -8, 1 + 201 * 2.0 ** -8):
+            near = np.float32(t * 16 / m)
+            scales += [float(near), float(np.nextafter(near, np.float32(2))), float(np.nextafter(near, np.float32(0)))]
+    scales += torch.tensor([0x00AE8B9C, 0x00E1C71C, 0x02064924, 0x02C80005, 0x00EB13B1, 0x00FBBBB8], dtype=torch.int32).view(torch.float32).tolist()
+    twice = 0
+    for i in range(0, len(scales), H):
+        s = torch.tensor(scales[i:i + H], dtype=torch.float32)
+        up, down = (torch.arange(256, dtype=torch.uint8).flip(f).expand(1, H, page, D).contiguous().view(FP8) for f in ((), 0))
+        cache = P.PagedCache(up.cuda(), down.cuda(), _int([[0]]), s.cuda(), s.flip(0).cuda())
+        k, v = P.kv_read(cache, _int([0]), _int([3]))
+        for got, c, sc in ((k, up, s), (v, down, s.flip(0))):
+            c = c[0, :, 3]
+            want = _nearest_bf16(c.double() * sc.double()[:, None])
+            twice += int(((c.float() * sc[:, None]).bfloat16() != want)[~want.isnan()].sum())
+            assert torch.equal(got[0].cpu().nan_to_num(7.0), want.nan_to_num(7.0))
+    assert len(scales) == 48 and twice > 40                # (so many that rounding twice would have shown)
+
+
 # ---- together ----
 
 def test_graph():
