@@ -455,8 +455,8 @@ typedef struct qwam_cache {
  * New keys and values into the pages: token t goes to position pos[t] of
  * sequence seq[t].  fp8: code = e4m3(clamp(x / scale[head], -448, 448)), to
  * nearest, ties to even.  fp4: E - 127 is the least e in [-123, 125] with
- * absmax <= 7 * 2^e over the group, code = e2m1(x / 2^e), to nearest, ties to the
- * even code, 6 at most; a group with an infinity or NaN gets E = 255.  A token
+ * absmax <= 7 * 2^e over the group (125 above 7 * 2^125), code = e2m1(x / 2^e), to
+ * nearest, ties to the even code, 6 at most; a group with an infinity or NaN gets E = 255.  A token
  * whose sequence or position does not exist, or whose page does not, is not
  * stored (a negative pos marks padding).  Two tokens of one call must not share
  * a slot.
@@ -471,7 +471,8 @@ qwam_status qwam_kv_append(const qwam_cache *c, int32_t tokens, const uint16_t *
 
 /*
  * Stored keys and values back as bf16: token t gets those of position pos[t] of
- * sequence seq[t], the value rounded once (bf16 and fp4: exactly the value), and
+ * sequence seq[t], the value rounded once (bf16 and fp4: exactly the value; fp4 with E
+ * of 253 or 254, which qwam_kv_append does not write: an infinity past bf16's range), and
  * zeros where qwam_kv_append would not store.
  *   tokens   in  as for qwam_kv_append
  *   seq, pos in  int32 [tokens]

@@ -479,6 +479,26 @@ def test_read(H, D, page, layout, kind):
     assert same(a, want[0]) and same(b, want[1])
 
 
+def test_read_of_every_scale():
+    """All sixteen codes at every scale byte, among them those that kv_append does not write: exactly the value down to the
+    smallest, an infinity past bf16's largest, NaN for 255."""
+    cache = P.new_cache(16, 1, 32, 1, 16, 16, FP4)
+    cache.table[0] = torch.arange(16)
+    codes = torch.arange(16, dtype=torch.uint8).repeat(2)
+    for c in (cache.k, cache.v):
+        c.view(torch.uint8)[:] = _pack(codes).cuda()
+    e = torch.arange(256, dtype=torch.uint8)
+    cache.k_scale.view(torch.uint8)[:, 0, 0] = e.view(16, 16).cuda()
+    cache.v_scale.view(torch.uint8)[:, 0, 0] = e.flip(0).view(16, 16).cuda()
+    k, v = P.kv_read(cache, _int([0] * 256), torch.arange(256, dtype=torch.int32).cuda())
+    grid = torch.from_numpy(np.concatenate((GRID, -GRID))).repeat(2)
+    for got, b in ((k, e), (v, e.flip(0))):
+        want = grid * torch.where(b == 255, NAN, 2.0 ** (b.double() - 127))[:, None]
+        want = torch.where(want.abs() >= 2.0 ** 128, want.sign() * INF, want).bfloat16()
+        got = got[:, 0].cpu()
+        assert torch.equal(got.nan_to_num(7.0, INF, -INF), want.nan_to_num(7.0, INF, -INF))
+
+
 def _nearest_bf16(x):
     """float64 -> the nearest bf16, ties to even, rounded once."""
     f = x.float()
