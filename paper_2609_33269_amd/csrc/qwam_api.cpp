@@ -479,6 +479,27 @@ bool rows_apart(int32_t rows, int64_t stride, int64_t width) {
   return rows <= 1 || stride >= width || stride <= -width;
 }
 
+// Whether rows of `width` elements, `rows` of them s apart from p on, and as many t apart from q on, have an element in common.
+// (Rows of one stride need one turn of the loop.  The places of others repeat after t / gcd(s, t) turns, and rows that fit the
+// memory have no more than half a million before that.)
+bool rows_meet(const uint16_t* p, int64_t s, const uint16_t* q, int64_t t, int32_t rows, int64_t width) {
+  typedef __int128 wide;                // (strides are any)
+  wide a = static_cast<wide>(reinterpret_cast<uintptr_t>(p) / 2), b = static_cast<wide>(reinterpret_cast<uintptr_t>(q) / 2);
+  wide sp = rows > 1 ? s : width, tq = rows > 1 ? t : width;
+  const wide last = rows - 1;
+  if (sp < 0) a += last * sp, sp = -sp;
+  if (tq < 0) b += last * tq, tq = -tq;
+  const wide end = b + last * tq + width;
+  wide first = -1;
+  for (wide i = a + width <= b ? (b - width - a) / sp + 1 : 0; i <= last && a + i * sp < end; ++i) {
+    const wide from = a + i * sp - b, place = from < 0 ? from + tq : from % tq;       // (from > -width)
+    if (place < width || place > tq - width) return true;
+    if (place == first) return false;
+    if (first < 0) first = place;
+  }
+  return false;
+}
+
 qwam_status check_attention(const char* fn, const qwam_cache* c, const qwam::CacheParams& cp, int32_t q_heads, int32_t max_len) {
   if (q_heads <= 0 || q_heads % c->heads != 0)
     return fail(QWAM_ERR_INVALID_ARG, "%s: q_heads must be a positive multiple of heads (got %d, %d)", fn, q_heads, c->heads);
@@ -610,6 +631,7 @@ qwam_status qwam_kv_read(const qwam_cache* c, int32_t tokens, const int32_t* seq
   if (!rows_apart(tokens, k_stride, width) || !rows_apart(tokens, v_stride, width))
     return fail(QWAM_ERR_INVALID_ARG, "%s: k_stride and v_stride must be at least heads * dim apart", fn);
   if (k == v) return fail(QWAM_ERR_INVALID_ARG, "%s: k and v are one output", fn);
+  if (rows_meet(k, k_stride, v, v_stride, tokens, width)) return fail(QWAM_ERR_INVALID_ARG, "%s: k and v overlap", fn);
   if ((s = check_device(fn)) != QWAM_OK) return s;
   return launched(fn, qwam::launch_kv_read(cp, type_of(c), tokens, seq, pos, k, k_stride, v, v_stride,
                                            static_cast<hipStream_t>(stream)));

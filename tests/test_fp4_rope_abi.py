@@ -52,6 +52,19 @@ def test_read_wants_two_outputs(lib):  # noqa: F811
         assert lib.qwam_last_error() == b"qwam_kv_read: k and v are one output"
 
 
+@pytest.mark.parametrize("n,k,ks,v,vs", [
+    (1, 0, 0, 120, 0), (1, 120, 0, 0, 0), (3, 0, 128, 8, 128), (3, 8, 128, 0, 128), (3, 0, 128, 256, 128), (3, 0, 128, 376, 128),
+    (3, 0, 256, 120, 256), (3, 128, 256, 8, 256), (3, 0, -128, -256, 128), (3, 256, -128, 0, 128), (3, 0, 256, 632, -256),
+    (5, 0, 256, 136, 384), (5, 0, 384, 264, 256), (4, 0, 1 << 40, 3 << 40, 128), (3, 0, 1 << 62, 8, 1 << 62), (100001, 0, 256, 128 + 256 * 100000, -136)])
+def test_read_wants_outputs_apart(lib, n, k, ks, v, vs):  # noqa: F811
+    """Rows of heads * dim = 128 elements, from element k and v on, ks and vs apart, that share one."""
+    at = 1 << 44
+    c = _cache4()
+    assert c.heads * c.dim == 128
+    assert _read(lib, c, n=n, k=at + 2 * k, ks=ks, v=at + 2 * v, vs=vs) == INVALID
+    assert lib.qwam_last_error() == b"qwam_kv_read: k and v overlap"
+
+
 def _plan(**kw):
     c = Q.QwamRopePlanC()
     base = dict(heads=4, dim=64, pairs=32, interleaved=0, axes=3, positions=6, pos_f32=0, x_f32=0, pos=FAKE, inv_freq=FAKE, axis=FAKE)

@@ -2,6 +2,7 @@
 exactly, paged_attention against float64 with the bound of the bf16 cache (every stored value is a bf16 value, so a bf16
 cache that holds them is the reference's)."""
 
+import ctypes
 import types
 
 import numpy as np
@@ -477,6 +478,31 @@ def test_read(H, D, page, layout, kind):
     a, b = P.kv_read(cache, _int(seq), _int(pos), stream=s)
     s.synchronize()
     assert same(a, want[0]) and same(b, want[1])
+
+
+@pytest.mark.parametrize("first,second", [((0, 128), (128, 128)), ((0, 256), (128, 256)), ((128, 256), (0, 256)), ((136, 384), (0, 384)),
+                                          ((0, 256), (7 * 256, 136)), ((0, 512), (128, 256)), ((128, 384), (0, 1152)), ((7 * 256, -256), (128, 256)),
+                                          ((7 * 256, -256), (128 + 7 * 256, -256))])
+def test_read_into_one_buffer(first, second):
+    """Outputs beside each other in one buffer, (element, stride) of each: columns of one matrix, rows in between, either sign; some
+    share a row and are refused, the others hold what separate outputs do and leave the rest as it was."""
+    H, D, n = 2, 64, 8
+    cache = _cache([20], H, D, 16)
+    seq, pos = _int([0] * n), _int(list(range(3, 3 + n)))
+    want = P.kv_read(cache, seq, pos)
+    elements = [torch.cat([torch.arange(128) + at + i * s for i in range(n)]) for at, s in (first, second)]
+    buf = torch.full((16384,), 5.0, dtype=torch.bfloat16, device="cuda")
+    c, lib = cache.c_struct(), Q.lib()
+    st = lib.qwam_kv_read(ctypes.byref(c), n, seq.data_ptr(), pos.data_ptr(), buf.data_ptr() + 2 * first[0], first[1], buf.data_ptr() + 2 * second[0],
+                          second[1], torch.cuda.current_stream().cuda_stream)
+    ref = torch.full((16384,), 5.0, dtype=torch.bfloat16, device="cuda")
+    if len(torch.cat(elements).unique()) < 2 * 128 * n:
+        assert st == 1 and lib.qwam_last_error() == b"qwam_kv_read: k and v overlap"
+    else:
+        assert st == 0
+        for e, w in zip(elements, want):
+            ref[e.cuda()] = w.flatten()
+    assert torch.equal(buf.nan_to_num(7.0), ref.nan_to_num(7.0))
 
 
 def test_read_of_every_scale():
