@@ -86,6 +86,8 @@ def _forward(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight,
     px = _q._req(x, "x", x.dtype, (T, D))
     pb = None if branch is None else _q._req(branch, "branch", torch.bfloat16, (T, D))
     xo, h = (None, None) if out is None else out
+    _q._on_current_device("block_norm", stream, x=x, branch=branch, gate=gate, post_weight=post_weight, weight=weight, scale=scale,
+                          shift=shift, **{"out[0]": xo, "out[1]": h})
     if branch is None:
         if xo is not None:
             raise ValueError("out[0] without a branch")
@@ -181,6 +183,8 @@ def block_norm_backward(dx_out: Optional[torch.Tensor], dh: torch.Tensor, x_out:
     ph = _q._req(dh, "dh", torch.bfloat16, (T, D))
     px = _q._req(x_out, "x_out", x_out.dtype, (T, D))
     pb = None if branch is None else _q._req(branch, "branch", torch.bfloat16, (T, D))
+    _q._on_current_device("block_norm_backward", stream, dx_out=dx_out, dh=dh, x_out=x_out, branch=branch, gate=gate,
+                          post_weight=post_weight, weight=weight, scale=scale, shift=shift)
     has = {"dbranch": branch is not None, "dgate": branch is not None and gate is not None,
            "dpost_weight": branch is not None and post_weight is not None, "dweight": weight is not None,
            "dscale": scale is not None, "dshift": shift is not None}
@@ -327,9 +331,11 @@ def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, s
     ps, pp = _q._req(seq, "seq", torch.int32, (n,)), _q._req(pos, "pos", torch.int32, (n,))
     _q._no_gradient("kv_read", **cache._values())
     shape = (n, c.heads, c.dim)
-    k, v = (_q._empty(shape, torch.bfloat16, cache.k.device, stream) for _ in range(2)) if out is None else out
+    k, v = (None, None) if out is None else out
     _q._no_gradient("kv_read", **{"out[0]": k, "out[1]": v})
     _q._on_current_device("kv_read", stream, seq=seq, pos=pos, table=cache.table, **{"out[0]": k, "out[1]": v}, **cache._values())
+    if out is None:
+        k, v = (_q._empty(shape, torch.bfloat16, cache.k.device, stream) for _ in range(2))
     st = _q.lib().qwam_kv_read(ctypes.byref(c), n, ps, pp, _rows(k, "out[0]", shape), k.stride(0) if n > 1 else 0,
                                _rows(v, "out[1]", shape), v.stride(0) if n > 1 else 0, _q._stream_ptr(stream))
     _q._check("qwam_kv_read", st)

@@ -79,6 +79,31 @@ bool data_of(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> sh
   return true;
 }
 
+// a GPU tensor; null for anything else
+const at::Tensor* tensor_of(PyObject* o) {
+  if (!THPVariable_Check(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return t.is_cuda() ? &t : nullptr;
+}
+
+// whether the kernels, which run on the current device, may take these (GPU tensors)
+bool on_current_device(std::initializer_list<const at::Tensor*> tensors) {
+  const auto now = c10::hip::current_device();
+  for (const at::Tensor* t : tensors)
+    if (t->get_device() != now) return false;
+  return true;
+}
+
+// the same of what may be None, or no tensor (which is refused elsewhere)
+bool on_current_device(std::initializer_list<PyObject*> objects) {
+  const auto now = c10::hip::current_device();
+  for (PyObject* o : objects) {
+    const at::Tensor* const t = o == nullptr ? nullptr : tensor_of(o);
+    if (t != nullptr && t->get_device() != now) return false;
+  }
+  return true;
+}
+
 // A layer's struct, and references that keep its tensors alive during the call.
 struct Layer {
   PyObject* held[kAttrs] = {};
@@ -117,6 +142,8 @@ struct Layer {
         !read_int(kHadamard, c.hadamard) || c.K <= 0 || c.group <= 0)
       return false;
     const int64_t G = c.K / c.group;
+    if (!on_current_device({held[kWq], held[kWs], held[kInv], held[kL1t], held[kL2t], held[kBias], held[kL1], held[kWsp], held[kL1f]}))
+      return false;
     return read(kWq, at::kByte, {c.N, c.K / 2}, c.wq, false) && read(kWs, at::kFloat, {G, c.N}, c.ws, false) &&
            read(kInv, at::kFloat, {c.K}, c.inv_smooth, matvec) &&
            ((matvec && c.r == 0) || (read(kL1t, at::kBFloat16, {c.r, c.K}, c.L1t, false) &&
@@ -200,7 +227,7 @@ PyObject* py_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor& xt = THPVariable_Unpack(args[1]);
   hipStream_t given_stream = nullptr;
   const bool explicit_stream = args[4] != Py_None;
-  if (explicit_stream && (!stream_of(args[4], &given_stream) || xt.get_device() != c10::hip::current_device()))
+  if (!on_current_device({args[1], given[0], given[1], given[2]}) || (explicit_stream && !stream_of(args[4], &given_stream)))
     return none_or_error();
   Held xq, xs, t;
   void *pq, *ps, *pt;
@@ -244,6 +271,7 @@ PyObject* py_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (M < 0 || !L.load(args[0]) || !data_of(args[1], at::kByte, {M, L.c.K / 2}, &xq) ||
       !data_of(args[2], at::kFloat, {L.c.K / L.c.group, M}, &xs) || !data_of(args[3], at::kBFloat16, {M, L.c.r}, &t))
     return none_or_error();
+  if (!on_current_device({args[1], args[2], args[3], args[4]})) Py_RETURN_NONE;
   Held y;
   if (!output(args[4], THPVariable_Unpack(args[1]), at::kBFloat16, M, L.c.N, &y.o, &py)) return none_or_error();
   void* stream = current_stream();
@@ -266,6 +294,7 @@ PyObject* py_layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t M = rows_of(args[1]);
   void *x, *py;
   if (M < 0 || !L.load(args[0]) || !data_of(args[1], at::kBFloat16, {M, L.c.K}, &x)) return none_or_error();
+  if (!on_current_device({args[1], args[2]})) Py_RETURN_NONE;
   Held y;
   if (!output(args[2], THPVariable_Unpack(args[1]), at::kBFloat16, M, L.c.N, &y.o, &py)) return none_or_error();
   void* stream = current_stream();
@@ -305,7 +334,9 @@ PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t M = rows_of(args[1]);
   void *x, *py;
   if (M < 0 || !L.load(args[0], true) || !data_of(args[1], at::kBFloat16, {M, L.c.K}, &x)) return none_or_error();
-  if (tracked({args[1], args[2], L.held[kWs], L.held[kInv], L.held[kL1t], L.held[kL2t], L.held[kBias], L.held[kL1f]})) Py_RETURN_NONE;
+  if (tracked({args[1], args[2], L.held[kWs], L.held[kInv], L.held[kL1t], L.held[kL2t], L.held[kBias], L.held[kL1f]}) ||
+      !on_current_device({args[1], args[2]}))
+    Py_RETURN_NONE;
   const at::Tensor& xt = THPVariable_Unpack(args[1]);
   Held y;
   if (!output(args[2], xt, at::kBFloat16, M, L.c.N, &y.o, &py)) return none_or_error();
@@ -322,21 +353,6 @@ PyObject* py_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   written({args[2]});
   return y.release();
   END_HANDLE_TH_ERRORS
-}
-
-// a GPU tensor; null for anything else
-const at::Tensor* tensor_of(PyObject* o) {
-  if (!THPVariable_Check(o)) return nullptr;
-  const at::Tensor& t = THPVariable_Unpack(o);
-  return t.is_cuda() ? &t : nullptr;
-}
-
-// whether the kernels, which run on the current device, may take these (GPU tensors)
-bool on_current_device(std::initializer_list<const at::Tensor*> tensors) {
-  const auto now = c10::hip::current_device();
-  for (const at::Tensor* t : tensors)
-    if (t->get_device() != now) return false;
-  return true;
 }
 
 // the arguments that the norm's calls share, from `a`: norm ("rms" or "layer"), eps, residual_scale, gate, post_norm, post_weight,
@@ -394,7 +410,9 @@ PyObject* py_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   void* branch = nullptr;
   if (!norm_of(args + 2, T, D, f32, p) || (args[1] != Py_None && !data_of(args[1], at::kBFloat16, {T, D}, &branch)))
     return none_or_error();
-  if (tracked({args[0], args[1], args[5], args[7], args[8], args[9], args[10]})) Py_RETURN_NONE;
+  if (tracked({args[0], args[1], args[5], args[7], args[8], args[9], args[10]}) ||
+      !on_current_device({args[0], args[1], args[5], args[7], args[8], args[9], args[10]}))
+    Py_RETURN_NONE;
   const at::Tensor h = at::empty({T, D}, x->options().dtype(at::kBFloat16));
   const at::Tensor xo = branch != nullptr ? at::empty({T, D}, x->options()) : at::Tensor();
   const qwam_status st = g_norm(&p, x->data_ptr(), static_cast<const uint16_t*>(branch), branch != nullptr ? xo.data_ptr() : nullptr,
@@ -423,6 +441,7 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return none_or_error();
   for (Py_ssize_t i = 0; i < nargs; ++i)
     if (tangent(args[i])) Py_RETURN_NONE;      // (false of what is no tensor)
+  if (!on_current_device({args[0], args[1], args[2], args[3], args[7], args[9], args[10], args[11], args[12]})) Py_RETURN_NONE;
   const int64_t need = g_norm_workspace(&p);
   if (need < 0) Py_RETURN_NONE;
   at::Tensor g[kGrads];

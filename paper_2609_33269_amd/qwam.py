@@ -205,6 +205,9 @@ class PackedLayer:
     wsp: Optional[torch.Tensor] = None    # int32 [K/group][N]: ws as bf16 pieces hi | lo << 16 (asp_linear reads it)
     L1f: Optional[torch.Tensor] = None    # bf16 [K/64][r/16][2][64][8]: L1 in fragment order (the activation calls read it)
 
+    def _tensors(self) -> dict:
+        return {"layer." + n: getattr(self, n) for n in ("wq", "ws", "inv_smooth", "L1t", "L2t", "bias", "L1", "wsp", "L1f")}
+
     def c_struct(self, matvec: bool = False) -> QwamLayerC:
         G = self.K // self.group
         c = QwamLayerC()
@@ -229,6 +232,7 @@ def pack_weights(R: torch.Tensor, smooth: torch.Tensor, stream=None, group: int 
     (wq uint8 [N][K/2], ws float32 [K/group][N], wsp int32 [K/group][N] (the
     scales as bf16 pieces hi | lo << 16), inv_smooth float32 [K])."""
     N, K = R.shape
+    _on_current_device("pack_weights", stream, R=R, smooth=smooth)
     dev = R.device
     wq = torch.empty((N, K // 2), dtype=torch.uint8, device=dev)
     ws = torch.empty((K // group, N), dtype=torch.float32, device=dev)
@@ -315,6 +319,8 @@ def _quantize(deflated: bool, name: str, layer: PackedLayer, x: torch.Tensor, st
             return done
     M = x.shape[0]
     dev = x.device
+    _on_current_device(name[len("qwam_"):], stream, x=x, **layer._tensors(),
+                       **{f"out[{i}]": t for i, t in enumerate(out or ())})
     if out is None:
         xq = torch.empty((M, layer.K // 2), dtype=torch.uint8, device=dev)
         xs = torch.empty((layer.K // layer.group, M), dtype=torch.float32, device=dev)
@@ -349,6 +355,7 @@ def asp_linear(layer: PackedLayer, xq: torch.Tensor, xs: torch.Tensor, t: torch.
             return y
     M = xq.shape[0]
     G = layer.K // layer.group
+    _on_current_device("asp_linear", stream, xq=xq, xs=xs, t=t, out=out, **layer._tensors())
     y = torch.empty((M, layer.N), dtype=torch.bfloat16, device=xq.device) if out is None else out
     c = layer.c_struct()
     st = lib().qwam_asp_linear(ctypes.byref(c), M, _req(xq, "xq", torch.uint8, (M, layer.K // 2)),
@@ -378,6 +385,8 @@ def asp_layer(layer: PackedLayer, x: torch.Tensor, out=None, act_out=None, strea
                 _check("qwam_asp_layer", y)
             return y
     M = x.shape[0]
+    _on_current_device("asp_layer", stream, x=x, out=out, **layer._tensors(),
+                       **{f"act_out[{i}]": t for i, t in enumerate(act_out or ())})
     y = torch.empty((M, layer.N), dtype=torch.bfloat16, device=x.device) if out is None else out
     c = layer.c_struct()
     if act_out is None:
@@ -402,10 +411,14 @@ def _need(fn: str, nbytes: int) -> int:
 
 
 def _on_current_device(fn: str, stream, **tensors) -> None:
-    """For a call whose kernels run on the current device: refuses tensors and streams of another."""
+    """For a call whose kernels run on the current device: refuses tensors and streams of another.  (Tensors of no GPU are
+    refused where the argument is read.)"""
+    there = {n: t for n, t in tensors.items() if isinstance(t, torch.Tensor) and t.device.type == "cuda"}
+    if not there and not isinstance(stream, torch.cuda.Stream):
+        return
     now = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.device.type == "cuda" and t.device.index != now:
+    for name, t in there.items():
+        if t.device.index != now:
             raise ValueError(f"{name} is on {t.device}, {fn} runs on the current device cuda:{now}")
     if isinstance(stream, torch.cuda.Stream) and stream.device.index != now:
         raise ValueError(f"stream is of {stream.device}, {fn} runs on the current device cuda:{now}")
@@ -445,6 +458,7 @@ def asp_matvec(layer: PackedLayer, x: torch.Tensor, out: Optional[torch.Tensor] 
     px = _req(x, "x", torch.bfloat16, (M, layer.K))
     _no_gradient("asp_matvec", x=x, out=out, ws=layer.ws, inv_smooth=layer.inv_smooth, L1t=layer.L1t, L2t=layer.L2t, bias=layer.bias,
                  L1f=layer.L1f)
+    _on_current_device("asp_matvec", stream, x=x, out=out, **layer._tensors())
     need = _need("qwam_asp_matvec", lib().qwam_asp_matvec_workspace(ctypes.byref(c), M))
     y = _empty((M, layer.N), torch.bfloat16, x.device, stream) if out is None else out
     ws = _workspace(need, x.device, stream)
@@ -459,6 +473,7 @@ def debug_group_partials(layer: PackedLayer, xq: torch.Tensor, stream=None) -> t
     """qwam_debug_group_partials: -> P int32 [M][N][K/group] (exact integer partials)."""
     M = xq.shape[0]
     G = layer.K // layer.group
+    _on_current_device("debug_group_partials", stream, xq=xq, **layer._tensors())
     P = torch.empty((M, layer.N, G), dtype=torch.int32, device=xq.device)
     c = layer.c_struct()
     st = lib().qwam_debug_group_partials(ctypes.byref(c), M,
@@ -472,6 +487,7 @@ def aog_accumulate(gT: torch.Tensor, A: torch.Tensor, stream=None) -> torch.Tens
     """qwam_aog_accumulate: A float32 [d][d] += gT gT^T for a batch of probe
     VJPs gT bf16 [d][n] (row c = channel c).  Returns A (updated in place)."""
     d, n = gT.shape
+    _on_current_device("aog_accumulate", stream, gT=gT, A=A)
     st = lib().qwam_aog_accumulate(d, n, _req(gT, "gT", torch.bfloat16, (d, n)),
                                    _req(A, "A", torch.float32, (d, d)), _stream_ptr(stream))
     _check("qwam_aog_accumulate", st)
@@ -495,6 +511,7 @@ def aog_protected_basis(A: torch.Tensor, r: int, iters: int = 20, scale: float =
     `workspace` (uint8, at least aog_protected_basis_workspace(d, r) bytes) is
     allocated here when not given."""
     d = A.shape[0]
+    _on_current_device("aog_protected_basis", stream, A=A, lam=lam, workspace=workspace)
     need = aog_protected_basis_workspace(d, r)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=A.device)
