@@ -343,6 +343,93 @@ def test_an_infinite_query_before_one_key(D, G):
             assert (got == 1).all()
 
 
+FORMS = [(32, 1), (32, 33), (64, 3), (64, 8), (96, 20), (128, 4), (128, 16), (160, 5), (256, 2), (256, 17)]
+
+
+@pytest.mark.parametrize("D,G", FORMS)
+def test_missing_pages_and_limits_of_every_form(D, G):
+    lengths = [200, 200, 64, 200, 5000, -3, 700]
+    cache = _cache([200, 200, 64, 200, 200, 16, 700], 2, D, 16, width=44, junk=120)
+    cache.table[0, 3] = -1
+    cache.table[1, 0] = cache.k.shape[0]
+    cache.table[1, 12] = 2 ** 31 - 1
+    cache.table[2, :] = -2 ** 31
+    cache.table[3, 4:9] = 10 ** 6
+    cache.table[6, 1:40:3] = -1
+    q, L, ref = _q(7, 2 * G, D), _int(lengths), _as_bf16(cache)
+    _check(ref, q, lengths, P.paged_attention(cache, q, L))
+    for n in (1, 50, 129, 704):
+        _check(ref, q, lengths, P.paged_attention(cache, q, L, max_len=n), max_len=n)
+    starts = [0, 199, 3, 70, 190, 0, 333]
+    _check(ref, q, lengths, P.paged_attention(cache, q, L, starts=_int(starts)), starts)
+
+
+@pytest.mark.parametrize("length", [40, 3000])
+@pytest.mark.parametrize("D,G", FORMS)
+def test_nan_groups_of_every_form(D, G, length):
+    cache = _cache([length] * 2, 2, D, 64)
+    q, L, last = _q(2, 2 * G, D), _int([length] * 2), D // 32 - 1
+    want = P.paged_attention(cache, q, L)
+    page = int(cache.table[1, 0])
+    for place in (0, 5, 39):
+        scale = cache.v_scale.view(torch.uint8)[page, 1, last, place].clone()
+        cache.v_scale.view(torch.uint8)[page, 1, last, place] = 255
+        got = P.paged_attention(cache, q, L)
+        assert got[1, G:, 32 * last:].isnan().all()
+        got[1, G:, 32 * last:] = want[1, G:, 32 * last:]
+        assert torch.equal(got, want)
+        cache.v_scale.view(torch.uint8)[page, 1, last, place] = scale
+        scale = cache.k_scale.view(torch.uint8)[page, 0, last, place].clone()
+        cache.k_scale.view(torch.uint8)[page, 0, last, place] = 255
+        got = P.paged_attention(cache, q, L)
+        assert got[1, :G].isnan().all()
+        got[1, :G] = want[1, :G]
+        assert torch.equal(got, want)
+        # a start behind it: it has no effect
+        after = _int([0, place + 1])
+        seen = P.paged_attention(cache, q, L, starts=after)
+        cache.k_scale.view(torch.uint8)[page, 0, last, place] = scale
+        assert torch.equal(seen, P.paged_attention(cache, q, L, starts=after))
+
+
+@pytest.mark.parametrize("D,G", FORMS)
+def test_rows_that_run_backwards_in_every_form(D, G):
+    lengths, H, page = [100, 3, 70, 1200], 3, 16
+    cache = _cache(lengths, H, D, page)
+    k, v = (c.view(torch.uint8).flip(0, 1, 2).contiguous() for c in (cache.k, cache.v))
+    q, L, Hq, reach = _q(4, G * H, D), _int(lengths), G * H, cache.table.shape[1] * page
+    want = P.paged_attention(cache, q, L)
+    c, lib = cache.c_struct(), Q.lib()
+    last = k.numel() - D // 2
+    c.k, c.v = k.data_ptr() + last, v.data_ptr() + last
+    c.page_stride, c.head_stride, c.row_stride = -H * page * D // 2, -page * D // 2, -D // 2
+    out = torch.full_like(want, NAN)
+    need = lib.qwam_paged_attention_workspace(ctypes.byref(c), Hq, reach)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    assert need >= 0 and lib.qwam_paged_attention(ctypes.byref(c), Hq, q.data_ptr(), q.stride(0), L.data_ptr(), None, reach, D ** -0.5,
+                                                  out.data_ptr(), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("D,G,H", [(32, 1, 1), (128, 3, 2), (64, 17, 1)])
+def test_more_ranges_than_a_grid_dimension(D, G, H):
+    """A table past 2^27 positions, nearly empty: what its few pages hold, the last range's among them, as from a table of them alone.
+    Its ranges (4096 positions each) are more than 32768."""
+    page, width, B = 4096, 32768 + 5, 2
+    near = _cache([5 * page - 100, 3 * page - 1], H, D, page)
+    far = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    at = ([0, 16000, 32767, 32768, width - 1], [1, 32766, 32769])
+    for b, places in enumerate(at):
+        far[b, places] = near.table[b, :len(places)]
+    L = _int([width * page - 100, 32770 * page - 1])
+    q = _q(B, G * H, D)
+    for seqs in ([0, 1], [0], [1]):
+        cache = P.PagedCache(near.k, near.v, far[seqs].contiguous(), near.k_scale, near.v_scale)
+        small = P.PagedCache(near.k, near.v, near.table[seqs].contiguous(), near.k_scale, near.v_scale)
+        assert Q.lib().qwam_paged_attention_workspace(ctypes.byref(cache.c_struct()), G * H, width * page) >= (width - 1) * len(seqs) * G * H * (D + 2) * 4
+        _check(_as_bf16(small), q[seqs], [[5 * page - 100, 3 * page - 1][b] for b in seqs], P.paged_attention(cache, q[seqs], L[seqs].contiguous()))
+
+
 # ---- append ----
 
 @pytest.mark.parametrize("layout", ["heads", "rows", "both"])

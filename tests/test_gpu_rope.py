@@ -214,6 +214,25 @@ def test_many_values():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,dims", [(64, (32,)), (66, (16, 16)), (128, (20, 22, 22)), (67, (32,)), (96, (30, 4))])
+def test_large_calls_that_turn_in_part(D, dims, interleaved, f32):
+    """2^18 pairs and more, where halves of bf16 take two pairs a thread: the channels behind them stay as they are, into a new
+    output, beside other columns and in place."""
+    plan = P.rope_plan(dims, interleaved=interleaved)
+    T, H = 1100, 17
+    assert T * H * sum(dims) // 2 >= 2 ** 18
+    x, pos = _x(T, H, D, f32, D), _pos(T // 2, len(dims))
+    want = P.rope(x, pos, plan)
+    _check(x, pos, plan, want)
+    wide = torch.full((T, H * D + 8), 5.0, dtype=x.dtype, device="cuda")
+    out = wide[:, 4:4 + H * D].view(T, H, D)
+    assert torch.equal(P.rope(x, pos, plan, out=out), want)
+    assert (wide[:, :4] == 5).all() and (wide[:, 4 + H * D:] == 5).all()
+    assert P.rope(x, pos, plan, out=x) is x and torch.equal(x, want)
+
+
 # ---- gradients ----
 
 @pytest.mark.parametrize("f32", [False, True])
