@@ -98,7 +98,7 @@ def _forward(x, branch, norm, eps, residual_scale, gate, post_norm, post_weight,
     st = _q.lib().qwam_block_norm(ctypes.byref(c), px, pb, None if xo is None else _q._req(xo, "out[0]", x.dtype, (T, D)),
                                   _q._req(h, "out[1]", torch.bfloat16, (T, D)), _q._stream_ptr(stream))
     _q._check("qwam_block_norm", st)
-    _q._written(*(out or ()))
+    _q._written(*(() if out is None else out))
     return xo, h
 
 
@@ -151,7 +151,7 @@ def block_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, *, norm: 
             return done
     _q._no_tangent("block_norm", x=x, branch=branch, gate=gate, post_weight=post_weight, weight=weight, scale=scale, shift=shift)
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
-                                       for t in (x, branch, gate, post_weight, weight, scale, shift, *(out or ()))):
+                                       for t in (x, branch, gate, post_weight, weight, scale, shift, *(() if out is None else out))):
         if out is not None or stream is not None:
             raise ValueError("block_norm under autograd takes neither out nor stream")
         return _BlockNorm.apply(x, branch, gate, post_weight, weight, scale, shift, norm, eps, residual_scale, post_norm)
@@ -339,7 +339,7 @@ def kv_read(cache: PagedCache, seq: torch.Tensor, pos: torch.Tensor, out=None, s
     st = _q.lib().qwam_kv_read(ctypes.byref(c), n, ps, pp, _rows(k, "out[0]", shape), k.stride(0) if n > 1 else 0,
                                _rows(v, "out[1]", shape), v.stride(0) if n > 1 else 0, _q._stream_ptr(stream))
     _q._check("qwam_kv_read", st)
-    _q._written(*(out or ()))
+    _q._written(*(() if out is None else out))
     return k, v
 
 

@@ -320,7 +320,7 @@ def _quantize(deflated: bool, name: str, layer: PackedLayer, x: torch.Tensor, st
     M = x.shape[0]
     dev = x.device
     _on_current_device(name[len("qwam_"):], stream, x=x, **layer._tensors(),
-                       **{f"out[{i}]": t for i, t in enumerate(out or ())})
+                       **{f"out[{i}]": t for i, t in enumerate(() if out is None else out)})
     if out is None:
         xq = torch.empty((M, layer.K // 2), dtype=torch.uint8, device=dev)
         xs = torch.empty((layer.K // layer.group, M), dtype=torch.float32, device=dev)
@@ -386,7 +386,7 @@ def asp_layer(layer: PackedLayer, x: torch.Tensor, out=None, act_out=None, strea
             return y
     M = x.shape[0]
     _on_current_device("asp_layer", stream, x=x, out=out, **layer._tensors(),
-                       **{f"act_out[{i}]": t for i, t in enumerate(act_out or ())})
+                       **{f"act_out[{i}]": t for i, t in enumerate(() if act_out is None else act_out)})
     y = torch.empty((M, layer.N), dtype=torch.bfloat16, device=x.device) if out is None else out
     c = layer.c_struct()
     if act_out is None:
@@ -399,7 +399,7 @@ def asp_layer(layer: PackedLayer, x: torch.Tensor, out=None, act_out=None, strea
     st = lib().qwam_asp_layer(ctypes.byref(c), M, _req(x, "x", torch.bfloat16, (M, layer.K)),
                               _req(y, "y", torch.bfloat16, (M, layer.N)), pq, ps, pt, _stream_ptr(stream))
     _check("qwam_asp_layer", st)
-    _written(out, *(act_out or ()))
+    _written(out, *(() if act_out is None else act_out))
     return y
 
 
