@@ -114,8 +114,8 @@ struct Span {
 // Over bf16 and fp8 pages a range is as long as the call laid out for the longest contexts.  Over 4-bit pages a context below an
 // eighth of those, or the only one of a call, has shorter ones: as many as the call has for the longest (a quarter of that
 // in a batch, whose sequences share the chip), none shorter than the call's least.  One context of 4096 positions in a table
-// that reaches 131072 takes 8.1 us, with the call's ranges 20.4; four of 60 to 9000 there 12.1 and 21.8 (8 x 3 heads of 128).
-// As many for every sequence of a batch took 8 ragged ones up to 16000, 16 x 2 heads of 256, from 39.7 to 47.4.
+// that reaches 131072 takes 8.4 us, with the call's ranges 20.6; four of 60 to 9000 there 12.8 and 22.6 (8 x 3 heads of 128).
+// As many for every sequence of a batch took 8 ragged ones up to 16000, 16 x 2 heads of 256, from 41.1 to 48.4.
 template <bool FP4>
 __device__ __forceinline__ Span span_of(const AttnArgs& a, int b) {
   const int64_t reach = static_cast<int64_t>(a.c.table_width) << a.c.page_bits;
@@ -437,16 +437,17 @@ __global__ __launch_bounds__(64 * kAttnWaves, FP8 && DP == 128 ? 4 : 1) void pag
 //     to 4 query heads (the narrow form) the 16 columns of that product hold each head four times, for both pieces of its
 //     weights and for even and odd channels: the operand's slots are then (key, parity) as the conversion leaves them,
 //     and a lane needs no transposing.  The same four lanes share a head's 64 weights, 16 each.  (8 x 3 heads of 128, a
-//     turn of a wave 310 instead of 460 instructions; 16 ragged contexts up to 4096 12.1 us, in the wide form 13.5; 4 up
-//     to 16384, 16 heads of 64, 13.9, 16.2.)
+//     turn of a wave 370 instead of 455 instructions; 16 ragged contexts up to 4096 12.7 us, in the wide form 14.0; 4 up
+//     to 16384, 16 heads of 64, 15.5 in either.)
 //   * Where a block of 16 positions lies is computed once, a lane each, and handed out by readlane; addresses are a
 //     scalar base and a lane's 32-bit offset that stays.
 //   * A new maximum counts from 2^kSlack above the old one on: weights stay below 2^kSlack, and o and the sum are
 //     rescaled in a few turns rather than in most (with 16 heads, one of them has a new maximum in most turns).
-// Measured, 8 x 3 heads of 128: two contexts up to 131072 41.4 us (38.3 of it this kernel, 4.6 TB/s), one of 32768 13.4 us, 16
-// ragged ones up to 4096 13.0 us (two turns of their workgroups of 1 us each behind launch, lengths, table and first keys,
-// and a join of 3.5); one of 77, 16 heads of 64, 4.5 us in a graph; windows of 6001 positions of 5 sequences, 2 x 16 heads
-// of 256, 13.2 us.
+// Measured (calls among others), 8 x 3 heads of 128: two contexts up to 131072 40.6 us (37.6 of it this kernel, 4.7 TB/s), one of
+// 32768 13.2 us, 16 ragged ones up to 4096 12.7 us, 11.9 in a graph (two turns of their workgroups of 1 us each behind launch,
+// lengths, table and first keys, and a join of 3.8); one of 77, 16 heads of 64, 4.7 us, 4.1 in a graph; windows of 6001
+// positions of 5 sequences, 2 x 16 heads of 256, 13.1 us.  Above 16 query heads each tile of 16 reads the pages: 8 contexts of
+// 4096, 8 key heads of 128, 17.7 us for 16 query heads each, 24.9 for 32 and 35.8 for 64; one of 65536 20.6, 32.0 and 49.5.
 constexpr float kSlack = 8.0f;
 constexpr int kNarrow = 4;              // query heads of a key head that the narrow form takes
 constexpr int kGridRanges = 32768;      // ranges in the grid's last dimension; more of them stand behind the heads
@@ -578,7 +579,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
   const bool has_v = FULL || DC * r < D;
 
   uint32_t kr[BL][NK][KW];
-  // values come a turn ahead too (in the wide form of 64 channels 64 ragged contexts up to 4096 24.7 us, without 25.6; of wider
+  // values come a turn ahead too (in the wide form of 64 channels 64 ragged contexts up to 4096, 4 x 8 heads, 17.1 us, without 17.7; of wider
   // heads it changes nothing or costs a wave)
   constexpr bool V_AHEAD = NARROW || DP == 64;
   uint32_t ke[BL][NK], va[BL][4][NV], vea[BL], vb[BL][4][NV], veb[BL];
@@ -807,8 +808,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, DP == 256 ? 2 : 3) void paged_atte
 // the ranges of a sequence into one result: one workgroup per (sequence, query
 // head, 4 LR channels of o), the ranges dealt out over its groups of LR lanes.
 // (4-bit pages: the first ranges are requested before the maximum is known, and
-// the groups of a wave are added in it: 512 ranges of two contexts up to 131072
-// 53 us in all, 67 without.)
+// the groups of a wave are added in it: two contexts up to 131072 40.4 us in all,
+// 41.2 without.)
 template <int LR, CacheType TYPE>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
   constexpr bool FP8 = TYPE == CacheType::kFp8, FP4 = TYPE == CacheType::kFp4;
@@ -903,10 +904,10 @@ struct Plan {
 
 constexpr int kOneRange = 512;
 
-// 4-bit pages: a call's ranges of turns of a workgroup.  One range up to 1024 positions (64 x 8 heads of 1024 12.0 us, in
-// two ranges 15.5; one sequence of 16 heads of 64 7.6, in four 7.7).  Else workgroups for every CU once for one sequence
-// (one context of 32768 13.6 us; for twice as many 14.4, for half 17.6), and as often as there are sequences up to four times,
-// whose lengths differ (32 ragged ones up to 8192 20.4 us, with half as many 23.4); no more than 256 ranges to join, and
+// 4-bit pages: a call's ranges of turns of a workgroup.  One range up to 1024 positions (64 x 8 heads of 1024 15.0 us, in
+// two ranges 18.8; one sequence of 16 heads of 64 6.9, in four 9.0).  Else workgroups for every CU once for one sequence
+// (one context of 32768 13.2 us; for twice as many 13.9, for half 16.4), and as often as there are sequences up to four times,
+// whose lengths differ (32 ragged ones up to 8192 26.6 us, with half as many 32.2); no more than 256 ranges to join, and
 // partial results at most half of what is read.
 Plan plan_of_fp4(const CacheParams& c, int q_heads, int max_len) {
   auto up = [](int64_t v, int64_t step) { return (v + step - 1) / step * step; };
@@ -916,7 +917,7 @@ Plan plan_of_fp4(const CacheParams& c, int q_heads, int max_len) {
   int64_t n = (rows * max_len + want - 1) / want;
   for (const int64_t least : {(static_cast<int64_t>(max_len) + 255) / 256, 16 * heads, int64_t(kTurn)}) n = n < least ? least : n;
   n = up(n, kTurn) > kMaxChunk ? kMaxChunk : up(n, kTurn);
-  // (512 rows of 500 positions in a table for 32768: one range each 11.2 us, two 19.7)
+  // (512 rows of 500 positions in a table for 32768: one range each 12.9 us, two 14.9)
   return {static_cast<int>(n), static_cast<int>((max_len + n - 1) / n), rows < 256 ? kTurn : 4 * kTurn};
 }
 
@@ -952,7 +953,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
     grid = dim3(static_cast<unsigned>(a.c.heads * ((a.group + 15) / 16) * high), static_cast<unsigned>(a.c.seqs),
                 static_cast<unsigned>(a.splits < kGridRanges ? a.splits : kGridRanges));
     kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, false> : paged_attention_fp4_kernel<DP, false, false>;
-    // (heads above 128: the narrow form is no faster, 32768 positions of 8 of 256 18.7 us to 18.8, and has too many registers)
+    // (heads above 128 have too many registers for the narrow form: it spilled)
     if constexpr (DP <= 128) {
       if (a.group <= kNarrow) kernel = a.c.dim == DP ? paged_attention_fp4_kernel<DP, true, true> : paged_attention_fp4_kernel<DP, false, true>;
     }

@@ -96,8 +96,8 @@ __device__ __forceinline__ float product_to_odd(float f, float scale) {
 }
 
 // e4m3 codes of keys and values times their scales as bf16, rounded once.  The float32 products serve where none of them is the
-// middle of two bf16 values, which is where a second rounding can go wrong.  (16384 tokens of 8 heads of 128 17.3 us; without the test
-// for one 17.0, with every product to odd 20.9.)
+// middle of two bf16 values, which is where a second rounding can go wrong.  (65536 tokens of 8 heads of 128 73.6 us; without
+// the test for one 71.4, with every product to odd 84.5.)
 __device__ __forceinline__ void fp8_values(uint2 kw, uint2 vw, float ks, float vs, uint32_t (&y)[8]) {
   typedef short v2i16 __attribute__((ext_vector_type(2)));
   v2f f[8];
@@ -123,8 +123,8 @@ __device__ __forceinline__ void fp8_values(uint2 kw, uint2 vw, float ks, float v
     }
 }
 
-// Bound by the writing: 16384 tokens of 8 heads of 128 15.3 us from 4-bit pages (5.5 TB/s), 17.0 from fp8, 21.3 from bf16;
-// 65536 tokens of caches that are not in the last-level cache 72, 75 and 94 (4.7, 5.4 and 5.7 TB/s).
+// Bound by the writing: 16384 tokens of 8 heads of 128 15.3 us from 4-bit pages (5.5 TB/s), 17.1 from fp8, 21.3 from bf16;
+// 65536 tokens of caches that are not in the last-level cache 69, 76 and 93 (4.9, 5.3 and 5.8 TB/s).
 template <CacheType TYPE, bool PAST>
 __global__ __launch_bounds__(256) void kv_read_kernel(CacheParams c, uint32_t threads, int run, const int32_t* seq, const int32_t* pos,
                                                       uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride) {
